@@ -492,6 +492,51 @@ gnn_status gnn_softmax_ce_workspace_size(int64_t b, size_t *bytes);
 gnn_status gnn_softmax_ce(const float *logits, int64_t b, int64_t c, const int64_t *labels, const int64_t *targets,
                           float *g_out, float *loss_out, void *ws, size_t ws_bytes, gnn_stream s);
 
+/* ------------------------------------------------------------------------
+ * Layer normalisation of the rows of an activation matrix, between the
+ * layers of a deep or residual model.  With mu_i and v_i the mean and the
+ * (biased) variance of row x_i,
+ *   rstd_i = 1 / sqrt(v_i + eps),  h = (x - mu) rstd,  y = gamma h + beta.
+ *   x      [device] cap_m x f of xdt (GNN_F32 or GNN_BF16), f <= GNN_MAX_DIM.
+ *   m_dev  [device] int64 row count, or NULL to use cap_m; rows at or past
+ *          it are neither read nor written.
+ *   gamma, beta  [device] fp32 f, or NULL (1 and 0).
+ *   eps    >= 0.  With eps = 0 a constant row has an infinite rstd and NaN
+ *          outputs.
+ *   y      [device] cap_m x f of ydt; may be x itself when ydt == xdt.
+ *   mean, rstd  [device] fp32 cap_m each, or NULL when no backward follows.
+ * The statistics are fp32: the mean first, then the squares of the distances
+ * from it, so rows far from zero lose nothing.  A NaN or an infinity makes
+ * its own row NaN and no other.  Errors: GNN_EINVAL for bad sizes, eps,
+ * NULL or misaligned (to the element) pointers; GNN_EUNSUPPORTED for other
+ * dtypes. */
+gnn_status gnn_layer_norm_fwd(const void *x, gnn_dtype xdt, const int64_t *m_dev, int64_t cap_m, int64_t f,
+                              const float *gamma, const float *beta, float eps, void *y, gnn_dtype ydt, float *mean,
+                              float *rstd, gnn_stream s);
+
+/* Its gradients from g = dLoss/dy, with q = gamma g and h as above:
+ *   d_x    = rstd (q - mean_j q - h mean_j (q h)) + d_res
+ *   dgamma = sum over the rows of g h,  dbeta = sum over the rows of g.
+ *   g, d_res, d_x [device] cap_m x f of gdt (GNN_F32 or GNN_BF16); d_res NULL:
+ *          no term (it is the gradient that reaches x along a skip
+ *          connection); d_x NULL: not wanted; d_x may be g or d_res itself.
+ *   mean, rstd  as gnn_layer_norm_fwd wrote them.
+ *   dgamma, dbeta [device] fp32 f, overwritten, or NULL (not wanted); with no
+ *          rows they are 0.
+ *   ws     [device] 256-byte aligned workspace of
+ *          gnn_layer_norm_bwd_workspace_size bytes: the row groups' partial
+ *          sums of dgamma and dbeta, added by a second kernel in a fixed
+ *          order, so results are bitwise reproducible.  It may be NULL when
+ *          neither is wanted.  No state is kept in it between calls; calls
+ *          sharing it must not overlap.
+ * Other arguments and errors as gnn_layer_norm_fwd; GNN_ESIZE when the
+ * workspace is too small. */
+gnn_status gnn_layer_norm_bwd_workspace_size(int64_t f, int64_t cap_m, size_t *bytes);
+gnn_status gnn_layer_norm_bwd(const void *g, gnn_dtype gdt, const void *x, gnn_dtype xdt, const int64_t *m_dev,
+                              int64_t cap_m, int64_t f, const float *gamma, const float *mean, const float *rstd,
+                              const void *d_res, void *d_x, float *dgamma, float *dbeta, void *ws, size_t ws_bytes,
+                              gnn_stream s);
+
 /* Plain SGD (synchronous SGD of Section II-B on one device): w -= lr * dw
  * over n fp32 values [device]. */
 gnn_status gnn_sgd(float *w, const float *dw, int64_t n, float lr, gnn_stream s);

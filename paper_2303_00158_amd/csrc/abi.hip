@@ -1,5 +1,6 @@
 // extern "C" entry points: host-side validation, then the launchers.
 #include <algorithm>
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 
@@ -51,6 +52,13 @@ namespace {
 
 bool act_dtype(int dt) { return dt == GNN_F32 || dt == GNN_BF16; }
 bool dim_ok(int64_t f) { return f >= 1 && f <= GNN_MAX_DIM; }
+
+gnn_status check_norm(const int64_t *m_dev, int64_t cap_m, int64_t f, const char *who) {
+    GNN_CHECK(dim_ok(f), GNN_EINVAL, "%s: f out of [1, %d]", who, GNN_MAX_DIM);
+    GNN_CHECK(cap_m >= 0 && cap_m <= kMaxGrid, GNN_EINVAL, "%s: bad cap_m", who);
+    GNN_CHECK(aligned(m_dev, 8), GNN_EINVAL, "%s: misaligned data", who);
+    return GNN_OK;
+}
 
 gnn_status check_graph(const gnn_graph *g, const char *who) {
     GNN_CHECK(g, GNN_EINVAL, "%s: graph is NULL", who);
@@ -533,6 +541,54 @@ gnn_status gnn_softmax_ce(const float *logits, int64_t b, int64_t c, const int64
               GNN_EINVAL, "%s: misaligned data", who);
     GNN_CHECK(ws_bytes >= softmax_ce_ws_bytes(b), GNN_ESIZE, "%s: workspace too small", who);
     return launch_softmax_ce(logits, b, c, labels, targets, g_out, loss_out, ws, stream_of(s));
+}
+
+gnn_status gnn_layer_norm_fwd(const void *x, gnn_dtype xdt, const int64_t *m_dev, int64_t cap_m, int64_t f,
+                              const float *gamma, const float *beta, float eps, void *y, gnn_dtype ydt, float *mean,
+                              float *rstd, gnn_stream s) {
+    clear_error();
+    const char *who = "gnn_layer_norm_fwd";
+    GNN_CHECK(act_dtype(xdt) && act_dtype(ydt), GNN_EUNSUPPORTED, "%s: dtypes must be GNN_F32 or GNN_BF16", who);
+    GNN_TRY(check_norm(m_dev, cap_m, f, who));
+    GNN_CHECK(eps >= 0.f && std::isfinite(eps), GNN_EINVAL, "%s: eps must be finite and not negative", who);
+    GNN_CHECK((x && y) || cap_m == 0, GNN_EINVAL, "%s: NULL pointer", who);
+    GNN_CHECK(x != y || xdt == ydt || cap_m == 0, GNN_EINVAL, "%s: y may be x only with the same dtype", who);
+    GNN_CHECK(aligned(x, dtype_size(xdt)) && aligned(y, dtype_size(ydt)) && aligned(gamma, 4) && aligned(beta, 4) &&
+                  aligned(mean, 4) && aligned(rstd, 4),
+              GNN_EINVAL, "%s: misaligned data", who);
+    return launch_layer_norm_fwd(x, xdt, m_dev, cap_m, f, gamma, beta, eps, y, ydt, mean, rstd, stream_of(s));
+}
+
+gnn_status gnn_layer_norm_bwd_workspace_size(int64_t f, int64_t cap_m, size_t *bytes) {
+    clear_error();
+    GNN_CHECK(bytes, GNN_EINVAL, "gnn_layer_norm_bwd_workspace_size: bytes is NULL");
+    GNN_TRY(check_norm(nullptr, cap_m, f, "gnn_layer_norm_bwd_workspace_size"));
+    *bytes = layer_norm_bwd_ws_bytes(f, cap_m);
+    return GNN_OK;
+}
+
+gnn_status gnn_layer_norm_bwd(const void *g, gnn_dtype gdt, const void *x, gnn_dtype xdt, const int64_t *m_dev,
+                              int64_t cap_m, int64_t f, const float *gamma, const float *mean, const float *rstd,
+                              const void *d_res, void *d_x, float *dgamma, float *dbeta, void *ws, size_t ws_bytes,
+                              gnn_stream s) {
+    clear_error();
+    const char *who = "gnn_layer_norm_bwd";
+    GNN_CHECK(act_dtype(gdt) && act_dtype(xdt), GNN_EUNSUPPORTED, "%s: dtypes must be GNN_F32 or GNN_BF16", who);
+    GNN_TRY(check_norm(m_dev, cap_m, f, who));
+    GNN_CHECK((g && x && mean && rstd) || cap_m == 0, GNN_EINVAL, "%s: NULL pointer", who);
+    GNN_CHECK(d_x || dgamma || dbeta, GNN_EINVAL, "%s: no output is wanted", who);
+    GNN_CHECK(d_x != x || cap_m == 0 || !d_x, GNN_EINVAL, "%s: d_x must not be x", who);
+    GNN_CHECK(aligned(g, dtype_size(gdt)) && aligned(x, dtype_size(xdt)) && aligned(d_res, dtype_size(gdt)) &&
+                  aligned(d_x, dtype_size(gdt)) && aligned(gamma, 4) && aligned(mean, 4) && aligned(rstd, 4) &&
+                  aligned(dgamma, 4) && aligned(dbeta, 4),
+              GNN_EINVAL, "%s: misaligned data", who);
+    if (dgamma || dbeta) {
+        const size_t need = layer_norm_bwd_ws_bytes(f, cap_m);
+        GNN_CHECK(ws && aligned(ws, 256), GNN_EINVAL, "%s: ws must be non-NULL and 256-byte aligned", who);
+        GNN_CHECK(ws_bytes >= need, GNN_ESIZE, "%s: workspace %zu bytes, need %zu", who, ws_bytes, need);
+    }
+    return launch_layer_norm_bwd(g, gdt, x, xdt, m_dev, cap_m, f, gamma, mean, rstd, d_res, d_x, dgamma, dbeta, ws,
+                                 stream_of(s));
 }
 
 gnn_status gnn_sgd(float *w, const float *dw, int64_t n, float lr, gnn_stream s) {

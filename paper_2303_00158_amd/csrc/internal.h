@@ -216,6 +216,14 @@ gnn_status launch_shadow_sync(const float *w, int64_t K, int64_t n, uint16_t *wt
 size_t softmax_ce_ws_bytes(int64_t b);
 gnn_status launch_softmax_ce(const float *logits, int64_t b, int64_t c, const int64_t *labels,
                              const int64_t *targets, float *g_out, float *loss_out, void *ws, hipStream_t s);
+// Layer normalisation and its gradients (layer_norm.hip).
+gnn_status launch_layer_norm_fwd(const void *x, int xdt, const int64_t *m_dev, int64_t cap_m, int64_t f,
+                                 const float *gamma, const float *beta, float eps, void *y, int ydt, float *mean,
+                                 float *rstd, hipStream_t s);
+size_t layer_norm_bwd_ws_bytes(int64_t f, int64_t cap_m);
+gnn_status launch_layer_norm_bwd(const void *g, int gdt, const void *x, int xdt, const int64_t *m_dev, int64_t cap_m,
+                                 int64_t f, const float *gamma, const float *mean, const float *rstd,
+                                 const void *d_res, void *d_x, float *dgamma, float *dbeta, void *ws, hipStream_t s);
 gnn_status launch_sgd(float *w, const float *dw, int64_t n, float lr, hipStream_t s);
 size_t sampler_ws_bytes(int64_t graph_n, int64_t cap_dst, int32_t fanout);
 gnn_status launch_sampler_ws_init(void *ws, int64_t graph_n, hipStream_t s);

@@ -22,6 +22,7 @@ GNN_F32, GNN_BF16, GNN_F16 = 0, 1, 2
 GNN_AGG_SAGE_MEAN, GNN_AGG_GCN_SYM, GNN_AGG_SAGE_MAX = 0, 1, 2
 GNN_LOC_DEVICE, GNN_LOC_HOST_PINNED = 0, 1
 GNN_MAX_LAYERS = 4
+GNN_MAX_DIM = 65536
 
 _i64, _i32, _u64, _f32, _vp, _sz = (ctypes.c_int64, ctypes.c_int32, ctypes.c_uint64, ctypes.c_float,
                                     ctypes.c_void_p, ctypes.c_size_t)
@@ -100,6 +101,10 @@ _SIGNATURES = {
     "gnn_update_bwd_noalloc": (_i32, [_vp, _vp, _i32, _i64, _vp, _i64, _vp, _vp, _i64, _i32, _vp, _vp, _vp, _vp]),
     "gnn_softmax_ce_workspace_size": (_i32, [_i64, _P(_sz)]),
     "gnn_softmax_ce": (_i32, [_vp, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "gnn_layer_norm_fwd": (_i32, [_vp, _i32, _vp, _i64, _i64, _vp, _vp, _f32, _vp, _i32, _vp, _vp, _vp]),
+    "gnn_layer_norm_bwd_workspace_size": (_i32, [_i64, _i64, _P(_sz)]),
+    "gnn_layer_norm_bwd": (_i32, [_vp, _i32, _vp, _i32, _vp, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz,
+                                  _vp]),
     "gnn_sgd": (_i32, [_vp, _vp, _i64, _f32, _vp]),
     "gnn_model_sync_shadow": (_i32, [_P(Model), _vp]),
     "gnn_train_step_layout": (_i32, [_P(Model), _i64, _i64, _P(StepLayout)]),
@@ -479,6 +484,116 @@ def softmax_ce(logits: torch.Tensor, labels: torch.Tensor, targets: Optional[tor
 def sgd(w: torch.Tensor, dw: torch.Tensor, lr: float, stream=None) -> torch.Tensor:
     _check(lib().gnn_sgd(_ptr(w), _ptr(dw), w.numel(), float(lr), _stream(stream)))
     return w
+
+
+# ---------------------------------------------------------------------------
+# layers of deep and residual models
+# ---------------------------------------------------------------------------
+
+_ACTIVATIONS = (torch.float32, torch.bfloat16)
+
+
+def _want(name: str, t: Optional[torch.Tensor], shape, dtypes, device=None) -> None:
+    """Raise ValueError unless t (None passes) is a dense tensor of that shape
+    (a None in it matches any length) and one of the dtypes, on the GPU that
+    ``device`` names."""
+    if t is None:
+        return
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name}: dtype {t.dtype}, expected {' or '.join(str(d) for d in dtypes)}")
+    if t.dim() != len(shape) or any(w is not None and n != w for n, w in zip(t.shape, shape)):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple('any' if w is None else w for w in shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: strides {t.stride()}, expected dense rows")
+    if not t.is_cuda:
+        raise ValueError(f"{name}: on {t.device}, expected a GPU")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name}: on {t.device}, expected {device}")
+
+
+def _want_rows(m_dev: Optional[torch.Tensor], cap_m: Optional[int], rows: int, device) -> int:
+    """The row capacity of a call on ``rows`` rows with a device count m_dev."""
+    _want("m_dev", m_dev, (1,), (torch.int64,), device)
+    if cap_m is None:
+        return rows
+    if not 0 <= cap_m <= rows:
+        raise ValueError(f"cap_m: {cap_m}, expected at most the {rows} rows given")
+    return int(cap_m)
+
+
+def _scratch(nbytes: int, device, stream) -> torch.Tensor:
+    """A workspace that belongs to the stream it is used on."""
+    if stream is None:
+        return _aligned_empty(nbytes, device)
+    with torch.cuda.stream(stream):
+        return _aligned_empty(nbytes, device)
+
+
+def _enqueue(fn, device, stream, *args) -> None:
+    """fn(*args, stream) with the tensors' GPU current, on its current stream
+    unless one is given."""
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+    elif stream.device != device:
+        raise ValueError(f"stream: on {stream.device}, expected {device}")
+    if device.index == torch.cuda.current_device():
+        _check(fn(*args, stream.cuda_stream))
+    else:
+        with torch.cuda.device(device):
+            _check(fn(*args, stream.cuda_stream))
+
+
+def layer_norm_fwd(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], y: torch.Tensor,
+                   eps: float = 1e-5, mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None,
+                   m_dev: Optional[torch.Tensor] = None, cap_m: Optional[int] = None, stream=None) -> torch.Tensor:
+    """gnn_layer_norm_fwd: y = gamma (x - mean) rstd + beta of every row of x
+    (rows x f); mean and rstd (fp32, one per row) are kept for the backward.
+    y may be x itself."""
+    _want("x", x, (None, None), _ACTIVATIONS)
+    rows, f = x.shape
+    dev = x.device
+    _want("y", y, (rows, f), _ACTIVATIONS, dev)
+    for name, t, n in (("gamma", gamma, f), ("beta", beta, f), ("mean", mean, rows), ("rstd", rstd, rows)):
+        _want(name, t, (n,), (torch.float32,), dev)
+    cap = _want_rows(m_dev, cap_m, rows, dev)
+    _enqueue(lib().gnn_layer_norm_fwd, dev, stream, _ptr(x), dtype_code(x.dtype), _ptr(m_dev), cap, f, _ptr(gamma),
+             _ptr(beta), float(eps), _ptr(y), dtype_code(y.dtype), _ptr(mean), _ptr(rstd))
+    return y
+
+
+def layer_norm_bwd_workspace(f: int, cap_m: int, device, stream=None) -> torch.Tensor:
+    """A workspace for gnn_layer_norm_bwd with these sizes."""
+    nb = _sz()
+    _check(lib().gnn_layer_norm_bwd_workspace_size(f, cap_m, ctypes.byref(nb)))
+    return _scratch(nb.value, device, stream)
+
+
+def layer_norm_bwd(g: torch.Tensor, x: torch.Tensor, gamma: Optional[torch.Tensor], mean: torch.Tensor,
+                   rstd: torch.Tensor, d_x: Optional[torch.Tensor], dgamma: Optional[torch.Tensor],
+                   dbeta: Optional[torch.Tensor], d_res: Optional[torch.Tensor] = None,
+                   m_dev: Optional[torch.Tensor] = None, cap_m: Optional[int] = None,
+                   ws: Optional[torch.Tensor] = None, stream=None):
+    """gnn_layer_norm_bwd: the gradients of layer_norm_fwd from g = dLoss/dy.
+    d_res (the type of g) is added to d_x: the gradient that reaches x along a
+    skip connection.  d_x may be g or d_res itself; outputs that are None are
+    not computed.  ws: workspace (allocated when None)."""
+    _want("x", x, (None, None), _ACTIVATIONS)
+    rows, f = x.shape
+    dev = x.device
+    _want("g", g, (rows, f), _ACTIVATIONS, dev)
+    _want("d_res", d_res, (rows, f), (g.dtype,), dev)
+    _want("d_x", d_x, (rows, f), (g.dtype,), dev)
+    for name, t, n in (("gamma", gamma, f), ("mean", mean, rows), ("rstd", rstd, rows), ("dgamma", dgamma, f),
+                       ("dbeta", dbeta, f)):
+        _want(name, t, (n,), (torch.float32,), dev)
+    cap = _want_rows(m_dev, cap_m, rows, dev)
+    if ws is None and (dgamma is not None or dbeta is not None):
+        ws = layer_norm_bwd_workspace(f, cap, dev, stream)
+    _want("ws", ws, (None,), (torch.uint8,), dev)
+    _enqueue(lib().gnn_layer_norm_bwd, dev, stream, _ptr(g), dtype_code(g.dtype), _ptr(x), dtype_code(x.dtype),
+             _ptr(m_dev), cap, f, _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(d_res), _ptr(d_x), _ptr(dgamma),
+             _ptr(dbeta), _ptr(ws), ws.numel() if ws is not None else 0)
+    return d_x, dgamma, dbeta
 
 
 # ---------------------------------------------------------------------------
