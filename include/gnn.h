@@ -492,6 +492,50 @@ gnn_status gnn_softmax_ce_workspace_size(int64_t b, size_t *bytes);
 gnn_status gnn_softmax_ce(const float *logits, int64_t b, int64_t c, const int64_t *labels, const int64_t *targets,
                           float *g_out, float *loss_out, void *ws, size_t ws_bytes, gnn_stream s);
 
+/* Distillation (the loss against a teacher model's outputs, beside or in
+ * place of the ground truth of Section II-B): the b rows of logits are the
+ * student's, and of each row's teacher outputs the k largest are known.
+ *   logits [device] b x c of ldt (GNN_F32 or GNN_BF16), c <= GNN_MAX_CLASSES.
+ *   t_val, t_idx [device] b x k (k <= GNN_MAX_TOP): the teacher's logits (tdt,
+ *          GNN_F32 or GNN_BF16) and the classes they belong to (int64).  An
+ *          entry whose index is outside [0, c) or whose value is -infinity is
+ *          absent; a class may be listed more than once.
+ *   With the temperature T > 0, p_i = softmax over row i's present entries of
+ *   t_val / T, and the targets y_i as in gnn_softmax_ce,
+ *     soft_i = T^2 sum_e p_ie (log p_ie - log softmax(z_i / T)[t_idx_ie]),
+ *              0 for a row without entries,
+ *     hard_i = -log softmax(z_i)[y_i], 0 for a label outside [0, c),
+ *     row_loss_i = alpha soft_i + (1 - alpha) hard_i,
+ *     loss = sum_i scale_i row_loss_i.
+ *   An entry whose p is 0 adds nothing, whatever its class's logit.
+ *   alpha  in [0, 1]; with 1 (0) the labels (the teacher) are not read.
+ *   labels [device] int64, or NULL: no hard term; targets [device] int64 b or
+ *          NULL as in gnn_softmax_ce.
+ *   row_scale [device] fp32 b, or NULL for 1 / b.  A row whose scale is 0 is
+ *          not read: its loss is 0 and its gradient 0 (rows that pad a batch).
+ *   g_out  [device] b x c of gdt (GNN_F32 or GNN_BF16): dLoss/dlogits,
+ *            scale [alpha T (softmax(z / T) - sum_e p_e onehot(t_idx_e))
+ *                   + (1 - alpha) (softmax(z) - onehot(y))],
+ *          each bracket where its term is present; it may be logits itself
+ *          when gdt == ldt, and NULL when only the loss is wanted.
+ *   row_loss [device] fp32 b, or NULL.  loss_out [device] fp32 scalar.
+ *   ws     [device] 256-byte aligned workspace of
+ *          gnn_distill_topk_workspace_size bytes; no state is kept in it
+ *          between calls; calls sharing it must not overlap.
+ * Sums and probabilities are fp32; every sum has a fixed order, so results
+ * are bitwise reproducible.  A NaN logit, a +infinity, or a row of -infinity
+ * alone makes its row's loss NaN; a -infinity logit has probability 0 (and
+ * an infinite loss where the teacher's is not 0).  Errors: GNN_EINVAL for bad
+ * sizes, temperature or alpha, NULL or misaligned (to the element) pointers;
+ * GNN_EUNSUPPORTED for other dtypes; GNN_ESIZE for a small workspace. */
+#define GNN_MAX_CLASSES (1 << 20)
+#define GNN_MAX_TOP 1024
+gnn_status gnn_distill_topk_workspace_size(int64_t b, int64_t c, int64_t k, size_t *bytes);
+gnn_status gnn_distill_topk(const void *logits, gnn_dtype ldt, int64_t b, int64_t c, const void *t_val, gnn_dtype tdt,
+                            const int64_t *t_idx, int64_t k, float temperature, float alpha, const int64_t *labels,
+                            const int64_t *targets, const float *row_scale, void *g_out, gnn_dtype gdt,
+                            float *row_loss, float *loss_out, void *ws, size_t ws_bytes, gnn_stream s);
+
 /* ------------------------------------------------------------------------
  * Layer normalisation of the rows of an activation matrix, between the
  * layers of a deep or residual model.  With mu_i and v_i the mean and the

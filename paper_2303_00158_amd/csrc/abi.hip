@@ -60,6 +60,13 @@ gnn_status check_norm(const int64_t *m_dev, int64_t cap_m, int64_t f, const char
     return GNN_OK;
 }
 
+gnn_status check_distill(int64_t b, int64_t c, int64_t k, const char *who) {
+    GNN_CHECK(b >= 0 && b <= kMaxGrid / 256, GNN_EINVAL, "%s: bad b", who);
+    GNN_CHECK(c >= 1 && c <= GNN_MAX_CLASSES, GNN_EINVAL, "%s: c out of [1, %d]", who, GNN_MAX_CLASSES);
+    GNN_CHECK(k >= 1 && k <= GNN_MAX_TOP, GNN_EINVAL, "%s: k out of [1, %d]", who, GNN_MAX_TOP);
+    return GNN_OK;
+}
+
 gnn_status check_graph(const gnn_graph *g, const char *who) {
     GNN_CHECK(g, GNN_EINVAL, "%s: graph is NULL", who);
     GNN_CHECK(g->n >= 0 && g->nnz >= 0, GNN_EINVAL, "%s: negative graph size", who);
@@ -541,6 +548,41 @@ gnn_status gnn_softmax_ce(const float *logits, int64_t b, int64_t c, const int64
               GNN_EINVAL, "%s: misaligned data", who);
     GNN_CHECK(ws_bytes >= softmax_ce_ws_bytes(b), GNN_ESIZE, "%s: workspace too small", who);
     return launch_softmax_ce(logits, b, c, labels, targets, g_out, loss_out, ws, stream_of(s));
+}
+
+gnn_status gnn_distill_topk_workspace_size(int64_t b, int64_t c, int64_t k, size_t *bytes) {
+    clear_error();
+    const char *who = "gnn_distill_topk_workspace_size";
+    GNN_CHECK(bytes, GNN_EINVAL, "%s: bytes is NULL", who);
+    GNN_TRY(check_distill(b, c, k, who));
+    *bytes = distill_ws_bytes(b, c, k);
+    return GNN_OK;
+}
+
+gnn_status gnn_distill_topk(const void *logits, gnn_dtype ldt, int64_t b, int64_t c, const void *t_val, gnn_dtype tdt,
+                            const int64_t *t_idx, int64_t k, float temperature, float alpha, const int64_t *labels,
+                            const int64_t *targets, const float *row_scale, void *g_out, gnn_dtype gdt,
+                            float *row_loss, float *loss_out, void *ws, size_t ws_bytes, gnn_stream s) {
+    clear_error();
+    const char *who = "gnn_distill_topk";
+    GNN_CHECK(act_dtype(ldt) && act_dtype(tdt) && act_dtype(gdt), GNN_EUNSUPPORTED,
+              "%s: dtypes must be GNN_F32 or GNN_BF16", who);
+    GNN_TRY(check_distill(b, c, k, who));
+    GNN_CHECK(temperature > 0.f && std::isfinite(temperature), GNN_EINVAL, "%s: temperature must be finite and positive",
+              who);
+    GNN_CHECK(alpha >= 0.f && alpha <= 1.f, GNN_EINVAL, "%s: alpha out of [0, 1]", who);
+    GNN_CHECK(((logits && t_val && t_idx) || b == 0) && loss_out && ws, GNN_EINVAL, "%s: NULL pointer", who);
+    GNN_CHECK(g_out != logits || !g_out || gdt == ldt, GNN_EINVAL, "%s: g_out may be logits only with the same dtype",
+              who);
+    GNN_CHECK(aligned(logits, dtype_size(ldt)) && aligned(t_val, dtype_size(tdt)) && aligned(t_idx, 8) &&
+                  aligned(labels, 8) && aligned(targets, 8) && aligned(row_scale, 4) &&
+                  aligned(g_out, dtype_size(gdt)) && aligned(row_loss, 4) && aligned(loss_out, 4) && aligned(ws, 256),
+              GNN_EINVAL, "%s: misaligned data", who);
+    GNN_CHECK(ws_bytes >= distill_ws_bytes(b, c, k), GNN_ESIZE, "%s: workspace %zu bytes, need %zu", who, ws_bytes,
+              distill_ws_bytes(b, c, k));
+    const DistillArgs a{logits, ldt, b, c, t_val, tdt, t_idx, k, temperature, alpha, labels, targets, row_scale, g_out,
+                        gdt, row_loss, loss_out};
+    return launch_distill(a, ws, stream_of(s));
 }
 
 gnn_status gnn_layer_norm_fwd(const void *x, gnn_dtype xdt, const int64_t *m_dev, int64_t cap_m, int64_t f,

@@ -216,6 +216,24 @@ gnn_status launch_shadow_sync(const float *w, int64_t K, int64_t n, uint16_t *wt
 size_t softmax_ce_ws_bytes(int64_t b);
 gnn_status launch_softmax_ce(const float *logits, int64_t b, int64_t c, const int64_t *labels,
                              const int64_t *targets, float *g_out, float *loss_out, void *ws, hipStream_t s);
+// The loss against a teacher's top logits (distill.hip).
+struct DistillArgs {
+    const void *logits;
+    int ldt;
+    int64_t b, c;
+    const void *t_val;
+    int tdt;
+    const int64_t *t_idx;
+    int64_t k;
+    float temperature, alpha;
+    const int64_t *labels, *targets;
+    const float *row_scale;
+    void *g_out;
+    int gdt;
+    float *row_loss, *loss_out;
+};
+size_t distill_ws_bytes(int64_t b, int64_t c, int64_t k);
+gnn_status launch_distill(const DistillArgs &a, void *ws, hipStream_t s);
 // Layer normalisation and its gradients (layer_norm.hip).
 gnn_status launch_layer_norm_fwd(const void *x, int xdt, const int64_t *m_dev, int64_t cap_m, int64_t f,
                                  const float *gamma, const float *beta, float eps, void *y, int ydt, float *mean,

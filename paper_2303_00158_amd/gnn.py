@@ -23,6 +23,7 @@ GNN_AGG_SAGE_MEAN, GNN_AGG_GCN_SYM, GNN_AGG_SAGE_MAX = 0, 1, 2
 GNN_LOC_DEVICE, GNN_LOC_HOST_PINNED = 0, 1
 GNN_MAX_LAYERS = 4
 GNN_MAX_DIM = 65536
+GNN_MAX_CLASSES, GNN_MAX_TOP = 1 << 20, 1024
 
 _i64, _i32, _u64, _f32, _vp, _sz = (ctypes.c_int64, ctypes.c_int32, ctypes.c_uint64, ctypes.c_float,
                                     ctypes.c_void_p, ctypes.c_size_t)
@@ -101,6 +102,9 @@ _SIGNATURES = {
     "gnn_update_bwd_noalloc": (_i32, [_vp, _vp, _i32, _i64, _vp, _i64, _vp, _vp, _i64, _i32, _vp, _vp, _vp, _vp]),
     "gnn_softmax_ce_workspace_size": (_i32, [_i64, _P(_sz)]),
     "gnn_softmax_ce": (_i32, [_vp, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "gnn_distill_topk_workspace_size": (_i32, [_i64, _i64, _i64, _P(_sz)]),
+    "gnn_distill_topk": (_i32, [_vp, _i32, _i64, _i64, _vp, _i32, _vp, _i64, _f32, _f32, _vp, _vp, _vp, _vp, _i32, _vp,
+                                _vp, _vp, _sz, _vp]),
     "gnn_layer_norm_fwd": (_i32, [_vp, _i32, _vp, _i64, _i64, _vp, _vp, _f32, _vp, _i32, _vp, _vp, _vp]),
     "gnn_layer_norm_bwd_workspace_size": (_i32, [_i64, _i64, _P(_sz)]),
     "gnn_layer_norm_bwd": (_i32, [_vp, _i32, _vp, _i32, _vp, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz,
@@ -594,6 +598,45 @@ def layer_norm_bwd(g: torch.Tensor, x: torch.Tensor, gamma: Optional[torch.Tenso
              _ptr(m_dev), cap, f, _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(d_res), _ptr(d_x), _ptr(dgamma),
              _ptr(dbeta), _ptr(ws), ws.numel() if ws is not None else 0)
     return d_x, dgamma, dbeta
+
+
+def distill_topk_workspace(b: int, c: int, k: int, device, stream=None) -> torch.Tensor:
+    """A workspace for gnn_distill_topk with these sizes."""
+    nb = _sz()
+    _check(lib().gnn_distill_topk_workspace_size(b, c, k, ctypes.byref(nb)))
+    return _scratch(nb.value, device, stream)
+
+
+def distill_topk(logits: torch.Tensor, t_val: torch.Tensor, t_idx: torch.Tensor, temperature: float,
+                 g_out: Optional[torch.Tensor], loss_out: torch.Tensor, row_loss: Optional[torch.Tensor] = None,
+                 alpha: float = 1.0, labels: Optional[torch.Tensor] = None, targets: Optional[torch.Tensor] = None,
+                 row_scale: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None):
+    """gnn_distill_topk: the loss of the student's logits (b x c) against the
+    teacher's k largest (t_val, t_idx: b x k; an entry with an index outside
+    [0, c) is absent) at a temperature, mixed as alpha soft + (1 - alpha) hard
+    with the labels' cross-entropy, and its gradient g_out (may be logits
+    itself; None: the loss alone).  row_scale: each row's factor in the loss
+    (1 / b when None; 0 skips the row).  ws: workspace (allocated when None)."""
+    _want("logits", logits, (None, None), _ACTIVATIONS)
+    b, c = logits.shape
+    dev = logits.device
+    _want("t_val", t_val, (b, None), _ACTIVATIONS, dev)
+    k = t_val.shape[1]
+    _want("t_idx", t_idx, (b, k), (torch.int64,), dev)
+    _want("g_out", g_out, (b, c), _ACTIVATIONS, dev)
+    _want("loss_out", loss_out, (1,) if loss_out.dim() else (), (torch.float32,), dev)
+    _want("row_loss", row_loss, (b,), (torch.float32,), dev)
+    _want("row_scale", row_scale, (b,), (torch.float32,), dev)
+    _want("targets", targets, (b,), (torch.int64,), dev)
+    _want("labels", labels, (None if targets is not None else b,), (torch.int64,), dev)
+    if ws is None:
+        ws = distill_topk_workspace(b, c, k, dev, stream)
+    _want("ws", ws, (None,), (torch.uint8,), dev)
+    _enqueue(lib().gnn_distill_topk, dev, stream, _ptr(logits), dtype_code(logits.dtype), b, c, _ptr(t_val),
+             dtype_code(t_val.dtype), _ptr(t_idx), k, float(temperature), float(alpha), _ptr(labels), _ptr(targets),
+             _ptr(row_scale), _ptr(g_out), dtype_code(g_out.dtype) if g_out is not None else GNN_F32, _ptr(row_loss),
+             _ptr(loss_out), _ptr(ws), ws.numel())
+    return loss_out, g_out
 
 
 # ---------------------------------------------------------------------------
