@@ -482,6 +482,60 @@ gnn_status gnn_update_bwd_noalloc(const void *a_self, const void *a_nbr, gnn_dty
                                   int64_t n_out, gnn_dtype gemm_dt, float *dw, float *db, float *d_a,
                                   gnn_stream s);
 
+/* The update of a deep or residual model: gnn_update_fwd with any of these
+ * activations and a residual added after it, in one epilogue,
+ *   Z = A W + b,  out = act(Z) + residual.
+ * GNN_ACT_GELU is z Phi(z) with the normal distribution's Phi, _GELU_TANH its
+ * form z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2, _SILU
+ * z / (1 + exp(-z)); _RELU gives 0 for a NaN, as gnn_update_fwd's.
+ *   a_self, a_nbr, adt, k_each, m_dev, cap_m, w, wt, bias, n_out, gemm_dt: as
+ *          gnn_update_fwd, and with GNN_BF16 either of w and wt may be NULL
+ *          (wt is read where both are given; any K).
+ *   residual [device] cap_m x n_out of odt, or NULL; out may be residual.
+ *   z      [device] cap_m x n_out of odt, or NULL: Z, for the backward.
+ *   out    [device] cap_m x n_out of odt (GNN_F32 or GNN_BF16).  The
+ *          activation is taken of Z in fp32, not of the stored value.
+ *   ws     [device] 256-byte aligned workspace of
+ *          gnn_update_fwd_act_workspace_size bytes, NULL when that is 0; no
+ *          state is kept in it between calls; calls sharing it must not
+ *          overlap.  The size is for the same adt, k_each, n_out, cap_m and
+ *          gemm_dt; two: a_nbr is given; shadow: wt is given.
+ * Rows at or past the count are not written (rows of A up to cap_m may be
+ * read, never used).  Errors as gnn_update_fwd, and GNN_EINVAL for an unknown
+ * activation; GNN_ESIZE for a small workspace. */
+typedef int32_t gnn_act;
+enum { GNN_ACT_NONE = 0, GNN_ACT_RELU = 1, GNN_ACT_GELU = 2, GNN_ACT_GELU_TANH = 3, GNN_ACT_SILU = 4 };
+gnn_status gnn_update_fwd_act_workspace_size(gnn_dtype adt, int64_t k_each, int32_t two, int64_t n_out, int64_t cap_m,
+                                             gnn_dtype gemm_dt, int32_t shadow, size_t *bytes);
+gnn_status gnn_update_fwd_act(const void *a_self, const void *a_nbr, gnn_dtype adt, int64_t k_each,
+                              const int64_t *m_dev, int64_t cap_m, const float *w, const uint16_t *wt,
+                              const float *bias, int64_t n_out, gnn_act act, const void *residual, void *z,
+                              gnn_dtype gemm_dt, void *out, gnn_dtype odt, void *ws, size_t ws_bytes, gnn_stream s);
+
+/* Its gradients from g = dLoss/dout (the residual's gradient is g itself):
+ *   dZ = g act'(Z),  dw = A^T dZ,  db = column sums of dZ,  d_a = dZ W^T.
+ *   z      [device] cap_m x n_out of zdt (GNN_F32 or GNN_BF16) as
+ *          gnn_update_fwd_act stored it; it may be NULL for GNN_ACT_NONE.
+ *   g      [device] cap_m x n_out of gdt (GNN_F32 or GNN_BF16).
+ *   w, wt  as above (read for d_a only).
+ *   dw     [device] K x n_out of dwdt (GNN_F32 or GNN_BF16), overwritten.
+ *   db     [device] fp32 n_out, or NULL.  dZ is summed unrounded.
+ *   d_a    [device] cap_m x K of gdt, or NULL (the first layer).
+ *   gemm_dt GNN_BF16: the products' operands (dZ among them) are rounded to
+ *          bf16, sums are fp32; GNN_F32: fp32 throughout, and gdt and dwdt
+ *          must be GNN_F32.
+ *   ws     as above, of gnn_update_bwd_act_workspace_size bytes.
+ * Sums have a fixed order: results are bitwise reproducible for the same
+ * sizes, types and row count.  Errors as gnn_update_fwd_act. */
+gnn_status gnn_update_bwd_act_workspace_size(gnn_dtype adt, int64_t k_each, int32_t two, int64_t n_out, int64_t cap_m,
+                                             gnn_dtype gdt, gnn_dtype dwdt, gnn_dtype gemm_dt, int32_t shadow,
+                                             size_t *bytes);
+gnn_status gnn_update_bwd_act(const void *a_self, const void *a_nbr, gnn_dtype adt, int64_t k_each,
+                              const int64_t *m_dev, int64_t cap_m, const float *w, const uint16_t *wt, const void *z,
+                              gnn_dtype zdt, const void *g, gnn_dtype gdt, int64_t n_out, gnn_act act,
+                              gnn_dtype gemm_dt, void *dw, gnn_dtype dwdt, float *db, void *d_a, void *ws,
+                              size_t ws_bytes, gnn_stream s);
+
 /* Loss against the ground truth (Section II-B): mean softmax cross-entropy
  * over the b target rows of logits [device] (fp32 b x c).  The label of row
  * i is labels[targets[i]] (labels/targets [device] int64; targets NULL means

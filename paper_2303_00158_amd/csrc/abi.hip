@@ -67,6 +67,50 @@ gnn_status check_distill(int64_t b, int64_t c, int64_t k, const char *who) {
     return GNN_OK;
 }
 
+gnn_status check_ws(const void *ws, size_t bytes, size_t need, const char *who) {
+    if (need == 0) return GNN_OK;
+    GNN_CHECK(ws && aligned(ws, 256), GNN_EINVAL, "%s: ws must be non-NULL and 256-byte aligned", who);
+    GNN_CHECK(bytes >= need, GNN_ESIZE, "%s: workspace %zu bytes, need %zu", who, bytes, need);
+    return GNN_OK;
+}
+
+gnn_status check_act_shape(int adt, int64_t k_each, int64_t n_out, int64_t cap_m, int gemm_dt,
+                           const char *who) {
+    GNN_CHECK(act_dtype(adt) && act_dtype(gemm_dt), GNN_EUNSUPPORTED, "%s: dtypes must be GNN_F32 or GNN_BF16", who);
+    GNN_CHECK(dim_ok(k_each) && dim_ok(n_out), GNN_EINVAL, "%s: k_each / n_out out of [1, %d]", who, GNN_MAX_DIM);
+    GNN_CHECK(cap_m >= 0 && cap_m <= kMaxGrid, GNN_EINVAL, "%s: bad cap_m", who);
+    return GNN_OK;
+}
+
+void fill_act(ActArgs &a, const void *a_self, const void *a_nbr, int adt, int64_t k_each, const int64_t *m_dev,
+              int64_t cap_m, const float *w, const uint16_t *wt, int64_t n_out, int act, int gemm_dt) {
+    a.a_self = a_self;
+    a.a_nbr = a_nbr;
+    a.adt = adt;
+    a.k_each = k_each;
+    a.m_dev = m_dev;
+    a.cap_m = cap_m;
+    a.w = w;
+    a.wt = gemm_dt == GNN_BF16 ? wt : nullptr;
+    a.n_out = n_out;
+    a.act = act;
+    a.gemm_dt = gemm_dt;
+}
+
+// What the two directions of the update with an activation share; the
+// weights are needed where a product reads them.
+gnn_status check_act(const ActArgs &a, bool weights, const char *who) {
+    GNN_TRY(check_act_shape(a.adt, a.k_each, a.n_out, a.cap_m, a.gemm_dt, who));
+    GNN_CHECK(a.act >= GNN_ACT_NONE && a.act <= GNN_ACT_SILU, GNN_EINVAL, "%s: unknown activation %d", who, a.act);
+    GNN_CHECK(a.a_self || a.cap_m == 0, GNN_EINVAL, "%s: NULL pointer", who);
+    GNN_CHECK(!weights || a.w || a.wt, GNN_EINVAL, "%s: NULL weights", who);
+    GNN_CHECK(aligned(a.a_self, dtype_size(a.adt)) && aligned(a.a_nbr, dtype_size(a.adt)) && aligned(a.w, 4) &&
+                  aligned(a.m_dev, 8),
+              GNN_EINVAL, "%s: misaligned data", who);
+    GNN_CHECK(aligned(a.wt, 8), GNN_EINVAL, "%s: wt must be 8-byte aligned", who);
+    return GNN_OK;
+}
+
 gnn_status check_graph(const gnn_graph *g, const char *who) {
     GNN_CHECK(g, GNN_EINVAL, "%s: graph is NULL", who);
     GNN_CHECK(g->n >= 0 && g->nnz >= 0, GNN_EINVAL, "%s: negative graph size", who);
@@ -527,6 +571,89 @@ gnn_status gnn_update_bwd(const void *a_self, const void *a_nbr, gnn_dtype adt, 
     GNN_CHECK(ws_bytes >= need, GNN_ESIZE, "%s: workspace %zu bytes, need %zu", who, ws_bytes, need);
     return launch_update_bwd(a_self, a_nbr, adt, k_each, m_dev, cap_m, w, g, n_out, gemm_dt, dw, db, d_a, ws,
                              nullptr, nullptr, nullptr, 0.f, stream_of(s));
+}
+
+gnn_status gnn_update_fwd_act_workspace_size(gnn_dtype adt, int64_t k_each, int32_t two, int64_t n_out, int64_t cap_m,
+                                             gnn_dtype gemm_dt, int32_t shadow, size_t *bytes) {
+    clear_error();
+    const char *who = "gnn_update_fwd_act_workspace_size";
+    GNN_CHECK(bytes, GNN_EINVAL, "%s: bytes is NULL", who);
+    GNN_TRY(check_act_shape(adt, k_each, n_out, cap_m, gemm_dt, who));
+    *bytes = act_fwd_ws_bytes(adt, k_each, two != 0, n_out, cap_m, gemm_dt, shadow != 0);
+    return GNN_OK;
+}
+
+gnn_status gnn_update_fwd_act(const void *a_self, const void *a_nbr, gnn_dtype adt, int64_t k_each,
+                              const int64_t *m_dev, int64_t cap_m, const float *w, const uint16_t *wt,
+                              const float *bias, int64_t n_out, gnn_act act, const void *residual, void *z,
+                              gnn_dtype gemm_dt, void *out, gnn_dtype odt, void *ws, size_t ws_bytes, gnn_stream s) {
+    clear_error();
+    const char *who = "gnn_update_fwd_act";
+    ActFwd a{};
+    fill_act(a, a_self, a_nbr, adt, k_each, m_dev, cap_m, w, wt, n_out, act, gemm_dt);
+    a.bias = bias;
+    a.residual = residual;
+    a.z = z;
+    a.out = out;
+    a.odt = odt;
+    GNN_CHECK(act_dtype(odt), GNN_EUNSUPPORTED, "%s: dtypes must be GNN_F32 or GNN_BF16", who);
+    GNN_TRY(check_act(a, true, who));
+    GNN_CHECK(out || cap_m == 0, GNN_EINVAL, "%s: NULL pointer", who);
+    GNN_CHECK(cap_m == 0 || !z || (z != out && z != residual), GNN_EINVAL, "%s: z must not be out or residual", who);
+    GNN_CHECK(cap_m == 0 || (out != a_self && out != a_nbr && (!z || (z != a_self && z != a_nbr))), GNN_EINVAL,
+              "%s: out and z must not be A", who);
+    const size_t os = dtype_size(odt);
+    GNN_CHECK(aligned(bias, 4) && aligned(residual, os) && aligned(z, os) && aligned(out, os), GNN_EINVAL,
+              "%s: misaligned data", who);
+    GNN_TRY(check_ws(ws, ws_bytes, act_fwd_ws_bytes(adt, k_each, a_nbr != nullptr, n_out, cap_m, gemm_dt, a.wt != nullptr),
+                     who));
+    return launch_act_fwd(a, ws, stream_of(s));
+}
+
+gnn_status gnn_update_bwd_act_workspace_size(gnn_dtype adt, int64_t k_each, int32_t two, int64_t n_out, int64_t cap_m,
+                                             gnn_dtype gdt, gnn_dtype dwdt, gnn_dtype gemm_dt, int32_t shadow,
+                                             size_t *bytes) {
+    clear_error();
+    const char *who = "gnn_update_bwd_act_workspace_size";
+    GNN_CHECK(bytes, GNN_EINVAL, "%s: bytes is NULL", who);
+    GNN_CHECK(act_dtype(gdt) && act_dtype(dwdt), GNN_EUNSUPPORTED, "%s: dtypes must be GNN_F32 or GNN_BF16", who);
+    GNN_TRY(check_act_shape(adt, k_each, n_out, cap_m, gemm_dt, who));
+    *bytes = act_bwd_ws_bytes(adt, k_each, two != 0, n_out, cap_m, gdt, dwdt, gemm_dt, shadow != 0);
+    return GNN_OK;
+}
+
+gnn_status gnn_update_bwd_act(const void *a_self, const void *a_nbr, gnn_dtype adt, int64_t k_each,
+                              const int64_t *m_dev, int64_t cap_m, const float *w, const uint16_t *wt, const void *z,
+                              gnn_dtype zdt, const void *g, gnn_dtype gdt, int64_t n_out, gnn_act act,
+                              gnn_dtype gemm_dt, void *dw, gnn_dtype dwdt, float *db, void *d_a, void *ws,
+                              size_t ws_bytes, gnn_stream s) {
+    clear_error();
+    const char *who = "gnn_update_bwd_act";
+    ActBwd a{};
+    fill_act(a, a_self, a_nbr, adt, k_each, m_dev, cap_m, w, wt, n_out, act, gemm_dt);
+    a.z = z;
+    a.zdt = zdt;
+    a.g = g;
+    a.gdt = gdt;
+    a.dw = dw;
+    a.dwdt = dwdt;
+    a.db = db;
+    a.d_a = d_a;
+    GNN_CHECK(act_dtype(zdt) && act_dtype(gdt) && act_dtype(dwdt), GNN_EUNSUPPORTED,
+              "%s: dtypes must be GNN_F32 or GNN_BF16", who);
+    GNN_TRY(check_act(a, d_a != nullptr, who));
+    GNN_CHECK(gemm_dt == GNN_BF16 || (gdt == GNN_F32 && dwdt == GNN_F32), GNN_EUNSUPPORTED,
+              "%s: GNN_F32 products need gdt and dwdt GNN_F32", who);
+    GNN_CHECK((g || cap_m == 0) && dw && (z || act == GNN_ACT_NONE || cap_m == 0), GNN_EINVAL, "%s: NULL pointer", who);
+    GNN_CHECK(!d_a || cap_m == 0 || (d_a != a_self && d_a != a_nbr && d_a != g && d_a != z), GNN_EINVAL,
+              "%s: d_a must not be an input", who);
+    GNN_CHECK(aligned(z, dtype_size(zdt)) && aligned(g, dtype_size(gdt)) && aligned(dw, dtype_size(dwdt)) &&
+                  aligned(db, 4) && aligned(d_a, dtype_size(gdt)),
+              GNN_EINVAL, "%s: misaligned data", who);
+    GNN_TRY(check_ws(ws, ws_bytes,
+                     act_bwd_ws_bytes(adt, k_each, a_nbr != nullptr, n_out, cap_m, gdt, dwdt, gemm_dt, a.wt != nullptr),
+                     who));
+    return launch_act_bwd(a, ws, stream_of(s));
 }
 
 gnn_status gnn_softmax_ce_workspace_size(int64_t b, size_t *bytes) {

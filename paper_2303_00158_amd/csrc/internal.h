@@ -216,6 +216,41 @@ gnn_status launch_shadow_sync(const float *w, int64_t K, int64_t n, uint16_t *wt
 size_t softmax_ce_ws_bytes(int64_t b);
 gnn_status launch_softmax_ce(const float *logits, int64_t b, int64_t c, const int64_t *labels,
                              const int64_t *targets, float *g_out, float *loss_out, void *ws, hipStream_t s);
+// The update with an activation and a residual (update_act.hip), and its
+// gradients (update_act_bwd.hip).
+struct ActArgs {
+    const void *a_self, *a_nbr;
+    int adt;
+    int64_t k_each;
+    const int64_t *m_dev;
+    int64_t cap_m;
+    const float *w;
+    const uint16_t *wt;
+    int64_t n_out;
+    int act, gemm_dt;
+    int64_t K() const { return a_nbr ? 2 * k_each : k_each; }
+};
+struct ActFwd : ActArgs {
+    const float *bias;
+    const void *residual;
+    void *z, *out;
+    int odt;
+};
+struct ActBwd : ActArgs {
+    const void *z;
+    int zdt;
+    const void *g;
+    int gdt;
+    void *dw;
+    int dwdt;
+    float *db;
+    void *d_a;
+};
+size_t act_fwd_ws_bytes(int adt, int64_t k_each, bool two, int64_t n_out, int64_t cap_m, int gemm_dt, bool shadow);
+gnn_status launch_act_fwd(const ActFwd &a, void *ws, hipStream_t s);
+size_t act_bwd_ws_bytes(int adt, int64_t k_each, bool two, int64_t n_out, int64_t cap_m, int gdt, int dwdt,
+                        int gemm_dt, bool shadow);
+gnn_status launch_act_bwd(const ActBwd &a, void *ws, hipStream_t s);
 // The loss against a teacher's top logits (distill.hip).
 struct DistillArgs {
     const void *logits;

@@ -1,0 +1,160 @@
+// The update with an activation and a residual in its epilogue:
+//   Z = [A_self || A_nbr] W + b,  out = act(Z) + residual
+// on the matrix-core engine of gemm_engine.h.
+#include "act_dev.h"
+#include "gemm_engine.h"
+
+namespace gnn {
+
+namespace {
+
+using namespace gemm;
+
+// One epilogue's operands.
+struct Epilogue {
+    const float *bias;
+    const void *residual;
+    void *z, *out;
+    int64_t n_out;
+    bool bf16;  // the type of residual, z and out
+    bool vec;   // rows and pointers allow four elements at a time
+};
+
+template <class TO> __device__ __forceinline__ void put4(TO *p, int64_t at, int64_t room, bool vec, float4 v) {
+    if (vec) {
+        store4(p, at, v);
+        return;
+    }
+    const float x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (e < room) Elem<TO>::store(p, at + e, x[e]);
+}
+template <class TO> __device__ __forceinline__ float4 get4(const TO *p, int64_t at, int64_t room, bool vec) {
+    if (vec) return load4(p, at);
+    float x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (e < room) x[e] = Elem<TO>::load(p, at + e);
+    return make_float4(x[0], x[1], x[2], x[3]);
+}
+
+// Columns c .. c + 3 (those below n_out) of row r: z + bias stored, activated,
+// the residual added.
+template <int ACT, class TO> __device__ __forceinline__ void finish4(const Epilogue &p, int64_t r, int64_t c, float4 v) {
+    const int64_t room = p.n_out - c, at = r * p.n_out + c;
+    if (room <= 0) return;
+    if (p.bias) {
+        const float4 b = get4(p.bias + c, 0, room, false);
+        v = make_float4(v.x + b.x, v.y + b.y, v.z + b.z, v.w + b.w);
+    }
+    if (p.z) put4(static_cast<TO *>(p.z), at, room, p.vec, v);
+    v = make_float4(act::apply<ACT>(v.x), act::apply<ACT>(v.y), act::apply<ACT>(v.z), act::apply<ACT>(v.w));
+    if (p.residual) {
+        const float4 d = get4(static_cast<const TO *>(p.residual), at, room, p.vec);
+        v = make_float4(v.x + d.x, v.y + d.y, v.z + d.z, v.w + d.w);
+    }
+    put4(static_cast<TO *>(p.out), at, room, p.vec, v);
+}
+
+// The W operand: fp32 W (K x n_out) transposed on the way, or the bf16
+// shadow W^T.
+template <bool BF16, int TILE, bool V, bool WT, int D> struct WOf {
+    using type = SrcCols<BF16, TILE, float, V, D>;
+    __device__ static type make(const void *w, int64_t, int64_t n_out, int64_t r_end, int64_t col0) {
+        return type{static_cast<const float *>(w), nullptr, n_out, n_out, n_out, r_end, col0, {}};
+    }
+};
+template <int TILE, bool V, int D> struct WOf<true, TILE, V, true, D> {
+    using type = SrcRows<true, TILE, uint16_t, V, D>;
+    __device__ static type make(const void *wt, int64_t K, int64_t n_out, int64_t, int64_t col0) {
+        return type{static_cast<const uint16_t *>(wt), nullptr, K, K, n_out, K, col0, {}};
+    }
+};
+
+struct EngineArgs {
+    const void *a_self, *a_nbr;
+    int64_t k_each, K;
+    const int64_t *m_dev;
+    int64_t cap_m;
+    const void *w;
+    TileMap map;
+    Epilogue ep;
+};
+
+template <bool BF16, int TILE, class TA, bool V, bool WT, int ACT>
+__global__ void __launch_bounds__(kThreads) act_engine_kernel(EngineArgs p) {
+    constexpr int D = depth<TILE>();
+    __shared__ __attribute__((aligned(16))) char lds[lds_bytes<TILE, TILE>()];
+    int64_t tx, ty;
+    p.map.tile_of(blockIdx.x, &tx, &ty);
+    const int64_t M = p.m_dev ? min(*p.m_dev, p.cap_m) : p.cap_m;
+    const int64_t row0 = tx * TILE, col0 = ty * TILE;
+    if (tx >= p.map.mt || row0 >= M) return;
+    SrcRows<BF16, TILE, TA, V, D> sp{static_cast<const TA *>(p.a_self), static_cast<const TA *>(p.a_nbr), p.k_each,
+                                     p.k_each, M, p.K, row0, {}};
+    auto sq = WOf<BF16, TILE, V, WT, D>::make(p.w, p.K, p.ep.n_out, p.K, col0);
+    Acc<TILE, TILE> acc;
+    run_tile<BF16, D>(acc, sp, sq, 0, p.K, lds, [](const auto &, int, int64_t, bool) {});
+    const int64_t gc = col0 + TileOut<TILE, TILE>::col();
+    emit_tile(acc, lds, [&](int, int r, int, float4 v) {
+        const int64_t gr = row0 + r;
+        if (gr >= M) return;
+        if (p.ep.bf16) finish4<ACT, uint16_t>(p.ep, gr, gc, v);
+        else finish4<ACT, float>(p.ep, gr, gc, v);
+    });
+}
+
+}  // namespace
+
+size_t act_fwd_ws_bytes(int, int64_t, bool, int64_t, int64_t, int, bool) { return 0; }
+
+gnn_status launch_act_fwd(const ActFwd &a, void *, hipStream_t s) {
+    if (a.cap_m == 0) return GNN_OK;
+    const bool bf = a.gemm_dt == GNN_BF16, wt = bf && a.wt;
+    const size_t asz = dtype_size(a.adt), osz = dtype_size(a.odt);
+    EngineArgs p{};
+    p.a_self = a.a_self;
+    p.a_nbr = a.a_nbr;
+    p.k_each = a.k_each;
+    p.K = a.K();
+    p.m_dev = a.m_dev;
+    p.cap_m = a.cap_m;
+    p.w = wt ? static_cast<const void *>(a.wt) : a.w;
+    p.ep = Epilogue{a.bias, a.residual, a.z, a.out, a.n_out, a.odt == GNN_BF16,
+                    a.n_out % 4 == 0 && aligned(a.residual, 4 * osz) && aligned(a.z, 4 * osz) && aligned(a.out, 4 * osz)};
+    const int tile = pick_tile(a.cap_m, a.n_out);
+    p.map = TileMap{ceil_div(a.cap_m, tile), ceil_div(a.n_out, tile)};
+    GNN_CHECK(p.map.blocks() <= kMaxGrid / kThreads, GNN_ESIZE, "update_fwd_act: cap_m exceeds the grid limit");
+    const bool vec = a.k_each % 4 == 0 && aligned(a.a_self, 4 * asz) && aligned(a.a_nbr, 4 * asz) &&
+                     (wt ? aligned(a.wt, 8) : a.n_out % 4 == 0 && aligned(a.w, 16));
+    const unsigned grid = static_cast<unsigned>(p.map.blocks());
+    act::with(a.act, [&](auto code) {
+        constexpr int ACT = decltype(code)::value;
+        auto go = [&](auto bf16, auto t, auto ta, auto v, auto shadow) {
+            act_engine_kernel<decltype(bf16)::value, decltype(t)::value, decltype(ta), decltype(v)::value,
+                              decltype(shadow)::value, ACT><<<grid, kThreads, 0, s>>>(p);
+        };
+        using std::bool_constant;
+        using std::integral_constant;
+        auto by_tile = [&](auto bf16, auto ta, auto v, auto shadow) {
+            if (tile == 128) go(bf16, integral_constant<int, 128>{}, ta, v, shadow);
+            else go(bf16, integral_constant<int, 64>{}, ta, v, shadow);
+        };
+        auto by_vec = [&](auto bf16, auto ta, auto shadow) {
+            if (vec) by_tile(bf16, ta, bool_constant<true>{}, shadow);
+            else by_tile(bf16, ta, bool_constant<false>{}, shadow);
+        };
+        auto by_type = [&](auto bf16, auto shadow) {
+            if (a.adt == GNN_BF16) by_vec(bf16, uint16_t{}, shadow);
+            else by_vec(bf16, float{}, shadow);
+        };
+        if (wt) by_type(bool_constant<true>{}, bool_constant<true>{});
+        else if (bf) by_type(bool_constant<true>{}, bool_constant<false>{});
+        else by_type(bool_constant<false>{}, bool_constant<false>{});
+    });
+    GNN_LAUNCHED("update_fwd_act");
+    return GNN_OK;
+}
+
+}  // namespace gnn

@@ -21,6 +21,7 @@ GNN_DEVERR_WAIT, GNN_DEVERR_RANGE = 1, 2
 GNN_F32, GNN_BF16, GNN_F16 = 0, 1, 2
 GNN_AGG_SAGE_MEAN, GNN_AGG_GCN_SYM, GNN_AGG_SAGE_MAX = 0, 1, 2
 GNN_LOC_DEVICE, GNN_LOC_HOST_PINNED = 0, 1
+GNN_ACT_NONE, GNN_ACT_RELU, GNN_ACT_GELU, GNN_ACT_GELU_TANH, GNN_ACT_SILU = 0, 1, 2, 3, 4
 GNN_MAX_LAYERS = 4
 GNN_MAX_DIM = 65536
 GNN_MAX_CLASSES, GNN_MAX_TOP = 1 << 20, 1024
@@ -100,6 +101,12 @@ _SIGNATURES = {
     "gnn_update_bwd": (_i32, [_vp, _vp, _i32, _i64, _vp, _i64, _vp, _vp, _i64, _i32, _vp, _vp, _vp, _vp, _sz,
                               _vp]),
     "gnn_update_bwd_noalloc": (_i32, [_vp, _vp, _i32, _i64, _vp, _i64, _vp, _vp, _i64, _i32, _vp, _vp, _vp, _vp]),
+    "gnn_update_fwd_act_workspace_size": (_i32, [_i32, _i64, _i32, _i64, _i64, _i32, _i32, _P(_sz)]),
+    "gnn_update_fwd_act": (_i32, [_vp, _vp, _i32, _i64, _vp, _i64, _vp, _vp, _vp, _i64, _i32, _vp, _vp, _i32, _vp,
+                                  _i32, _vp, _sz, _vp]),
+    "gnn_update_bwd_act_workspace_size": (_i32, [_i32, _i64, _i32, _i64, _i64, _i32, _i32, _i32, _i32, _P(_sz)]),
+    "gnn_update_bwd_act": (_i32, [_vp, _vp, _i32, _i64, _vp, _i64, _vp, _vp, _vp, _i32, _vp, _i32, _i64, _i32, _i32,
+                                  _vp, _i32, _vp, _vp, _vp, _sz, _vp]),
     "gnn_softmax_ce_workspace_size": (_i32, [_i64, _P(_sz)]),
     "gnn_softmax_ce": (_i32, [_vp, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
     "gnn_distill_topk_workspace_size": (_i32, [_i64, _i64, _i64, _P(_sz)]),
@@ -598,6 +605,98 @@ def layer_norm_bwd(g: torch.Tensor, x: torch.Tensor, gamma: Optional[torch.Tenso
              _ptr(m_dev), cap, f, _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(d_res), _ptr(d_x), _ptr(dgamma),
              _ptr(dbeta), _ptr(ws), ws.numel() if ws is not None else 0)
     return d_x, dgamma, dbeta
+
+
+def _want_update(a_self, a_nbr, w, wt, n_out, gemm_dtype, need_w):
+    """Check what the two directions of the update with an activation share;
+    (rows, k_each, K, device)."""
+    _want("a_self", a_self, (None, None), _ACTIVATIONS)
+    rows, k_each = a_self.shape
+    dev = a_self.device
+    _want("a_nbr", a_nbr, (rows, k_each), (a_self.dtype,), dev)
+    K = k_each * (2 if a_nbr is not None else 1)
+    _want("w", w, (K, n_out), (torch.float32,), dev)
+    _want("wt", wt, (n_out, K), (torch.bfloat16,), dev)
+    if need_w and w is None and (wt is None or gemm_dtype != GNN_BF16):
+        raise ValueError("w: None, expected the weights" if wt is None else "w: None with GNN_F32 products")
+    return rows, k_each, K, dev
+
+
+def update_fwd_act_workspace(a_self: torch.Tensor, a_nbr: Optional[torch.Tensor], n_out: int, gemm_dtype: int,
+                             shadow: bool, cap_m: Optional[int] = None, stream=None) -> torch.Tensor:
+    """A workspace for update_fwd_act on inputs of these shapes and types
+    (shadow: wt is given)."""
+    nb = _sz()
+    _check(lib().gnn_update_fwd_act_workspace_size(dtype_code(a_self.dtype), a_self.shape[1], int(a_nbr is not None),
+                                                   n_out, a_self.shape[0] if cap_m is None else cap_m, gemm_dtype,
+                                                   int(shadow), ctypes.byref(nb)))
+    return _scratch(nb.value, a_self.device, stream)
+
+
+def update_fwd_act(a_self: torch.Tensor, a_nbr: Optional[torch.Tensor], w: Optional[torch.Tensor],
+                   bias: Optional[torch.Tensor], out: torch.Tensor, act: int, gemm_dtype: int,
+                   residual: Optional[torch.Tensor] = None, z: Optional[torch.Tensor] = None,
+                   m_dev: Optional[torch.Tensor] = None, cap_m: Optional[int] = None,
+                   ws: Optional[torch.Tensor] = None, wt: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """gnn_update_fwd_act: out = act([a_self || a_nbr] w + bias) + residual,
+    act one of GNN_ACT_*; z (the type of out) keeps the product for the
+    backward.  residual may be out itself.  wt: the bf16 W^T shadow (n_out x
+    K), read in bf16 mode in place of w.  ws: workspace (allocated when None)."""
+    _want("out", out, (None, None), _ACTIVATIONS)
+    n_out = out.shape[1]
+    rows, k_each, K, dev = _want_update(a_self, a_nbr, w, wt, n_out, gemm_dtype, True)
+    _want("out", out, (rows, n_out), _ACTIVATIONS, dev)
+    _want("bias", bias, (n_out,), (torch.float32,), dev)
+    _want("residual", residual, (rows, n_out), (out.dtype,), dev)
+    _want("z", z, (rows, n_out), (out.dtype,), dev)
+    cap = _want_rows(m_dev, cap_m, rows, dev)
+    if ws is None:
+        ws = update_fwd_act_workspace(a_self, a_nbr, n_out, gemm_dtype, wt is not None, cap, stream)
+    _want("ws", ws, (None,), (torch.uint8,), dev)
+    _enqueue(lib().gnn_update_fwd_act, dev, stream, _ptr(a_self), _ptr(a_nbr), dtype_code(a_self.dtype), k_each,
+             _ptr(m_dev), cap, _ptr(w), _ptr(wt), _ptr(bias), n_out, int(act), _ptr(residual), _ptr(z), gemm_dtype,
+             _ptr(out), dtype_code(out.dtype), _ptr(ws), ws.numel())
+    return out
+
+
+def update_bwd_act_workspace(a_self: torch.Tensor, a_nbr: Optional[torch.Tensor], n_out: int, gemm_dtype: int,
+                             shadow: bool, g_dtype: torch.dtype, dw_dtype: torch.dtype, cap_m: Optional[int] = None,
+                             stream=None) -> torch.Tensor:
+    """A workspace for update_bwd_act on inputs of these shapes and types."""
+    nb = _sz()
+    _check(lib().gnn_update_bwd_act_workspace_size(dtype_code(a_self.dtype), a_self.shape[1], int(a_nbr is not None),
+                                                   n_out, a_self.shape[0] if cap_m is None else cap_m,
+                                                   dtype_code(g_dtype), dtype_code(dw_dtype), gemm_dtype, int(shadow),
+                                                   ctypes.byref(nb)))
+    return _scratch(nb.value, a_self.device, stream)
+
+
+def update_bwd_act(a_self: torch.Tensor, a_nbr: Optional[torch.Tensor], w: Optional[torch.Tensor],
+                   z: Optional[torch.Tensor], g: torch.Tensor, dw: torch.Tensor, db: Optional[torch.Tensor],
+                   d_a: Optional[torch.Tensor], act: int, gemm_dtype: int, m_dev: Optional[torch.Tensor] = None,
+                   cap_m: Optional[int] = None, ws: Optional[torch.Tensor] = None, wt: Optional[torch.Tensor] = None,
+                   stream=None):
+    """gnn_update_bwd_act: the gradients of update_fwd_act from g = dLoss/dout
+    and the z it kept: dw (K x n_out), db and d_a (the type of g; None for the
+    first layer).  The residual's gradient is g.  ws: workspace (allocated when
+    None)."""
+    _want("g", g, (None, None), _ACTIVATIONS)
+    n_out = g.shape[1]
+    rows, k_each, K, dev = _want_update(a_self, a_nbr, w, wt, n_out, gemm_dtype, d_a is not None)
+    _want("g", g, (rows, n_out), _ACTIVATIONS, dev)
+    _want("z", z, (rows, n_out), _ACTIVATIONS, dev)
+    _want("dw", dw, (K, n_out), _ACTIVATIONS, dev)
+    _want("db", db, (n_out,), (torch.float32,), dev)
+    _want("d_a", d_a, (rows, K), (g.dtype,), dev)
+    cap = _want_rows(m_dev, cap_m, rows, dev)
+    if ws is None:
+        ws = update_bwd_act_workspace(a_self, a_nbr, n_out, gemm_dtype, wt is not None, g.dtype, dw.dtype, cap, stream)
+    _want("ws", ws, (None,), (torch.uint8,), dev)
+    _enqueue(lib().gnn_update_bwd_act, dev, stream, _ptr(a_self), _ptr(a_nbr), dtype_code(a_self.dtype), k_each,
+             _ptr(m_dev), cap, _ptr(w), _ptr(wt), _ptr(z), dtype_code(z.dtype) if z is not None else GNN_F32, _ptr(g),
+             dtype_code(g.dtype), n_out, int(act), gemm_dtype, _ptr(dw), dtype_code(dw.dtype), _ptr(db), _ptr(d_a),
+             _ptr(ws), ws.numel())
+    return dw, db, d_a
 
 
 def distill_topk_workspace(b: int, c: int, k: int, device, stream=None) -> torch.Tensor:
