@@ -171,8 +171,11 @@ def _stream(stream=None):
     return ctypes.c_void_p(stream.cuda_stream)
 
 
+_DTYPE_CODES = {torch.float32: GNN_F32, torch.bfloat16: GNN_BF16, torch.float16: GNN_F16}
+
+
 def dtype_code(dt: torch.dtype) -> int:
-    return {torch.float32: GNN_F32, torch.bfloat16: GNN_BF16, torch.float16: GNN_F16}[dt]
+    return _DTYPE_CODES[dt]
 
 
 def torch_dtype(code: int) -> torch.dtype:
@@ -502,13 +505,15 @@ def sgd(w: torch.Tensor, dw: torch.Tensor, lr: float, stream=None) -> torch.Tens
 # ---------------------------------------------------------------------------
 
 _ACTIVATIONS = (torch.float32, torch.bfloat16)
+_FP32, _INT64 = (torch.float32,), (torch.int64,)
 
 
 def _want(name: str, t: Optional[torch.Tensor], shape, dtypes, device=None) -> None:
     """Raise ValueError unless t (None passes) is a dense tensor of that shape
     (a None in it matches any length) and one of the dtypes, on the GPU that
     ``device`` names."""
-    if t is None:
+    if t is None or (t.shape == shape and t.dtype in dtypes and t.device == device and t.is_contiguous()
+                     and device.type == "cuda"):
         return
     if t.dtype not in dtypes:
         raise ValueError(f"{name}: dtype {t.dtype}, expected {' or '.join(str(d) for d in dtypes)}")
@@ -522,9 +527,16 @@ def _want(name: str, t: Optional[torch.Tensor], shape, dtypes, device=None) -> N
         raise ValueError(f"{name}: on {t.device}, expected {device}")
 
 
+def _matrix(name: str, t: torch.Tensor):
+    """(rows, columns) of the matrix that an operator's other shapes go by."""
+    _want(name, t, t.shape if t.dim() == 2 else (None, None), _ACTIVATIONS, t.device)
+    return t.shape
+
+
 def _want_rows(m_dev: Optional[torch.Tensor], cap_m: Optional[int], rows: int, device) -> int:
     """The row capacity of a call on ``rows`` rows with a device count m_dev."""
-    _want("m_dev", m_dev, (1,), (torch.int64,), device)
+    if m_dev is not None:
+        _want("m_dev", m_dev, (1,), _INT64, device)
     if cap_m is None:
         return rows
     if not 0 <= cap_m <= rows:
@@ -544,14 +556,20 @@ def _enqueue(fn, device, stream, *args) -> None:
     """fn(*args, stream) with the tensors' GPU current, on its current stream
     unless one is given."""
     if stream is None:
-        stream = torch.cuda.current_stream(device)
+        # what torch.cuda.current_stream(device).cuda_stream gives, without
+        # the object (0.1 us instead of 1.7)
+        handle = torch._C._cuda_getCurrentRawStream(device.index)
     elif stream.device != device:
         raise ValueError(f"stream: on {stream.device}, expected {device}")
+    else:
+        handle = stream.cuda_stream
     if device.index == torch.cuda.current_device():
-        _check(fn(*args, stream.cuda_stream))
+        code = fn(*args, handle)
     else:
         with torch.cuda.device(device):
-            _check(fn(*args, stream.cuda_stream))
+            code = fn(*args, handle)
+    if code != GNN_OK:
+        _check(code)
 
 
 def layer_norm_fwd(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], y: torch.Tensor,
@@ -560,12 +578,13 @@ def layer_norm_fwd(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optiona
     """gnn_layer_norm_fwd: y = gamma (x - mean) rstd + beta of every row of x
     (rows x f); mean and rstd (fp32, one per row) are kept for the backward.
     y may be x itself."""
-    _want("x", x, (None, None), _ACTIVATIONS)
-    rows, f = x.shape
+    rows, f = _matrix("x", x)
     dev = x.device
     _want("y", y, (rows, f), _ACTIVATIONS, dev)
-    for name, t, n in (("gamma", gamma, f), ("beta", beta, f), ("mean", mean, rows), ("rstd", rstd, rows)):
-        _want(name, t, (n,), (torch.float32,), dev)
+    _want("gamma", gamma, (f,), _FP32, dev)
+    _want("beta", beta, (f,), _FP32, dev)
+    _want("mean", mean, (rows,), _FP32, dev)
+    _want("rstd", rstd, (rows,), _FP32, dev)
     cap = _want_rows(m_dev, cap_m, rows, dev)
     _enqueue(lib().gnn_layer_norm_fwd, dev, stream, _ptr(x), dtype_code(x.dtype), _ptr(m_dev), cap, f, _ptr(gamma),
              _ptr(beta), float(eps), _ptr(y), dtype_code(y.dtype), _ptr(mean), _ptr(rstd))
@@ -588,15 +607,16 @@ def layer_norm_bwd(g: torch.Tensor, x: torch.Tensor, gamma: Optional[torch.Tenso
     d_res (the type of g) is added to d_x: the gradient that reaches x along a
     skip connection.  d_x may be g or d_res itself; outputs that are None are
     not computed.  ws: workspace (allocated when None)."""
-    _want("x", x, (None, None), _ACTIVATIONS)
-    rows, f = x.shape
+    rows, f = _matrix("x", x)
     dev = x.device
     _want("g", g, (rows, f), _ACTIVATIONS, dev)
     _want("d_res", d_res, (rows, f), (g.dtype,), dev)
     _want("d_x", d_x, (rows, f), (g.dtype,), dev)
-    for name, t, n in (("gamma", gamma, f), ("mean", mean, rows), ("rstd", rstd, rows), ("dgamma", dgamma, f),
-                       ("dbeta", dbeta, f)):
-        _want(name, t, (n,), (torch.float32,), dev)
+    _want("gamma", gamma, (f,), _FP32, dev)
+    _want("mean", mean, (rows,), _FP32, dev)
+    _want("rstd", rstd, (rows,), _FP32, dev)
+    _want("dgamma", dgamma, (f,), _FP32, dev)
+    _want("dbeta", dbeta, (f,), _FP32, dev)
     cap = _want_rows(m_dev, cap_m, rows, dev)
     if ws is None and (dgamma is not None or dbeta is not None):
         ws = layer_norm_bwd_workspace(f, cap, dev, stream)
@@ -610,12 +630,11 @@ def layer_norm_bwd(g: torch.Tensor, x: torch.Tensor, gamma: Optional[torch.Tenso
 def _want_update(a_self, a_nbr, w, wt, n_out, gemm_dtype, need_w):
     """Check what the two directions of the update with an activation share;
     (rows, k_each, K, device)."""
-    _want("a_self", a_self, (None, None), _ACTIVATIONS)
-    rows, k_each = a_self.shape
+    rows, k_each = _matrix("a_self", a_self)
     dev = a_self.device
     _want("a_nbr", a_nbr, (rows, k_each), (a_self.dtype,), dev)
     K = k_each * (2 if a_nbr is not None else 1)
-    _want("w", w, (K, n_out), (torch.float32,), dev)
+    _want("w", w, (K, n_out), _FP32, dev)
     _want("wt", wt, (n_out, K), (torch.bfloat16,), dev)
     if need_w and w is None and (wt is None or gemm_dtype != GNN_BF16):
         raise ValueError("w: None, expected the weights" if wt is None else "w: None with GNN_F32 products")
@@ -642,11 +661,10 @@ def update_fwd_act(a_self: torch.Tensor, a_nbr: Optional[torch.Tensor], w: Optio
     act one of GNN_ACT_*; z (the type of out) keeps the product for the
     backward.  residual may be out itself.  wt: the bf16 W^T shadow (n_out x
     K), read in bf16 mode in place of w.  ws: workspace (allocated when None)."""
-    _want("out", out, (None, None), _ACTIVATIONS)
-    n_out = out.shape[1]
+    n_out = _matrix("out", out)[1]
     rows, k_each, K, dev = _want_update(a_self, a_nbr, w, wt, n_out, gemm_dtype, True)
     _want("out", out, (rows, n_out), _ACTIVATIONS, dev)
-    _want("bias", bias, (n_out,), (torch.float32,), dev)
+    _want("bias", bias, (n_out,), _FP32, dev)
     _want("residual", residual, (rows, n_out), (out.dtype,), dev)
     _want("z", z, (rows, n_out), (out.dtype,), dev)
     cap = _want_rows(m_dev, cap_m, rows, dev)
@@ -680,13 +698,12 @@ def update_bwd_act(a_self: torch.Tensor, a_nbr: Optional[torch.Tensor], w: Optio
     and the z it kept: dw (K x n_out), db and d_a (the type of g; None for the
     first layer).  The residual's gradient is g.  ws: workspace (allocated when
     None)."""
-    _want("g", g, (None, None), _ACTIVATIONS)
-    n_out = g.shape[1]
+    n_out = _matrix("g", g)[1]
     rows, k_each, K, dev = _want_update(a_self, a_nbr, w, wt, n_out, gemm_dtype, d_a is not None)
     _want("g", g, (rows, n_out), _ACTIVATIONS, dev)
     _want("z", z, (rows, n_out), _ACTIVATIONS, dev)
     _want("dw", dw, (K, n_out), _ACTIVATIONS, dev)
-    _want("db", db, (n_out,), (torch.float32,), dev)
+    _want("db", db, (n_out,), _FP32, dev)
     _want("d_a", d_a, (rows, K), (g.dtype,), dev)
     cap = _want_rows(m_dev, cap_m, rows, dev)
     if ws is None:
@@ -716,18 +733,17 @@ def distill_topk(logits: torch.Tensor, t_val: torch.Tensor, t_idx: torch.Tensor,
     with the labels' cross-entropy, and its gradient g_out (may be logits
     itself; None: the loss alone).  row_scale: each row's factor in the loss
     (1 / b when None; 0 skips the row).  ws: workspace (allocated when None)."""
-    _want("logits", logits, (None, None), _ACTIVATIONS)
-    b, c = logits.shape
+    b, c = _matrix("logits", logits)
     dev = logits.device
     _want("t_val", t_val, (b, None), _ACTIVATIONS, dev)
     k = t_val.shape[1]
-    _want("t_idx", t_idx, (b, k), (torch.int64,), dev)
+    _want("t_idx", t_idx, (b, k), _INT64, dev)
     _want("g_out", g_out, (b, c), _ACTIVATIONS, dev)
-    _want("loss_out", loss_out, (1,) if loss_out.dim() else (), (torch.float32,), dev)
-    _want("row_loss", row_loss, (b,), (torch.float32,), dev)
-    _want("row_scale", row_scale, (b,), (torch.float32,), dev)
-    _want("targets", targets, (b,), (torch.int64,), dev)
-    _want("labels", labels, (None if targets is not None else b,), (torch.int64,), dev)
+    _want("loss_out", loss_out, (1,) if loss_out.dim() else (), _FP32, dev)
+    _want("row_loss", row_loss, (b,), _FP32, dev)
+    _want("row_scale", row_scale, (b,), _FP32, dev)
+    _want("targets", targets, (b,), _INT64, dev)
+    _want("labels", labels, (None if targets is not None else b,), _INT64, dev)
     if ws is None:
         ws = distill_topk_workspace(b, c, k, dev, stream)
     _want("ws", ws, (None,), (torch.uint8,), dev)
