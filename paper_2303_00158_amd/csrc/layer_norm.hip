@@ -16,116 +16,15 @@
 // workgroups' partial rows are added by a second kernel in their order.  Rows
 // above 16,384 columns, whose sums do not fit the registers beside the row,
 // read x and g once more for them, column stripe by column stripe.
-#include "internal.h"
+#include "row_dev.h"
 
 namespace gnn {
 
 namespace {
 
+using namespace row;
+
 constexpr int64_t kCus = 256;
-
-__device__ __forceinline__ int64_t live_rows(const int64_t *m_dev, int64_t cap_m) {
-    return m_dev ? max(min(*m_dev, cap_m), int64_t(0)) : cap_m;
-}
-
-// ---------------------------------------------------------------------------
-// VE consecutive elements as they lie in memory
-// ---------------------------------------------------------------------------
-template <class T, int VE> struct Vec {
-    static constexpr int kWords = VE * static_cast<int>(sizeof(T)) / 4;
-    uint32_t w[kWords];
-    // 16-byte accesses that ask for no more than the element's alignment
-    struct __attribute__((packed, aligned(sizeof(T)))) Quad {
-        uint32_t w[4];
-    };
-    __device__ __forceinline__ void load(const T *p) {
-#pragma unroll
-        for (int q = 0; q < kWords / 4; ++q) {
-            const Quad v = reinterpret_cast<const Quad *>(p)[q];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w[4 * q + e] = v.w[e];
-        }
-    }
-    __device__ __forceinline__ void store(T *p) const {
-#pragma unroll
-        for (int q = 0; q < kWords / 4; ++q) {
-            Quad v;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v.w[e] = w[4 * q + e];
-            reinterpret_cast<Quad *>(p)[q] = v;
-        }
-    }
-    __device__ __forceinline__ float get(int e) const {
-        if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
-        else return __uint_as_float((e & 1) ? (w[e / 2] & 0xffff0000u) : (w[e / 2] << 16));
-    }
-    __device__ __forceinline__ void set(const float *x) {
-#pragma unroll
-        for (int i = 0; i < kWords; ++i) {
-            if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(x[i]);
-            else w[i] = static_cast<uint32_t>(f32_to_bf16(x[2 * i])) | (static_cast<uint32_t>(f32_to_bf16(x[2 * i + 1])) << 16);
-        }
-    }
-    // elements [0, n) of p, n below VE; the rest are 0
-    __device__ __forceinline__ void load_some(const T *p, int n) {
-        float x[VE];
-#pragma unroll
-        for (int e = 0; e < VE; ++e) x[e] = e < n ? Elem<T>::load(p, e) : 0.f;
-        set(x);
-    }
-    __device__ __forceinline__ void store_some(T *p, int n) const {
-#pragma unroll
-        for (int e = 0; e < VE; ++e)
-            if (e < n) Elem<T>::store(p, e, get(e));
-    }
-    __device__ __forceinline__ void load_upto(const T *p, int64_t n) {
-        if (n >= VE) load(p);
-        else load_some(p, static_cast<int>(max(n, int64_t(0))));
-    }
-    __device__ __forceinline__ void store_upto(T *p, int64_t n) const {
-        if (n >= VE) store(p);
-        else store_some(p, static_cast<int>(max(n, int64_t(0))));
-    }
-};
-
-// T threads to a row, E elements to a thread, in vectors of VE.
-template <int T_, int E_, int VE_> struct Shape {
-    static constexpr int T = T_, E = E_, VE = VE_, NV = E / VE;
-    static constexpr int kThreads = T > 256 ? T : 256;
-    static constexpr int kRows = kThreads / T;  // rows of a workgroup at a time
-    __device__ __forceinline__ static int lane() { return static_cast<int>(threadIdx.x) % T; }
-    __device__ __forceinline__ static int row() { return static_cast<int>(threadIdx.x) / T; }
-    __device__ __forceinline__ static int64_t col(int v) { return (static_cast<int64_t>(v) * T + lane()) * VE; }
-};
-
-// Sums of N values over a row's threads, in all of them.  More than a
-// wavefront meets in LDS, where two buffers in turn make one barrier enough.
-template <class S, int N> struct RowSum {
-    static constexpr int kWaves = S::T / 64;
-    float (*sh)[kWaves > 0 ? kWaves : 1];
-    int turn = 0;
-    __device__ __forceinline__ void operator()(float (&v)[N]) {
-#pragma unroll
-        for (int o = (S::T < 64 ? S::T : 64) / 2; o > 0; o >>= 1)
-#pragma unroll
-            for (int n = 0; n < N; ++n) v[n] += __shfl_xor(v[n], o, 64);
-        if constexpr (kWaves > 1) {
-            const int wave = threadIdx.x >> 6;
-            if ((threadIdx.x & 63) == 0)
-#pragma unroll
-                for (int n = 0; n < N; ++n) sh[turn * N + n][wave] = v[n];
-            __syncthreads();
-#pragma unroll
-            for (int n = 0; n < N; ++n) {
-                float t = 0.f;
-#pragma unroll
-                for (int w = 0; w < kWaves; ++w) t += sh[turn * N + n][w];
-                v[n] = t;
-            }
-            turn ^= 1;
-        }
-    }
-};
 
 // A thread's copies of gamma (or 1) or beta (or 0).  Up to 8 (16 in the
 // backward) stay in registers over all rows; more come from the caches where
@@ -163,8 +62,8 @@ template <class S, class TX, class TY>
 __global__ void __launch_bounds__(S::kThreads) layer_norm_fwd_kernel(const TX *x, const int64_t *m_dev, int64_t cap_m,
                                                                      int64_t f, const float *gamma, const float *beta,
                                                                      float eps, TY *y, float *mean, float *rstd) {
-    __shared__ float sh[2][S::T > 64 ? S::T / 64 : 1];
-    RowSum<S, 1> sum{sh};
+    __shared__ typename RowReduce<S>::Shared sh;
+    RowReduce<S> over(sh);
     const int64_t M = live_rows(m_dev, cap_m);
     const float n = static_cast<float>(f);
     const Weights<S, S::E <= 8> ga(gamma, f, 1.f), be(beta, f, 0.f);
@@ -187,7 +86,7 @@ __global__ void __launch_bounds__(S::kThreads) layer_norm_fwd_kernel(const TX *x
 #pragma unroll
             for (int e = 0; e < S::VE; ++e) s[0] += o.get(e);
         }
-        sum(s);
+        over(Add{}, s);
         const float mu = s[0] / n;
         s[0] = 0.f;
 #pragma unroll(kHold ? S::NV : 1)
@@ -200,7 +99,7 @@ __global__ void __launch_bounds__(S::kThreads) layer_norm_fwd_kernel(const TX *x
                 if (S::col(v) + e < f) s[0] = fmaf(d, d, s[0]);
             }
         }
-        sum(s);
+        over(Add{}, s);
         const float q = 1.f / sqrtf(s[0] / n + eps);
         if (live) {
 #pragma unroll(kHold ? S::NV : 1)
@@ -239,8 +138,8 @@ struct BwdArgs {
 // d_x of every row, and with SUMS the workgroup's column sums.
 template <class S, class TG, class TX, bool SUMS>
 __global__ void __launch_bounds__(S::kThreads) layer_norm_bwd_kernel(BwdArgs p) {
-    __shared__ float sh[4][S::T > 64 ? S::T / 64 : 1];
-    RowSum<S, 2> sum{sh};
+    __shared__ typename RowReduce<S>::Shared sh;
+    RowReduce<S> over(sh);
     const int64_t M = live_rows(p.m_dev, p.cap_m), f = p.f;
     const TG *g = static_cast<const TG *>(p.g), *d_res = static_cast<const TG *>(p.d_res);
     const TX *x = static_cast<const TX *>(p.x);
@@ -297,7 +196,7 @@ __global__ void __launch_bounds__(S::kThreads) layer_norm_bwd_kernel(BwdArgs p) 
             }
         }
         if (!d_x) continue;
-        sum(s);
+        over(Add{}, s);
         const float m0 = s[0] / n, m1 = s[1] / n;
         if (!live) continue;
 #pragma unroll(kHold ? S::NV : 1)
