@@ -47,27 +47,44 @@ __device__ __forceinline__ Entries entries_at(float *lds, int slot, int kp) {
     return Entries{p, p + kp, reinterpret_cast<int32_t *>(p + 2 * kp)};
 }
 
-__device__ __forceinline__ float teacher_value(const DistillArgs &a, int64_t at) {
-    return a.tdt == GNN_BF16 ? bf16_to_f32(static_cast<const uint16_t *>(a.t_val)[at])
-                             : static_cast<const float *>(a.t_val)[at];
-}
-
-// Row i's class of entry e (-1: absent) and, for a present teacher's entry, its
-// value.
-__device__ __forceinline__ int32_t entry_of(const DistillArgs &a, int64_t i, int e, float *value) {
-    *value = -INFINITY;
-    if (e < a.k) {
-        if (!(a.alpha > 0.f)) return -1;
-        const int64_t id = a.t_idx[i * a.k + e];
-        const float v = teacher_value(a, i * a.k + e);
-        if (id < 0 || id >= a.c || v == -INFINITY) return -1;
-        *value = v;
-        return static_cast<int32_t>(id);
+// Entry e of row i as it lies in memory: nothing is looked at here, so that the
+// loads are still on their way when a row ahead asks for them.
+struct RawEntry {
+    int64_t id;
+    uint32_t bits;
+    __device__ __forceinline__ void load(const DistillArgs &a, int64_t i, int e) {
+        id = -1;
+        bits = 0;
+        if (e < a.k) {
+            if (!(a.alpha > 0.f)) return;
+            const int64_t at = i * a.k + e;
+            id = a.t_idx[at];
+            if (a.tdt == GNN_BF16) bits = static_cast<const uint16_t *>(a.t_val)[at];
+            else bits = static_cast<const uint32_t *>(a.t_val)[at];
+        } else if (e == a.k && a.labels && a.alpha < 1.f) {
+            id = a.labels[a.targets ? a.targets[i] : i];
+        }
     }
-    if (e > a.k || !a.labels || !(a.alpha < 1.f)) return -1;
-    const int64_t y = a.labels[a.targets ? a.targets[i] : i];
-    return y < 0 || y >= a.c ? -1 : static_cast<int32_t>(y);
-}
+};
+
+// One entry of a row: class (-1: absent), teacher's value (-infinity for the
+// label's and absent ones), the class's logit.
+struct Entry {
+    int32_t cls;
+    float value, z;
+    __device__ __forceinline__ void take(const DistillArgs &a, const RawEntry &r, int e) {
+        value = a.tdt == GNN_BF16 ? __uint_as_float(r.bits << 16) : __uint_as_float(r.bits);
+        const bool teacher = e < a.k, in = r.id >= 0 && r.id < a.c && !(teacher && value == -INFINITY);
+        cls = in ? static_cast<int32_t>(r.id) : -1;
+        if (!in || !teacher) value = -INFINITY;
+        z = 0.f;
+    }
+    __device__ __forceinline__ void load(const DistillArgs &a, int64_t i, int e) {
+        RawEntry r;
+        r.load(a, i, e);
+        take(a, r, e);
+    }
+};
 
 // The constants of a row whose maximum and sums are known.
 struct RowTerms {
@@ -107,26 +124,28 @@ __device__ __forceinline__ float row_scale_of(const DistillArgs &a, int64_t i) {
 }
 
 // Write each listed class of [lo, hi) again: its dense part less its weights.
+// A first look over the list, without branches, tells whether a class stands
+// there more than once; only then are its weights added up.
 template <bool TWO, class TG>
 __device__ __forceinline__ void put_entries(const Entries &en, const RowTerms &t, int kp, int first, int step, TG *g,
                                             int64_t lo, int64_t hi) {
     for (int e = first; e < kp; e += step) {
         const int32_t id = en.cls[e];
         if (id < 0 || id < lo || id >= hi) continue;
-        bool mine = true;
-        float w = 0.f;
+        int earlier = 0, times = 0;
+#pragma unroll 4
         for (int o = 0; o < kp; o += 4) {
             const int4 c = *reinterpret_cast<const int4 *>(en.cls + o);
-            const int32_t cc[4] = {c.x, c.y, c.z, c.w};
-            if (cc[0] != id && cc[1] != id && cc[2] != id && cc[3] != id) continue;
-#pragma unroll
-            for (int x = 0; x < 4; ++x)
-                if (cc[x] == id) {
-                    mine = mine && o + x >= e;
-                    w += en.w[o + x];
-                }
+            const int n = (c.x == id) + (c.y == id) + (c.z == id) + (c.w == id);
+            times += n;
+            earlier |= (c.x == id && o < e) | (c.y == id && o + 1 < e) | (c.z == id && o + 2 < e) | (c.w == id && o + 3 < e);
         }
-        if (mine) Elem<TG>::store(g, id, t.dense<TWO>(en.z[e]) - w);
+        if (earlier) continue;
+        float w = en.w[e];
+        if (times > 1)
+            for (int o = e + 1; o < kp; ++o)
+                if (en.cls[o] == id) w += en.w[o];
+        Elem<TG>::store(g, id, t.dense<TWO>(en.z[e]) - w);
     }
 }
 
@@ -134,115 +153,251 @@ __device__ __forceinline__ void put_entries(const Entries &en, const RowTerms &t
 // rows in registers
 // ---------------------------------------------------------------------------
 
-// A thread's share of a row of c elements: the vectors that are whole in all of
-// the row's threads (`full` of them, at most NV, the same in every thread), and
-// the one after them, of which the row's end leaves some threads a part or
-// nothing.  One uniform count in place of every vector's bounds keeps those out
-// of the registers: with bounds, 1,024 threads x 128 elements spilled 154.
-template <class S, class TL> struct RowRegs {
-    Vec<TL, S::VE> r[S::NV], tail;
-    int full, rest;  // rest: elements of `tail` that belong to the row (of this thread)
-    static constexpr int64_t kMost = static_cast<int64_t>(S::T) * (S::E + S::VE) - 1;  // longest row
-    __device__ __forceinline__ explicit RowRegs(int64_t c) {
-        full = static_cast<int>(c / (S::T * S::VE));
-        rest = static_cast<int>(c) - (full * S::T + S::lane()) * S::VE;
+// A thread's share of a row of c elements, in vectors that lie at 16-byte
+// addresses whatever the row's own (a row of 100,003 bf16 classes read and
+// written off them took 18% longer than one of 100,000).  `full` vectors hold
+// elements in all of the row's threads (at most NV, the same in every thread);
+// the one after them is the row's end, of which some threads have a part or
+// nothing; the row's first thread has less of the first one.  One uniform count
+// in place of every vector's bounds keeps those out of the registers: with
+// bounds, 1,024 threads x 128 elements spilled 154.
+template <class S, class TL> struct Span {
+    int head, full, rest;  // elements before the row in its first vector; see above; elements from the tail's place to the row's end
+    static constexpr int64_t kMost = static_cast<int64_t>(S::T) * (S::E + S::VE) - S::VE;  // longest row
+    static constexpr int kStep = S::T * S::VE;
+    __device__ __forceinline__ Span(const TL *row, int64_t c) {
+        head = static_cast<int>((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(TL)) % S::VE;
+        full = static_cast<int>(c + head) / kStep;
+        rest = static_cast<int>(c) + head - (full * S::T + S::lane()) * S::VE;
     }
     __device__ __forceinline__ static uint32_t off() { return static_cast<uint32_t>(S::lane()) * S::VE; }
-    template <class F> __device__ __forceinline__ void each(F &&go) {
-#pragma unroll
-        for (int v = 0; v < S::NV; ++v)
-            if (v < full) go(r[v]);
-        go(tail);
+    __device__ __forceinline__ bool first(int v) const { return v == 0 && head != 0 && S::lane() == 0; }
+    template <class T> __device__ __forceinline__ T *at(T *row, int v) const { return row - head + v * kStep + off(); }
+    __device__ __forceinline__ void load(Vec<TL, S::VE> &x, const TL *row, int v) const {
+        if (first(v)) x.load_some(at(row, v), head, S::VE, -INFINITY);
+        else x.load(at(row, v));
     }
-    __device__ __forceinline__ void load(const TL *row, int v) { r[v].load(row + v * (S::T * S::VE) + off()); }
-    __device__ __forceinline__ void load_tail(const TL *row) {
-        tail.load_upto(row + full * (S::T * S::VE) + off(), rest, -INFINITY);
+    __device__ __forceinline__ void load_tail(Vec<TL, S::VE> &x, const TL *row) const {
+        if (rest >= S::VE && !first(full)) x.load(at(row, full));
+        else x.load_some(at(row, full), first(full) ? head : 0, rest, -INFINITY);
     }
-    __device__ __forceinline__ void load(const TL *row) {
-#pragma unroll
-        for (int v = 0; v < S::NV; ++v)
-            if (v < full) load(row, v);
-        load_tail(row);
+    template <class T> __device__ __forceinline__ void store(const Vec<T, S::VE> &x, T *row, int v) const {
+        if (first(v)) x.store_some(at(row, v), head, S::VE);
+        else x.store(at(row, v));
+    }
+    template <class T> __device__ __forceinline__ void store_tail(const Vec<T, S::VE> &x, T *row) const {
+        if (rest >= S::VE && !first(full)) x.store(at(row, full));
+        else x.store_some(at(row, full), first(full) ? head : 0, rest);
     }
 };
 
-// Workgroups to a CU that the registers are to leave room for.
-template <class S> constexpr int waves_wanted() { return S::T >= 512 ? 4 : 1; }
+// A thread's running maximum and the sums relative to it.
+template <bool TWO> struct Online {
+    float m = -INFINITY, sa = 0.f, sb = 0.f;
+    // nothing but -infinity so far: distances are from 0 (a NaN is kept by the sums)
+    __device__ __forceinline__ float from() const { return m == -INFINITY ? 0.f : m; }
+    template <class V, int VE> __device__ __forceinline__ void add(const V &x, float ka, float kb) {
+        float top = x.get(0);
+#pragma unroll
+        for (int e = 1; e < VE; ++e) top = fmaxf(top, x.get(e));
+        if (top > m) {
+            sa *= exp2_of((m - top) * ka);
+            if constexpr (TWO) sb *= exp2_of((m - top) * kb);
+            m = top;
+        }
+        const float at = from();
+#pragma unroll
+        for (int e = 0; e < VE; ++e) {
+            const float d = x.get(e) - at;
+            sa += exp2_of(d * ka);
+            if constexpr (TWO) sb += exp2_of(d * kb);
+        }
+    }
+    // the sums relative to `top`, which is at least m
+    __device__ __forceinline__ void to(float top, float ka, float kb) {
+        const float d = m == top ? 0.f : m - top;
+        sa *= exp2_of(d * ka);
+        if constexpr (TWO) sb *= exp2_of(d * kb);
+    }
+};
 
+// Maxima and sums over a row's threads with one meeting: a wavefront's in
+// registers, then each wavefront joins all of theirs from LDS by itself.
+// tm, ts: the teacher's.
+template <class S> struct Meeting {
+    static constexpr int kWaves = S::T > 64 ? S::T / 64 : 1;
+    typedef float Shared[2][5][kWaves];
+    static constexpr int kIn = S::T < 64 ? S::T : 64;
+    template <int W, class Op> __device__ __forceinline__ static float fold(Op op, float v) {
+#pragma unroll
+        for (int o = W / 2; o > 0; o >>= 1) v = op(v, __shfl_xor(v, o, 64));
+        return v;
+    }
+    // each thread's own: `on`, and its entries' largest value; sum(tm) is its
+    // entries' sum relative to tm
+    template <bool TWO, class F>
+    __device__ __forceinline__ static void inside(Online<TWO> &on, float &tm, float &ts, float ka, float kb, F &&sum) {
+        const float top = fold<kIn>(Max{}, on.m);
+        tm = fold<kIn>(Max{}, tm);
+        on.to(top, ka, kb);
+        on.m = top;
+        on.sa = fold<kIn>(Add{}, on.sa);
+        if constexpr (TWO) on.sb = fold<kIn>(Add{}, on.sb);
+        ts = fold<kIn>(Add{}, sum(tm));
+    }
+    template <bool TWO> __device__ __forceinline__ static void put(Shared &sh, int turn, const Online<TWO> &on, float tm, float ts) {
+        if constexpr (kWaves > 1)
+            if ((threadIdx.x & 63) == 0) {
+                const int w = threadIdx.x >> 6;
+                sh[turn][0][w] = on.m;
+                sh[turn][1][w] = on.sa;
+                if constexpr (TWO) sh[turn][2][w] = on.sb;
+                sh[turn][3][w] = tm;
+                sh[turn][4][w] = ts;
+            }
+    }
+    template <bool TWO>
+    __device__ __forceinline__ static void join(const Shared &sh, int turn, Online<TWO> &on, float &tm, float &ts, float kt,
+                                                float ka, float kb) {
+        if constexpr (kWaves > 1) {
+            const int w = threadIdx.x % kWaves;
+            on.m = sh[turn][0][w];
+            on.sa = sh[turn][1][w];
+            if constexpr (TWO) on.sb = sh[turn][2][w];
+            tm = sh[turn][3][w];
+            ts = sh[turn][4][w];
+            const float top = fold<kWaves>(Max{}, on.m), t_top = fold<kWaves>(Max{}, tm);
+            on.to(top, ka, kb);
+            on.m = top;
+            on.sa = fold<kWaves>(Add{}, on.sa);
+            if constexpr (TWO) on.sb = fold<kWaves>(Add{}, on.sb);
+            ts = fold<kWaves>(Add{}, ts * exp2_of(tm == t_top ? 0.f : (tm - t_top) * kt));
+            tm = t_top;
+        }
+    }
+};
+
+// Wavefronts to a SIMD that the registers are to leave room for.
+template <class S> constexpr int waves_wanted() { return S::T >= 512 ? 4 : 1; }
+// Vectors between a load and its use: a vector of 1,024 threads takes a CU's
+// share of the memory 1.6 us, in and out.
+constexpr int kLag = 2;
+// Sets of entries: a row's are read until after the next row's meeting, when a
+// thread may be at the row after that.
+constexpr int kSets = 3;
+
+// A row passes one meeting of its threads, after which its constants are known;
+// what is left of the row before (its listed classes' second store, its loss) is
+// done after the same meeting, which orders it behind that row's dense stores.
 template <class S, class TL, class TG, bool TWO>
 __global__ void __launch_bounds__(S::kThreads, waves_wanted<S>()) distill_rows_kernel(DistillArgs a, float *row_loss) {
     extern __shared__ __attribute__((aligned(16))) float lds[];
-    __shared__ typename RowReduce<S>::Shared sh;
-    RowReduce<S> over(sh);
+    typedef Meeting<S> Meet;
+    __shared__ typename Meet::Shared sh;
+    __shared__ float sh_loss[2][Meet::kWaves];
+    typedef Vec<TL, S::VE> V;
     const int kp = entries_padded(a.k), lane = S::lane();
     const int64_t c = a.c, step = static_cast<int64_t>(gridDim.x) * S::kRows;
     const TL *logits = static_cast<const TL *>(a.logits);
     TG *grad = static_cast<TG *>(a.g_out);
+    const float ka = factor_a(a), kb = kLog2e, inv_t = 1.f / a.temperature, kt = inv_t * kLog2e;
     int64_t i = static_cast<int64_t>(blockIdx.x) * S::kRows + S::row();
     if (i >= a.b) return;  // threads of whole rows; above 64 a workgroup has one
-    RowRegs<S, TL> r(c);
+    V r[S::NV], tail;
+    Span<S, TL> span(logits + i * c, c);
+    Online<TWO> on;
+    // the first entry of each thread is fetched a row ahead
+    Entry mine{-1, -INFINITY, 0.f};
     float scale = row_scale_of(a, i);
-    if (scale != 0.f) r.load(logits + i * c);
-    for (int turn = 0; i < a.b; i += step, turn ^= 1) {
+    if (scale != 0.f) {
+        const TL *z = logits + i * c;
+#pragma unroll
+        for (int v = 0; v < S::NV; ++v)
+            if (v < span.full) span.load(r[v], z, v);
+        span.load_tail(tail, z);
+        if (lane < kp) mine.load(a, i, lane);
+        if (mine.cls >= 0) mine.z = Elem<TL>::load(z, mine.cls);
+#pragma unroll
+        for (int v = 0; v < S::NV; ++v)
+            if (v < span.full) on.template add<V, S::VE>(r[v], ka, kb);
+        on.template add<V, S::VE>(tail, ka, kb);
+    }
+    // the row before: its constants, its entries' set and where its gradient is
+    RowTerms tp{0.f, ka, kb, 0.f, 0.f, false};
+    int set = 0, turn = 0;
+    int64_t before = -1;
+    auto finish_before = [&]() {
+        if (before < 0) return;
+        const Entries en = entries_at(lds, S::row() * kSets + (set + kSets - 1) % kSets, kp);
+        if (grad && tp.any) put_entries<TWO>(en, tp, kp, lane, S::T, grad + before * c, 0, c);
+        if (lane == 0) {
+            float l = 0.f;
+#pragma unroll
+            for (int w = 0; w < Meet::kWaves; ++w) l += sh_loss[turn ^ 1][w];
+            if constexpr (Meet::kWaves > 1) row_loss[before] = l;
+        }
+    };
+    for (; i < a.b; i += step) {
         const int64_t next = i + step;
         const float next_scale = next < a.b ? row_scale_of(a, next) : 0.f;
-        RowTerms t{0.f, factor_a(a), kLog2e, 0.f, 0.f, false};
-        // two sets of entries in turn: a row's are read until its last store
-        const Entries en = entries_at(lds, S::row() * 2 + turn, kp);
-        float loss = 0.f;
+        RawEntry coming{-1, 0};
+        if (next_scale != 0.f && lane < kp) coming.load(a, next, lane);
+        const Entries en = entries_at(lds, S::row() * kSets + set, kp);
+        float tm = -INFINITY, ts = 0.f;
         if (scale != 0.f) {
-            float mx[2] = {-INFINITY, -INFINITY};
             for (int e = lane; e < kp; e += S::T) {
-                float value;
-                const int32_t id = entry_of(a, i, e, &value);
-                en.cls[e] = id;
-                en.w[e] = value;
-                if (id >= 0) en.z[e] = Elem<TL>::load(logits, i * c + id);
-                mx[1] = fmaxf(mx[1], value);
-            }
-            r.each([&](Vec<TL, S::VE> &x) {
-#pragma unroll
-                for (int e = 0; e < S::VE; ++e) mx[0] = fmaxf(mx[0], x.get(e));
-                x.pin();
-            });
-            over(Max{}, mx);
-            if constexpr (S::T <= 64) row_sync<S>();
-            t.m = mx[0];
-            float s[3] = {0.f, 0.f, 0.f};
-            r.each([&](Vec<TL, S::VE> &x) {
-#pragma unroll
-                for (int e = 0; e < S::VE; ++e) {
-                    const float d = x.get(e) - t.m;
-                    s[0] += exp2_of(d * t.ka);
-                    if constexpr (TWO) s[1] += exp2_of(d * t.kb);
+                Entry x = mine;
+                if (e >= S::T) {
+                    x.load(a, i, e);
+                    if (x.cls >= 0) x.z = Elem<TL>::load(logits, i * c + x.cls);
                 }
-                x.pin();
+                en.cls[e] = x.cls;
+                en.w[e] = x.value;
+                en.z[e] = x.z;
+                tm = fmaxf(tm, x.value);
+            }
+            Meet::template inside<TWO>(on, tm, ts, ka, kb, [&](float top) {
+                float x = 0.f;
+                for (int e = lane; e < kp; e += S::T)
+                    if (en.cls[e] >= 0 && e < a.k) x += exp2_of((en.w[e] - top) * kt);
+                return x;
             });
-            const float inv_t = 1.f / a.temperature;
-            for (int e = lane; e < kp; e += S::T)
-                if (en.cls[e] >= 0 && e < a.k) s[2] += exp2_of((en.w[e] - mx[1]) * inv_t * kLog2e);
-            over(Add{}, s);
-            const float s1 = TWO ? s[1] : s[0];
-            const LossTerms lt{a.alpha, a.temperature, inv_t, scale, mx[1], s[2], logf(s[2]), t.m, logf(s[0]), logf(s1)};
-            const bool soft = s[2] != 0.f, hard = en.cls[a.k] >= 0;
-            float l[1] = {0.f};
+            Meet::template put<TWO>(sh, turn, on, tm, ts);
+        }
+        row_sync<S>();
+        finish_before();
+        RowTerms t{0.f, ka, kb, 0.f, 0.f, false};
+        float l = 0.f;
+        if (scale != 0.f) {
+            Meet::template join<TWO>(sh, turn, on, tm, ts, kt, ka, kb);
+            t.m = on.m;
+            const float s1 = TWO ? on.sb : on.sa;
+            const LossTerms lt{a.alpha, a.temperature, inv_t, scale, tm, ts, logf(ts), t.m, logf(on.sa), logf(s1)};
+            const bool soft = ts != 0.f, hard = en.cls[a.k] >= 0;
             for (int e = lane; e < kp; e += S::T) {
                 float w = 0.f;
-                if (en.cls[e] >= 0) l[0] += e < a.k ? lt.teacher(en.w[e], en.z[e], &w) : lt.label(en.z[e], &w);
+                if (en.cls[e] >= 0) l += e < a.k ? lt.teacher(en.w[e], en.z[e], &w) : lt.label(en.z[e], &w);
                 en.w[e] = w;
             }
-            over(Add{}, l);
-            loss = l[0];
+            l = Meet::template fold<Meet::kIn>(Add{}, l);
             t.any = soft || hard;
             const float cs = soft ? scale * a.alpha * a.temperature : 0.f, ch = hard ? scale * (1.f - a.alpha) : 0.f;
-            t.ca = TWO ? cs / s[0] : (cs + ch) / s[0];
+            t.ca = TWO ? cs / on.sa : (cs + ch) / on.sa;
             t.cb = ch / s1;
         }
-        if (lane == 0) row_loss[i] = loss;
-        // the gradient, vector by vector, and the next row into its registers
-        const TL *ahead = logits + next * c;
+        if constexpr (Meet::kWaves > 1) {
+            if ((threadIdx.x & 63) == 0) sh_loss[turn][threadIdx.x >> 6] = l;
+        } else {
+            if (lane == 0) row_loss[i] = l;
+        }
+        const TL *below = logits + next * c;
+        Entry ahead;
+        ahead.take(a, coming, lane);
+        if (ahead.cls >= 0) ahead.z = Elem<TL>::load(below, ahead.cls);
+        // the gradient, vector by vector; the next row into its registers, and
+        // its maximum and sums kLag vectors behind
         TG *g = grad + i * c;
-        auto dense = [&](const Vec<TL, S::VE> &x) {
+        auto dense = [&](const V &x) {
             float o[S::VE];
 #pragma unroll
             for (int e = 0; e < S::VE; ++e) o[e] = t.any ? t.dense<TWO>(x.get(e)) : 0.f;
@@ -250,20 +405,39 @@ __global__ void __launch_bounds__(S::kThreads, waves_wanted<S>()) distill_rows_k
             w.set(o);
             return w;
         };
+        on = Online<TWO>{};
+        auto take = [&](V &x) {
+            on.template add<V, S::VE>(x, ka, kb);
+            x.pin();
+        };
+        const Span<S, TL> to(below, c);
+        const int to_full = next_scale != 0.f ? to.full : 0;
+        if (grad) span.store_tail(dense(tail), g);
 #pragma unroll
-        for (int v = 0; v < S::NV; ++v)
-            if (v < r.full) {
-                if (grad) dense(r.r[v]).store(g + v * (S::T * S::VE) + r.off());
-                if (next_scale != 0.f) r.load(ahead, v);
+        for (int v = 0; v < S::NV; ++v) {
+            if (grad && v < span.full) span.store(dense(r[v]), g, v);
+            if (v < to_full) {
+                to.load(r[v], below, v);
+                if (v >= kLag) take(r[v >= kLag ? v - kLag : 0]);
             }
-        if (grad) dense(r.tail).store_upto(g + r.full * (S::T * S::VE) + r.off(), r.rest);
-        if (next_scale != 0.f) r.load_tail(ahead);
-        if (grad) {
-            row_sync<S>();
-            if (t.any) put_entries<TWO>(en, t, kp, lane, S::T, g, 0, c);
         }
+        if (next_scale != 0.f) {
+            to.load_tail(tail, below);
+#pragma unroll
+            for (int v = 0; v < S::NV; ++v)
+                if (v < to_full && v >= to_full - kLag) take(r[v]);
+            take(tail);
+        }
+        before = i;
+        tp = t;
+        span = to;
+        mine = ahead;
         scale = next_scale;
+        set = (set + 1) % kSets;
+        turn ^= 1;
     }
+    row_sync<S>();
+    finish_before();
 }
 
 // ---------------------------------------------------------------------------
@@ -293,38 +467,22 @@ __global__ void __launch_bounds__(kSplitThreads) distill_part_kernel(DistillArgs
     const int kp = entries_padded(a.k);
     if (part == 0)
         for (int e = threadIdx.x; e < kp; e += kSplitThreads) {
-            float value;
-            const int32_t id = entry_of(a, i, e, &value);
-            if (id >= 0) st.z[i * kp + e] = Elem<TL>::load(z, id);
+            Entry x;
+            x.load(a, i, e);
+            if (x.cls >= 0) st.z[i * kp + e] = Elem<TL>::load(z, x.cls);
         }
     const float ka = factor_a(a), kb = kLog2e;
-    // each thread's own running maximum; sums move to a new one as it comes
-    float m = -INFINITY, sa = 0.f, sb = 0.f;
+    Online<TWO> on;
     for (int64_t c0 = lo; c0 < hi; c0 += kSplitThreads * S::VE) {
         Vec<TL, S::VE> r;
         const int64_t c = c0 + S::col(0);
         r.load_upto(z + c, hi - c, -INFINITY);
-        float top = r.get(0);
-#pragma unroll
-        for (int e = 1; e < S::VE; ++e) top = fmaxf(top, r.get(e));
-        if (top > m) {
-            sa *= exp2_of((m - top) * ka);
-            if constexpr (TWO) sb *= exp2_of((m - top) * kb);
-            m = top;
-        }
-        // nothing but -infinity so far (or a NaN, which the sums keep)
-        const float at = m == -INFINITY ? 0.f : m;
-#pragma unroll
-        for (int e = 0; e < S::VE; ++e) {
-            const float d = r.get(e) - at;
-            sa += exp2_of(d * ka);
-            if constexpr (TWO) sb += exp2_of(d * kb);
-        }
+        on.template add<Vec<TL, S::VE>, S::VE>(r, ka, kb);
     }
-    float top[1] = {m};
+    float top[1] = {on.m};
     over(Max{}, top);
-    const float at = top[0] == -INFINITY ? 0.f : top[0], own = m == -INFINITY ? at : m;
-    float s[2] = {sa * exp2_of((own - at) * ka), TWO ? sb * exp2_of((own - at) * kb) : 0.f};
+    on.to(top[0], ka, kb);
+    float s[2] = {on.sa, on.sb};
     over(Add{}, s);
     if (threadIdx.x == 0) {
         float *o = st.stats + (i * p.parts + part) * 3;
@@ -356,19 +514,19 @@ __global__ void __launch_bounds__(kSplitThreads) distill_join_kernel(DistillArgs
         float mx[2] = {-INFINITY, -INFINITY};
         for (int64_t e = threadIdx.x; e < p.parts; e += kSplitThreads) mx[0] = fmaxf(mx[0], q[e * 3]);
         for (int e = threadIdx.x; e < kp; e += kSplitThreads) {
-            float value;
-            const int32_t id = entry_of(a, i, e, &value);
-            en.cls[e] = id;
-            en.w[e] = value;
-            if (id >= 0) en.z[e] = st.z[i * kp + e];
-            mx[1] = fmaxf(mx[1], value);
+            Entry x;
+            x.load(a, i, e);
+            en.cls[e] = x.cls;
+            en.w[e] = x.value;
+            if (x.cls >= 0) en.z[e] = st.z[i * kp + e];
+            mx[1] = fmaxf(mx[1], x.value);
         }
         over(Max{}, mx);
         t.m = mx[0];
         const float inv_t = 1.f / a.temperature;
         float s[3] = {0.f, 0.f, 0.f};
         for (int64_t e = threadIdx.x; e < p.parts; e += kSplitThreads) {
-            const float d = q[e * 3] == -INFINITY && t.m != -INFINITY ? -INFINITY : q[e * 3] - t.m;
+            const float d = q[e * 3] == t.m ? 0.f : q[e * 3] - t.m;
             s[0] += q[e * 3 + 1] * exp2_of(d * t.ka);
             if constexpr (TWO) s[1] += q[e * 3 + 2] * exp2_of(d * t.kb);
         }
@@ -430,20 +588,24 @@ __global__ void __launch_bounds__(kLossThreads) distill_loss_kernel(const float 
 }
 
 // The shape of a row of c classes in registers: at most 68 words a thread.
-template <class S, class F> bool if_fits(int64_t c, F &&go) {
-    if (c > RowRegs<S, float>::kMost) return false;
+// Long lists take a workgroup to a row: the sets of all its rows' entries lie in
+// LDS (64 KB hold 112 entries of 16 rows, 454 of four).
+template <class S, class F> bool if_fits(int64_t c, int64_t k, F &&go) {
+    if (c > Span<S, float>::kMost || kSets * S::kRows * entries_padded(k) * 12 > (64 << 10)) return false;
     go(S{});
     return true;
 }
-template <int VE, bool BF16, class F> bool with_shape(int64_t c, F &&go) {
-    return if_fits<Shape<16, 8, VE>>(c, go) || if_fits<Shape<64, 8, VE>>(c, go) || if_fits<Shape<64, 16, VE>>(c, go) ||
-           if_fits<Shape<256, 16, VE>>(c, go) || if_fits<Shape<256, 32, VE>>(c, go) ||
-           if_fits<Shape<256, 64, VE>>(c, go) || if_fits<Shape<512, 64, VE>>(c, go) ||
-           if_fits<Shape<1024, 64, VE>>(c, go) || (BF16 && if_fits<Shape<1024, BF16 ? 128 : 64, VE>>(c, go));
+template <int VE, bool BF16, class F> bool with_shape(int64_t c, int64_t k, F &&go) {
+    return if_fits<Shape<16, 8, VE>>(c, k, go) || if_fits<Shape<64, 8, VE>>(c, k, go) ||
+           if_fits<Shape<64, 16, VE>>(c, k, go) || if_fits<Shape<64, 32, VE>>(c, k, go) ||
+           if_fits<Shape<64, 64, VE>>(c, k, go) || if_fits<Shape<256, 32, VE>>(c, k, go) ||
+           if_fits<Shape<256, 64, VE>>(c, k, go) ||
+           if_fits<Shape<512, 64, VE>>(c, k, go) || if_fits<Shape<1024, 64, VE>>(c, k, go) ||
+           (BF16 && if_fits<Shape<1024, BF16 ? 128 : 64, VE>>(c, k, go));
 }
 
 // Classes of a row in registers, fp32 (with a gradient of either type) and bf16.
-constexpr int64_t kRowsMax[2] = {RowRegs<Shape<1024, 64, 4>, float>::kMost, RowRegs<Shape<1024, 128, 8>, uint16_t>::kMost};
+constexpr int64_t kRowsMax[2] = {Span<Shape<1024, 64, 4>, float>::kMost, Span<Shape<1024, 128, 8>, uint16_t>::kMost};
 
 // Rows are split when they do not fit, and where so few of 8,192 classes and
 // more come that most CUs would have none.
@@ -494,13 +656,13 @@ gnn_status launch_distill(const DistillArgs &a, void *ws, hipStream_t s) {
                 distill_join_kernel<TL, TG, TWO><<<grid, kSplitThreads, entry_bytes, s>>>(a, p, st, row_loss);
                 return;
             }
-            with_shape<sizeof(TL) == 4 ? 4 : 8, sizeof(TL) == 2>(a.c, [&](auto shape) {
+            with_shape<sizeof(TL) == 4 ? 4 : 8, sizeof(TL) == 2>(a.c, a.k, [&](auto shape) {
                 using S = decltype(shape);
                 // one round of the CUs with what fits on each: workgroups walk
                 // their rows and load each ahead
                 const int64_t grid = std::min<int64_t>(ceil_div(a.b, S::kRows), kCus * (S::T >= 256 ? 1024 / S::T : 8));
                 distill_rows_kernel<S, TL, TG, TWO>
-                    <<<static_cast<unsigned>(grid), S::kThreads, 2 * S::kRows * entry_bytes, s>>>(a, row_loss);
+                    <<<static_cast<unsigned>(grid), S::kThreads, kSets * S::kRows * entry_bytes, s>>>(a, row_loss);
             });
         };
         auto by_two = [&](auto tl, auto tg) {

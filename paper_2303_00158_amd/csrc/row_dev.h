@@ -57,25 +57,25 @@ template <class T, int VE> struct Vec {
 #pragma unroll
         for (int i = 0; i < kWords; ++i) asm volatile("" : "+v"(w[i]));
     }
-    // elements [0, n) of p, n below VE; the rest are `fill`
-    __device__ __forceinline__ void load_some(const T *p, int n, float fill) {
+    // elements [lo, hi) of p; the rest are `fill`, or are not written
+    __device__ __forceinline__ void load_some(const T *p, int lo, int hi, float fill) {
         float x[VE];
 #pragma unroll
-        for (int e = 0; e < VE; ++e) x[e] = e < n ? Elem<T>::load(p, e) : fill;
+        for (int e = 0; e < VE; ++e) x[e] = e >= lo && e < hi ? Elem<T>::load(p, e) : fill;
         set(x);
     }
-    __device__ __forceinline__ void store_some(T *p, int n) const {
+    __device__ __forceinline__ void store_some(T *p, int lo, int hi) const {
 #pragma unroll
         for (int e = 0; e < VE; ++e)
-            if (e < n) Elem<T>::store(p, e, get(e));
+            if (e >= lo && e < hi) Elem<T>::store(p, e, get(e));
     }
     __device__ __forceinline__ void load_upto(const T *p, int64_t n, float fill = 0.f) {
         if (n >= VE) load(p);
-        else load_some(p, static_cast<int>(max(n, int64_t(0))), fill);
+        else load_some(p, 0, static_cast<int>(max(n, int64_t(0))), fill);
     }
     __device__ __forceinline__ void store_upto(T *p, int64_t n) const {
         if (n >= VE) store(p);
-        else store_some(p, static_cast<int>(max(n, int64_t(0))));
+        else store_some(p, 0, static_cast<int>(max(n, int64_t(0))));
     }
 };
 
@@ -85,7 +85,12 @@ template <int T_, int E_, int VE_> struct Shape {
     static constexpr int kThreads = T > 256 ? T : 256;
     static constexpr int kRows = kThreads / T;  // rows of a workgroup at a time
     __device__ __forceinline__ static int lane() { return static_cast<int>(threadIdx.x) % T; }
-    __device__ __forceinline__ static int row() { return kRows == 1 ? 0 : static_cast<int>(threadIdx.x) / T; }
+    // one value in a wavefront's scalar registers where a row is a wavefront's
+    __device__ __forceinline__ static int row() {
+        if constexpr (kRows == 1) return 0;
+        const int r = static_cast<int>(threadIdx.x) / T;
+        return T == 64 ? __builtin_amdgcn_readfirstlane(r) : r;
+    }
     __device__ __forceinline__ static int64_t col(int v) { return (static_cast<int64_t>(v) * T + lane()) * VE; }
 };
 

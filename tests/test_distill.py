@@ -125,7 +125,11 @@ def check(z, t, idx, temp, alpha=1.0, labels=None, scale=None, gdt=None, **kw):
 
 SIZES = [(1, 1, 1), (3, 2, 2), (5, 7, 3), (64, 47, 8), (33, 172, 5), (16, 255, 16), (9, 256, 4), (7, 1000, 64), (5, 1023, 33), (4, 1025, 100), (6, 2049, 10),
          (3, 4096, 128), (4, 8191, 7), (2, 10_000, 256), (3, 16_385, 64), (2, 32_768, 20), (1, 50_001, 64), (3, 65_537, 1000),
-         (2, 131_072, 64), (1, 200_003, 1024), (1, 1 << 20, 3), (300, 3000, 6), (700, 10, 3)]
+         (2, 131_072, 64), (1, 200_003, 1024), (1, 1 << 20, 3), (300, 3000, 6), (700, 10, 3),
+         # long lists over few classes, every shape's longest row and the next one
+         (40, 30, 112), (40, 30, 113), (9, 250, 454), (9, 250, 455), (3, 12, 1024), (20, 248, 9), (20, 249, 9), (9, 1016, 5),
+         (9, 1017, 5), (6, 1528, 5), (6, 1529, 5), (3, 6136, 5), (3, 6145, 5), (2, 10_232, 5), (2, 18_433, 3), (130, 8192, 4),
+         (140, 36_856, 3), (140, 36_865, 3), (129, 69_628, 3), (129, 73_725, 3), (129, 139_256, 3), (129, 139_257, 3), (2, 139_300, 3)]
 
 
 @pytest.mark.gpu
