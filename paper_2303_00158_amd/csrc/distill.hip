@@ -153,41 +153,55 @@ __device__ __forceinline__ void put_entries(const Entries &en, const RowTerms &t
 // rows in registers
 // ---------------------------------------------------------------------------
 
-// A thread's share of a row of c elements, in vectors that lie at 16-byte
-// addresses whatever the row's own (a row of 100,003 bf16 classes read and
-// written off them took 18% longer than one of 100,000).  `full` vectors hold
-// elements in all of the row's threads (at most NV, the same in every thread);
-// the one after them is the row's end, of which some threads have a part or
-// nothing; the row's first thread has less of the first one.  One uniform count
-// in place of every vector's bounds keeps those out of the registers: with
-// bounds, 1,024 threads x 128 elements spilled 154.
+// A thread's share of a row of c elements, in vectors that lie in whole 128-byte
+// lines whatever the row's own address (off them a row of 100,003 bf16 classes
+// took 18% longer than one of 100,000).  `full` vectors hold elements in all of
+// the row's threads (at most NV, the same in every thread) but for the first
+// line's; the one after them is the row's end, of which some threads have a
+// part or nothing.  One uniform count in place of every vector's bounds keeps
+// those out of the registers: with bounds, 1,024 threads x 128 elements spilled
+// 154.  Where a thread's vector reaches over the row's start or end, the row's
+// first or last VE elements are loaded in its place, and those that are other
+// threads' are masked when it is used (trim): nothing waits for the load.
 template <class S, class TL> struct Span {
-    int head, full, rest;  // elements before the row in its first vector; see above; elements from the tail's place to the row's end
-    static constexpr int64_t kMost = static_cast<int64_t>(S::T) * (S::E + S::VE) - S::VE;  // longest row
+    int c, head, full, rest;  // head: elements from the line to the row; rest: from the tail's place to the row's end
+    static constexpr int kLine = 128 / sizeof(TL);
+    static constexpr int64_t kMost = static_cast<int64_t>(S::T) * (S::E + S::VE) - kLine;  // longest row
     static constexpr int kStep = S::T * S::VE;
-    __device__ __forceinline__ Span(const TL *row, int64_t c) {
-        head = static_cast<int>((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(TL)) % S::VE;
-        full = static_cast<int>(c + head) / kStep;
-        rest = static_cast<int>(c) + head - (full * S::T + S::lane()) * S::VE;
+    __device__ __forceinline__ Span(const TL *row, int64_t c_) {
+        c = static_cast<int>(c_);
+        head = static_cast<int>((reinterpret_cast<uintptr_t>(row) & 127) / sizeof(TL));
+        full = (c + head) / kStep;
+        rest = c + head - (full * S::T + S::lane()) * S::VE;
     }
     __device__ __forceinline__ static uint32_t off() { return static_cast<uint32_t>(S::lane()) * S::VE; }
-    __device__ __forceinline__ bool first(int v) const { return v == 0 && head != 0 && S::lane() == 0; }
+    __device__ __forceinline__ int skip() const { return head - S::lane() * S::VE; }  // of the first vector, before the row
+    __device__ __forceinline__ bool first(int v) const { return v == 0 && skip() > 0; }
     template <class T> __device__ __forceinline__ T *at(T *row, int v) const { return row - head + v * kStep + off(); }
+    // a whole vector (v < full)
     __device__ __forceinline__ void load(Vec<TL, S::VE> &x, const TL *row, int v) const {
-        if (first(v)) x.load_some(at(row, v), head, S::VE, -INFINITY);
-        else x.load(at(row, v));
+        x.load(first(v) ? row : at(row, v));
     }
-    __device__ __forceinline__ void load_tail(Vec<TL, S::VE> &x, const TL *row) const {
-        if (rest >= S::VE && !first(full)) x.load(at(row, full));
-        else x.load_some(at(row, full), first(full) ? head : 0, rest, -INFINITY);
+    __device__ __forceinline__ void trim(Vec<TL, S::VE> &x, int v) const {
+        if (first(v)) x.keep(0, S::VE - skip());
     }
     template <class T> __device__ __forceinline__ void store(const Vec<T, S::VE> &x, T *row, int v) const {
-        if (first(v)) x.store_some(at(row, v), head, S::VE);
+        if (first(v)) x.store_some(row, 0, S::VE - skip());
         else x.store(at(row, v));
     }
+    // the row's end; rows of less than one whole vector a thread are taken
+    // element by element
+    __device__ __forceinline__ void load_tail(Vec<TL, S::VE> &x, const TL *row) const {
+        if (full == 0) x.load_some(at(row, 0), max(skip(), 0), rest, -INFINITY);
+        else x.load(rest >= S::VE ? at(row, full) : row + c - S::VE);
+    }
+    __device__ __forceinline__ void trim_tail(Vec<TL, S::VE> &x) const {
+        if (full != 0 && rest < S::VE) x.keep(S::VE - max(rest, 0), S::VE);
+    }
     template <class T> __device__ __forceinline__ void store_tail(const Vec<T, S::VE> &x, T *row) const {
-        if (rest >= S::VE && !first(full)) x.store(at(row, full));
-        else x.store_some(at(row, full), first(full) ? head : 0, rest);
+        if (full == 0) x.store_some(at(row, 0), max(skip(), 0), rest);
+        else if (rest >= S::VE) x.store(at(row, full));
+        else if (rest > 0) x.store_some(row + c - S::VE, S::VE - rest, S::VE);
     }
 };
 
@@ -319,7 +333,11 @@ __global__ void __launch_bounds__(S::kThreads, waves_wanted<S>()) distill_rows_k
         if (mine.cls >= 0) mine.z = Elem<TL>::load(z, mine.cls);
 #pragma unroll
         for (int v = 0; v < S::NV; ++v)
-            if (v < span.full) on.template add<V, S::VE>(r[v], ka, kb);
+            if (v < span.full) {
+                span.trim(r[v], v);
+                on.template add<V, S::VE>(r[v], ka, kb);
+            }
+        span.trim_tail(tail);
         on.template add<V, S::VE>(tail, ka, kb);
     }
     // the row before: its constants, its entries' set and where its gradient is
@@ -418,14 +436,21 @@ __global__ void __launch_bounds__(S::kThreads, waves_wanted<S>()) distill_rows_k
             if (grad && v < span.full) span.store(dense(r[v]), g, v);
             if (v < to_full) {
                 to.load(r[v], below, v);
-                if (v >= kLag) take(r[v >= kLag ? v - kLag : 0]);
+                if (v >= kLag) {
+                    to.trim(r[v >= kLag ? v - kLag : 0], v - kLag);
+                    take(r[v >= kLag ? v - kLag : 0]);
+                }
             }
         }
         if (next_scale != 0.f) {
             to.load_tail(tail, below);
 #pragma unroll
             for (int v = 0; v < S::NV; ++v)
-                if (v < to_full && v >= to_full - kLag) take(r[v]);
+                if (v < to_full && v >= to_full - kLag) {
+                    to.trim(r[v], v);
+                    take(r[v]);
+                }
+            to.trim_tail(tail);
             take(tail);
         }
         before = i;

@@ -57,6 +57,16 @@ template <class T, int VE> struct Vec {
 #pragma unroll
         for (int i = 0; i < kWords; ++i) asm volatile("" : "+v"(w[i]));
     }
+    // -infinity everywhere but in elements [lo, hi)
+    __device__ __forceinline__ void keep(int lo, int hi) {
+        constexpr int kPer = 4 / static_cast<int>(sizeof(T));
+        constexpr uint32_t kNone = sizeof(T) == 4 ? 0xff800000u : 0xff80u, kMask = sizeof(T) == 4 ? 0xffffffffu : 0xffffu;
+#pragma unroll
+        for (int e = 0; e < VE; ++e) {
+            const int at = (e % kPer) * 16;
+            if (e < lo || e >= hi) w[e / kPer] = (w[e / kPer] & ~(kMask << at)) | (kNone << at);
+        }
+    }
     // elements [lo, hi) of p; the rest are `fill`, or are not written
     __device__ __forceinline__ void load_some(const T *p, int lo, int hi, float fill) {
         float x[VE];
