@@ -1,0 +1,46 @@
+// bf16 operands as the tiles' kernels read them (act_pack.hip): 16-byte
+// aligned rows of a multiple of eight values.  Operands that lie so are used where
+// they are; others (fp32 activations, weights without a shadow, odd row lengths,
+// halves that are no whole number of chunks, misaligned pointers) are copied to the
+// workspace first, which always has room for both.
+#pragma once
+
+#include "internal.h"
+
+namespace gnn {
+
+gnn_status launch_act_engine(const ActFwd &a, hipStream_t s);
+
+namespace pack {
+
+// Products so small that launches and latency are all there is, and fp32
+// ones, stay with the general engine, which reads any operand as it lies.
+inline bool small(int64_t cap_m, int64_t K, int64_t n_out, int gemm_dt) {
+    return gemm_dt != GNN_BF16 || static_cast<double>(cap_m) * static_cast<double>(K) * static_cast<double>(n_out) < double(1 << 25);
+}
+
+inline int64_t row8(int64_t n) { return (n + 7) / 8 * 8; }
+
+struct Layout {
+    size_t a = 0, w = 0, total = 0;
+    Layout(int64_t cap_m, int64_t K, int64_t n_out) {
+        Carver c(nullptr);
+        a = c.take(static_cast<size_t>(cap_m * row8(K) * 2));
+        w = c.take(static_cast<size_t>(row8(n_out) * row8(K) * 2));
+        total = round_up(c.off, 256);
+    }
+};
+
+struct Operands {
+    const uint16_t *a0, *a1;   // A = [a0 || a1] (a1 null: A = a0), lda values a row each
+    int64_t k_each, K, lda;    // K: row8 of the operator's K where A was copied
+    const uint16_t *wt;        // W^T: n_out rows, ldw values apart
+    int64_t ldw;
+};
+
+// The operands of a (a1's halves of a whole number of `chunk` values), copied on s
+// where they must be.  weights: wt is wanted.
+gnn_status prepare(const ActArgs &a, int64_t chunk, bool weights, void *ws, Operands *o, hipStream_t s);
+
+}  // namespace pack
+}  // namespace gnn

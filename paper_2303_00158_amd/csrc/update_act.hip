@@ -107,10 +107,7 @@ __global__ void __launch_bounds__(kThreads) act_engine_kernel(EngineArgs p) {
 
 }  // namespace
 
-size_t act_fwd_ws_bytes(int, int64_t, bool, int64_t, int64_t, int, bool) { return 0; }
-
-gnn_status launch_act_fwd(const ActFwd &a, void *, hipStream_t s) {
-    if (a.cap_m == 0) return GNN_OK;
+gnn_status launch_act_engine(const ActFwd &a, hipStream_t s) {
     const bool bf = a.gemm_dt == GNN_BF16, wt = bf && a.wt;
     const size_t asz = dtype_size(a.adt), osz = dtype_size(a.odt);
     EngineArgs p{};
