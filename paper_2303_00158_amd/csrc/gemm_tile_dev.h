@@ -88,7 +88,8 @@ template <int W> __device__ __forceinline__ int t_idx(int k, int c) {
 
 // N layout: `rows` output rows of `red` reduction elements (a multiple of 8)
 // from x0, or the second half of them from x1 (each then `half` wide, a multiple of
-// 64).  T layout: `red` reduction rows of which the tile's `rows` columns start at x0.
+// 64).  T layout: `red` reduction rows, from whose ends x0's column is `rows` values
+// away, a multiple of 8 (a copy of 16 bytes that reaches past the bound is all 0).
 struct Operand {
     const uint16_t *x0, *x1;
     int64_t ld, half, rows, red;
