@@ -9,7 +9,13 @@
 
 namespace gnn {
 
-gnn_status launch_act_engine(const ActFwd &a, hipStream_t s);
+size_t act_engine_ws_bytes(int64_t K, int64_t n_out, int64_t cap_m, int gemm_dt);
+gnn_status launch_act_engine(const ActFwd &a, void *ws, hipStream_t s);
+
+// The epilogue of a split reduction: out = act(sum of the partials, in order, +
+// bias) + residual for the counted rows.  Partial q's row r starts at
+// part + (q cap_m + r) ld, ld a multiple of 4.
+gnn_status launch_act_finish(const ActFwd &a, const float *part, int64_t nsplit, int64_t ld, hipStream_t s);
 
 namespace pack {
 

@@ -60,21 +60,47 @@ using Big7 = Cfg<7, 8, 1>;   // 224 x 256
 using Mid = Cfg<4, 4, 2>;    // 128 x 128
 using Small = Cfg<2, 2, 4>;  // 64 x 64
 
-// The tile size for an output of rows x cols: the one whose rounds of the CUs take
-// the least time, going by what a tile's area takes on a CU at the measured rates
-// (8,192^3: 1.15 PFLOP/s in 256 x 256 tiles, 1.00 in 128 x 128, 0.70 in 64 x 64).
+// The tile size for an output of rows x cols over a reduction of `red`, and how many
+// ways the reduction is split: the choice that takes the least time by its rounds of
+// the CUs, going by what a tile's area takes at the measured rates (8,192^3: 1.15
+// PFLOP/s in 256 x 256 tiles, 1.00 in 128 x 128, 0.70 in 64 x 64) and 3 us for its
+// first copies and its epilogue.  A split (fp32 partial tiles, added in order by
+// another kernel) costs their bytes, out and in, and a launch; each has at least
+// four chunks.
 enum Pick { kBig, kBig7, kMid, kSmall };
-inline Pick pick(int64_t rows, int64_t cols) {
-    auto cost = [&](auto cfg, double rate) {
+struct Choice {
+    Pick pick;
+    int64_t nsplit;
+};
+inline Choice choose(int64_t rows, int64_t cols, int64_t red) {
+    Choice best{kSmall, 1};
+    double least = -1;
+    auto look = [&](auto cfg, Pick pick, double rate) {
         using C = decltype(cfg);
+        const int64_t chunks = std::max<int64_t>(ceil_div(red, int64_t(kBK)), 1);
         const int64_t tiles = ceil_div(rows, int64_t(C::BM)) * ceil_div(cols, int64_t(C::BN)), round = 256 * C::PER_CU;
-        return static_cast<double>(tiles / round * C::PER_CU + ceil_div(tiles % round, int64_t(256))) * C::BM * C::BN / rate;
+        for (int64_t n = 1; n <= 16 && (n == 1 || (n * tiles <= round && n * 4 <= chunks)); n *= 2) {
+            const int64_t items = n * tiles;
+            const double per_cu = static_cast<double>(items / round * C::PER_CU + ceil_div(items % round, int64_t(256)));
+            const double us = 3 + 2.0 * C::BM * C::BN * kBK * static_cast<double>(ceil_div(chunks, n)) / (rate * 1e9 / 256);
+            const double t = per_cu * us + (n > 1 ? 4 + static_cast<double>(n) * rows * cols * 8 / 4e6 : 0);
+            if (least < 0 || t < least) {
+                least = t;
+                best = Choice{pick, n};
+            }
+        }
     };
-    const double c[4] = {cost(Big{}, 1.15), cost(Big7{}, 1.13), cost(Mid{}, 1.0), cost(Small{}, 0.7)};
-    int best = 0;
-    for (int i = 1; i < 4; ++i)
-        if (c[i] < c[best]) best = i;
-    return static_cast<Pick>(best);
+    look(Big{}, kBig, 1.15);
+    look(Big7{}, kBig7, 1.13);
+    look(Mid{}, kMid, 1.0);
+    look(Small{}, kSmall, 0.7);
+    return best;
+}
+// Reduction elements [*beg, *end) of split `split`, whole chunks.
+__device__ __forceinline__ void split_of(int64_t red, int64_t nsplit, int64_t split, int64_t *beg, int64_t *end) {
+    const int64_t per = ceil_div(ceil_div(red, nsplit), int64_t(kBK)) * kBK;
+    *beg = min(red, split * per);
+    *end = min(red, *beg + per);
 }
 
 // --- one operand's copies --------------------------------------------------
@@ -87,8 +113,8 @@ template <int W> __device__ __forceinline__ int t_idx(int k, int c) {
 }
 
 // N layout: `rows` output rows of `red` reduction elements (a multiple of 8)
-// from x0, or the second half of them from x1 (each then `half` wide, a multiple of
-// 64).  T layout: `red` reduction rows, from whose ends x0's column is `rows` values
+// from x0, or the first `half` of them (a multiple of 64) from x0 and the others
+// from x1.  T layout: `red` reduction rows, from whose ends x0's column is `rows` values
 // away, a multiple of 8 (a copy of 16 bytes that reaches past the bound is all 0).
 struct Operand {
     const uint16_t *x0, *x1;
@@ -119,9 +145,10 @@ template <int W, int COPIES, bool T> struct Copier {
                 off[i] = static_cast<int>((k * o.ld + t_unit<W>(k, u) * 8) * 2);
             }
         } else {
-            const int64_t rows = min(o.rows, int64_t(W)), bytes = rows > 0 ? ((rows - 1) * o.ld + half) * 2 : 0;
-            r0 = desc(o.x0, bytes);
-            r1 = desc(o.x1 ? o.x1 : o.x0, bytes);
+            const int64_t rows = min(o.rows, int64_t(W));
+            auto bytes = [&](int64_t cols) { return rows > 0 ? ((rows - 1) * o.ld + cols) * 2 : 0; };
+            r0 = desc(o.x0, bytes(half));
+            r1 = desc(o.x1 ? o.x1 : o.x0, bytes(o.red - half));
             k8 = ((lane & 7) ^ (lane >> 3)) * 8;
 #pragma unroll
             for (int i = 0; i < COPIES; ++i)

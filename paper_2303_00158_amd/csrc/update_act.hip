@@ -1,6 +1,7 @@
 // The update with an activation and a residual in its epilogue:
 //   Z = [A_self || A_nbr] W + b,  out = act(Z) + residual
 // on the matrix-core engine of gemm_engine.h.
+#include "act_pack.h"
 #include "act_dev.h"
 #include "gemm_engine.h"
 
@@ -80,6 +81,7 @@ struct EngineArgs {
     const void *w;
     TileMap map;
     Epilogue ep;
+    float *part;   // partial tiles of a split reduction (gridDim.z of them), rows part_ld(n_out) long
 };
 
 template <bool BF16, int TILE, class TA, bool V, bool WT, int ACT>
@@ -93,10 +95,20 @@ __global__ void __launch_bounds__(kThreads) act_engine_kernel(EngineArgs p) {
     if (tx >= p.map.mt || row0 >= M) return;
     SrcRows<BF16, TILE, TA, V, D> sp{static_cast<const TA *>(p.a_self), static_cast<const TA *>(p.a_nbr), p.k_each,
                                      p.k_each, M, p.K, row0, {}};
-    auto sq = WOf<BF16, TILE, V, WT, D>::make(p.w, p.K, p.ep.n_out, p.K, col0);
+    int64_t r_beg, r_end;
+    split_range<Cfg<BF16>::BK>(p.K, gridDim.z, blockIdx.z, &r_beg, &r_end);
+    auto sq = WOf<BF16, TILE, V, WT, D>::make(p.w, p.K, p.ep.n_out, r_end, col0);
     Acc<TILE, TILE> acc;
-    run_tile<BF16, D>(acc, sp, sq, 0, p.K, lds, [](const auto &, int, int64_t, bool) {});
+    run_tile<BF16, D>(acc, sp, sq, r_beg, r_end, lds, [](const auto &, int, int64_t, bool) {});
     const int64_t gc = col0 + TileOut<TILE, TILE>::col();
+    if (gridDim.z > 1) {
+        const int64_t ld = part_ld(p.ep.n_out);
+        emit_tile(acc, lds, [&](int, int r, int, float4 v) {
+            const int64_t gr = row0 + r;
+            if (gr < M && gc < ld) *reinterpret_cast<float4 *>(p.part + (blockIdx.z * p.cap_m + gr) * ld + gc) = v;
+        });
+        return;
+    }
     emit_tile(acc, lds, [&](int, int r, int, float4 v) {
         const int64_t gr = row0 + r;
         if (gr >= M) return;
@@ -105,11 +117,56 @@ __global__ void __launch_bounds__(kThreads) act_engine_kernel(EngineArgs p) {
     });
 }
 
+// Four columns of a row from the partials.
+template <int ACT, class TO>
+__global__ void __launch_bounds__(kThreads) act_finish_kernel(const float *part, int64_t nsplit, int64_t ld,
+                                                              const int64_t *m_dev, int64_t cap_m, Epilogue ep) {
+    const int64_t M = m_dev ? max(min(*m_dev, cap_m), int64_t(0)) : cap_m, groups = ld / 4;
+    for (int64_t t = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; t < M * groups;
+         t += static_cast<int64_t>(gridDim.x) * kThreads) {
+        const int64_t r = t / groups, c = (t - r * groups) * 4;
+        finish4<ACT, TO>(ep, r, c, sum_splits(part + r * ld + c, cap_m * ld, static_cast<int>(nsplit)));
+    }
+}
+
+Epilogue epilogue_of(const ActFwd &a) {
+    const size_t osz = dtype_size(a.odt);
+    return Epilogue{a.bias, a.residual, a.z, a.out, a.n_out, a.odt == GNN_BF16,
+                    a.n_out % 4 == 0 && aligned(a.residual, 4 * osz) && aligned(a.z, 4 * osz) && aligned(a.out, 4 * osz)};
+}
+
+// Few tiles of a long reduction are split, eight chunks a split at least (fp32,
+// 880 x 512 x 100: 28 tiles of 16 chunks).
+int engine_splits(int64_t K, int64_t n_out, int64_t cap_m, bool bf) {
+    const int tile = pick_tile(cap_m, n_out);
+    const int64_t tiles = ceil_div(std::max<int64_t>(cap_m, 1), tile) * ceil_div(n_out, tile), chunks = ceil_div(K, bk_of(bf));
+    if (tiles >= 128 || chunks < 16) return 1;
+    return static_cast<int>(std::min<int64_t>({chunks / 8, ceil_div(256, tiles), 16}));
+}
+
 }  // namespace
 
-gnn_status launch_act_engine(const ActFwd &a, hipStream_t s) {
+size_t act_engine_ws_bytes(int64_t K, int64_t n_out, int64_t cap_m, int gemm_dt) {
+    const int n = engine_splits(K, n_out, cap_m, gemm_dt == GNN_BF16);
+    return n > 1 ? round_up(static_cast<size_t>(n * cap_m * part_ld(n_out) * 4), 256) : 0;
+}
+
+gnn_status launch_act_finish(const ActFwd &a, const float *part, int64_t nsplit, int64_t ld, hipStream_t s) {
+    const unsigned grid = static_cast<unsigned>(std::min<int64_t>(ceil_div(a.cap_m * (ld / 4), int64_t(kThreads)), 8192));
+    act::with(a.act, [&](auto code) {
+        constexpr int ACT = decltype(code)::value;
+        if (a.odt == GNN_BF16)
+            act_finish_kernel<ACT, uint16_t><<<grid, kThreads, 0, s>>>(part, nsplit, ld, a.m_dev, a.cap_m, epilogue_of(a));
+        else
+            act_finish_kernel<ACT, float><<<grid, kThreads, 0, s>>>(part, nsplit, ld, a.m_dev, a.cap_m, epilogue_of(a));
+    });
+    GNN_LAUNCHED("update_fwd_act_finish");
+    return GNN_OK;
+}
+
+gnn_status launch_act_engine(const ActFwd &a, void *ws, hipStream_t s) {
     const bool bf = a.gemm_dt == GNN_BF16, wt = bf && a.wt;
-    const size_t asz = dtype_size(a.adt), osz = dtype_size(a.odt);
+    const size_t asz = dtype_size(a.adt);
     EngineArgs p{};
     p.a_self = a.a_self;
     p.a_nbr = a.a_nbr;
@@ -118,14 +175,14 @@ gnn_status launch_act_engine(const ActFwd &a, hipStream_t s) {
     p.m_dev = a.m_dev;
     p.cap_m = a.cap_m;
     p.w = wt ? static_cast<const void *>(a.wt) : a.w;
-    p.ep = Epilogue{a.bias, a.residual, a.z, a.out, a.n_out, a.odt == GNN_BF16,
-                    a.n_out % 4 == 0 && aligned(a.residual, 4 * osz) && aligned(a.z, 4 * osz) && aligned(a.out, 4 * osz)};
-    const int tile = pick_tile(a.cap_m, a.n_out);
+    p.ep = epilogue_of(a);
+    p.part = static_cast<float *>(ws);
+    const int tile = pick_tile(a.cap_m, a.n_out), nsplit = engine_splits(p.K, a.n_out, a.cap_m, bf);
     p.map = TileMap{ceil_div(a.cap_m, tile), ceil_div(a.n_out, tile)};
     GNN_CHECK(p.map.blocks() <= kMaxGrid / kThreads, GNN_ESIZE, "update_fwd_act: cap_m exceeds the grid limit");
     const bool vec = a.k_each % 4 == 0 && aligned(a.a_self, 4 * asz) && aligned(a.a_nbr, 4 * asz) &&
                      (wt ? aligned(a.wt, 8) : a.n_out % 4 == 0 && aligned(a.w, 16));
-    const unsigned grid = static_cast<unsigned>(p.map.blocks());
+    const dim3 grid(static_cast<unsigned>(p.map.blocks()), 1, static_cast<unsigned>(nsplit));
     act::with(a.act, [&](auto code) {
         constexpr int ACT = decltype(code)::value;
         auto go = [&](auto bf16, auto t, auto ta, auto v, auto shadow) {
@@ -151,7 +208,7 @@ gnn_status launch_act_engine(const ActFwd &a, hipStream_t s) {
         else by_type(bool_constant<false>{}, bool_constant<false>{});
     });
     GNN_LAUNCHED("update_fwd_act");
-    return GNN_OK;
+    return nsplit > 1 ? launch_act_finish(a, p.part, nsplit, part_ld(a.n_out), s) : GNN_OK;
 }
 
 }  // namespace gnn

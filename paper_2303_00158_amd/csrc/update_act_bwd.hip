@@ -10,8 +10,7 @@
 // shadow W^T, whose rows are the reduction, a T operand, so that the weights are
 // read as the forward keeps them.  (Without the shadow, W is rounded to bf16 rows
 // in the workspace, an N operand.)
-// fp32 products, and small ones, take the update's own kernels (gemm_bwd.hip) on an
-// fp32 dZ.
+// fp32 products take the update's own kernels (gemm_bwd.hip) on an fp32 dZ.
 #include "act_pack.h"
 #include "gemm_tile_dev.h"
 
@@ -55,75 +54,39 @@ __global__ void __launch_bounds__(kThreads) act_slope_kernel(const TG *g, const 
     }
 }
 
-// out (the counted rows of row length ld) = bf16(in)
-__global__ void __launch_bounds__(kThreads) act_narrow_kernel(const float *in, const int64_t *m_dev, int64_t rows,
-                                                              int64_t ld, uint16_t *out) {
-    const int64_t n = count(m_dev, rows) * ld;
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i < n;
-         i += static_cast<int64_t>(gridDim.x) * kThreads)
-        out[i] = f32_to_bf16(in[i]);
-}
-
-// w[k][n] = wt[n][k]
-__global__ void __launch_bounds__(kThreads) act_unshadow_kernel(const uint16_t *wt, int64_t K, int64_t n_out, float *w) {
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i < K * n_out;
-         i += static_cast<int64_t>(gridDim.x) * kThreads)
-        w[i] = bf16_to_f32(wt[(i % n_out) * K + i / n_out]);
-}
-
 struct EngineLayout {
-    size_t dz, w, dw, d_a, gemm, total;
-    EngineLayout(int64_t K, int64_t n_out, int64_t cap_m, int gdt, int dwdt, int gemm_dt, bool shadow) {
+    size_t dz, gemm, total;
+    EngineLayout(int64_t K, int64_t n_out, int64_t cap_m) {
         Carver c(nullptr);
         dz = c.take(static_cast<size_t>(cap_m * n_out * 4));
-        w = c.take(shadow ? static_cast<size_t>(K * n_out * 4) : 0);
-        dw = c.take(dwdt == GNN_BF16 ? static_cast<size_t>(K * n_out * 4) : 0);
-        d_a = c.take(gdt == GNN_BF16 ? static_cast<size_t>(cap_m * K * 4) : 0);
-        gemm = c.take(update_bwd_ws_bytes(K, n_out, cap_m, gemm_dt));
+        gemm = c.take(update_bwd_ws_bytes(K, n_out, cap_m, GNN_F32));
         total = round_up(c.off, 256);
     }
 };
 
+// fp32 products: every operand but A and Z is fp32.
 gnn_status launch_engine(const ActBwd &a, void *ws, hipStream_t s) {
-    const int64_t K = a.K();
-    const EngineLayout l(K, a.n_out, a.cap_m, a.gdt, a.dwdt, a.gemm_dt, a.wt != nullptr);
+    const EngineLayout l(a.K(), a.n_out, a.cap_m);
     char *base = static_cast<char *>(ws);
     float *dz = reinterpret_cast<float *>(base + l.dz);
-    if (a.cap_m > 0) {
+    const float *g = static_cast<const float *>(a.g);
+    if (a.cap_m > 0 && a.act != GNN_ACT_NONE) {
         const unsigned grid = grid_of(a.cap_m * a.n_out);
         act::with(a.act, [&](auto code) {
             constexpr int ACT = decltype(code)::value;
-            with_types(a.gdt, a.zdt, [&](auto tg, auto tz) {
-                using TG = decltype(tg);
-                using TZ = decltype(tz);
-                act_slope_kernel<ACT, TG, TZ><<<grid, kThreads, 0, s>>>(
-                    static_cast<const TG *>(a.g), static_cast<const TZ *>(a.z), a.m_dev, a.cap_m, a.n_out, dz);
-            });
+            if (a.zdt == GNN_BF16)
+                act_slope_kernel<ACT, float, uint16_t><<<grid, kThreads, 0, s>>>(g, static_cast<const uint16_t *>(a.z), a.m_dev,
+                                                                                 a.cap_m, a.n_out, dz);
+            else
+                act_slope_kernel<ACT, float, float><<<grid, kThreads, 0, s>>>(g, static_cast<const float *>(a.z), a.m_dev,
+                                                                              a.cap_m, a.n_out, dz);
         });
         GNN_LAUNCHED("act_slope");
+        g = dz;
     }
-    const float *w = a.w;
-    if (a.d_a && a.wt) {
-        float *wf = reinterpret_cast<float *>(base + l.w);
-        act_unshadow_kernel<<<grid_of(K * a.n_out), kThreads, 0, s>>>(a.wt, K, a.n_out, wf);
-        GNN_LAUNCHED("act_unshadow");
-        w = wf;
-    }
-    float *dw = a.dwdt == GNN_BF16 ? reinterpret_cast<float *>(base + l.dw) : static_cast<float *>(a.dw);
-    float *d_a = !a.d_a ? nullptr : a.gdt == GNN_BF16 ? reinterpret_cast<float *>(base + l.d_a) : static_cast<float *>(a.d_a);
-    GNN_TRY(launch_update_bwd(a.a_self, a.a_nbr, a.adt, a.k_each, a.m_dev, a.cap_m, w, dz, a.n_out, a.gemm_dt, dw, a.db,
-                              d_a, base + l.gemm, nullptr, nullptr, nullptr, 0.f, s));
-    if (a.dwdt == GNN_BF16) {
-        act_narrow_kernel<<<grid_of(K * a.n_out), kThreads, 0, s>>>(dw, nullptr, K, a.n_out,
-                                                                    static_cast<uint16_t *>(a.dw));
-        GNN_LAUNCHED("act_narrow");
-    }
-    if (a.d_a && a.gdt == GNN_BF16 && a.cap_m > 0) {
-        act_narrow_kernel<<<grid_of(a.cap_m * K), kThreads, 0, s>>>(d_a, a.m_dev, a.cap_m, K,
-                                                                    static_cast<uint16_t *>(a.d_a));
-        GNN_LAUNCHED("act_narrow");
-    }
-    return GNN_OK;
+    return launch_update_bwd(a.a_self, a.a_nbr, a.adt, a.k_each, a.m_dev, a.cap_m, a.w, g, a.n_out, GNN_F32,
+                             static_cast<float *>(a.dw), a.db, static_cast<float *>(a.d_a), base + l.gemm, nullptr, nullptr,
+                             nullptr, 0.f, s);
 }
 
 // ---------------------------------------------------------------------------
@@ -254,6 +217,7 @@ struct DaArgs {
     const uint16_t *w;
     int64_t ldw;
     void *out;
+    int64_t ld, split_stride, nsplit;
     bool vec;
 };
 
@@ -262,20 +226,23 @@ __global__ void __launch_bounds__(C::kThreads, C::PER_CU) act_da_kernel(DaArgs p
     __shared__ __attribute__((aligned(16))) uint16_t st0[C::kStageElems], st1[C::kStageElems];
     const int64_t M = count(p.m_dev, p.cap_m);
     const int64_t tm = ceil_div(M, int64_t(C::BM)), tn = ceil_div(p.K, int64_t(C::BN));
-    const int64_t t = wide::xcd_item(blockIdx.x, tm * tn);
-    if (t < 0) return;
-    int64_t m, n;
-    tile::tile_of(t, tm, tn, &m, &n);
-    const int64_t row0 = m * C::BM, col0 = n * C::BN;
-    const tile::Operand oa{p.dz + row0 * p.ldz, nullptr, p.ldz, p.ldz, M - row0, p.ldz};
-    const tile::Operand ob = TB ? tile::Operand{p.w + col0, nullptr, p.ldw, 0, p.ldw - col0, p.n_out}
-                                : tile::Operand{p.w + col0 * p.ldw, nullptr, p.ldw, p.ldw, p.K - col0, p.ldw};
+    const int64_t item = wide::xcd_item(blockIdx.x, tm * tn * p.nsplit);
+    if (item < 0) return;
+    const int64_t split = item / (tm * tn);
+    int64_t m, n, beg, end;
+    tile::tile_of(item - split * (tm * tn), tm, tn, &m, &n);
+    tile::split_of(p.ldz, p.nsplit, split, &beg, &end);
+    const int64_t row0 = m * C::BM, col0 = n * C::BN, red = end - beg;
+    const tile::Operand oa{p.dz + row0 * p.ldz + beg, nullptr, p.ldz, 0, M - row0, red};
+    const tile::Operand ob = TB ? tile::Operand{p.w + beg * p.ldw + col0, nullptr, p.ldw, 0, p.ldw - col0, min(end, p.n_out) - beg}
+                                : tile::Operand{p.w + col0 * p.ldw + beg, nullptr, p.ldw, 0, p.K - col0, red};
     tile::Acc<C> acc;
     acc.clear();
     const tile::Ring ring{{st0, st1}};
-    tile::Product<C, false, TB>(oa, ob).run(acc, ring, static_cast<int>(ceil_div(p.ldz, int64_t(tile::kBK))));
+    if (red > 0)
+        tile::Product<C, false, TB>(oa, ob).run(acc, ring, static_cast<int>(ceil_div(red, int64_t(tile::kBK))));
     const int wave = threadIdx.x >> 6;
-    const tile::Epilogue ep{nullptr, nullptr, nullptr, p.out, p.K, p.vec};
+    const tile::Epilogue ep{nullptr, nullptr, nullptr, static_cast<T *>(p.out) + split * p.split_stride, p.ld, p.vec};
     tile::finish<C, GNN_ACT_NONE, T>(acc, ep, row0 + (wave >> 1) * 16 * C::MI, col0 + (wave & 1) * 16 * C::NI, M);
 }
 
@@ -300,11 +267,20 @@ __global__ void __launch_bounds__(kThreads) act_w_rows_kernel(const float *w, in
 // dW = the splits' partials in their order (when there are any); db = the row
 // parts' sums, in a fixed order: a workgroup takes 32 columns, each of its 8 groups
 // every eighth part.
-template <class T>
-__global__ void __launch_bounds__(kThreads) act_reduce_kernel(const float *part, int64_t nsplit, int64_t K, int64_t n_out,
-                                                              int64_t ld, T *dw, unsigned db_blocks, const float *db_part,
-                                                              int64_t parts, float *db) {
-    if (blockIdx.x < db_blocks) {
+struct ReduceArgs {
+    const float *part;   // nsplit partials of `rows` x ld; of them the rows counted by m_dev are summed
+    int64_t nsplit, rows, cols, ld;
+    const int64_t *m_dev;
+    void *out;
+    const float *db_part;
+    int64_t parts, n_out;
+    float *db;
+    unsigned db_blocks;
+};
+template <class T> __global__ void __launch_bounds__(kThreads) act_reduce_kernel(ReduceArgs a) {
+    const float *db_part = a.db_part;
+    const int64_t n_out = a.n_out, parts = a.parts;
+    if (blockIdx.x < a.db_blocks) {
         __shared__ float sh[8][32];
         const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
         const int64_t c = static_cast<int64_t>(blockIdx.x) * 32 + x;
@@ -318,34 +294,46 @@ __global__ void __launch_bounds__(kThreads) act_reduce_kernel(const float *part,
         t = 0.f;
 #pragma unroll
         for (int k = 0; k < 8; ++k) t += sh[k][x];
-        db[c] = t;
+        a.db[c] = t;
         return;
     }
-    const int64_t groups = ld / 4;
-    for (int64_t t = static_cast<int64_t>(blockIdx.x - db_blocks) * kThreads + threadIdx.x; t < K * groups;
-         t += static_cast<int64_t>(gridDim.x - db_blocks) * kThreads) {
-        const int64_t k = t / groups, n = (t - k * groups) * 4;
-        const float *p = part + k * ld + n;
+    const int64_t groups = a.ld / 4, rows = count(a.m_dev, a.rows);
+    const bool vec = a.cols % 4 == 0 && aligned_dev(a.out, 4 * sizeof(T));
+    for (int64_t t = static_cast<int64_t>(blockIdx.x - a.db_blocks) * kThreads + threadIdx.x; t < rows * groups;
+         t += static_cast<int64_t>(gridDim.x - a.db_blocks) * kThreads) {
+        const int64_t r = t / groups, c = (t - r * groups) * 4;
+        const float *p = a.part + r * a.ld + c;
         tile::f32x4 s{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
-        for (int64_t q = 0; q < nsplit; ++q) {
-            const float4 v = *reinterpret_cast<const float4 *>(p + q * K * ld);
+        for (int64_t q = 0; q < a.nsplit; ++q) {
+            const float4 v = *reinterpret_cast<const float4 *>(p + q * a.rows * a.ld);
             s[0] += v.x;
             s[1] += v.y;
             s[2] += v.z;
             s[3] += v.w;
         }
-        tile::put4(dw + k * n_out + n, static_cast<int>(min(n_out - n, int64_t(4))), n_out % 4 == 0 && aligned_dev(dw, 4 * sizeof(T)), s);
+        tile::put4(static_cast<T *>(a.out) + r * a.cols + c, static_cast<int>(min(a.cols - c, int64_t(4))), vec, s);
     }
+}
+
+gnn_status launch_reduce(const ReduceArgs &a, int odt, bool sums, hipStream_t s) {
+    const unsigned blocks = sums ? static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>(ceil_div(a.rows * (a.ld / 4), int64_t(kThreads)), 4096))) : 0;
+    if (odt == GNN_BF16) act_reduce_kernel<uint16_t><<<a.db_blocks + blocks, kThreads, 0, s>>>(a);
+    else act_reduce_kernel<float><<<a.db_blocks + blocks, kThreads, 0, s>>>(a);
+    GNN_LAUNCHED("update_bwd_act_reduce");
+    return GNN_OK;
 }
 
 struct Plan {
     bool mid;            // dW in 128 x 128 tiles, else 256 x 256
-    int64_t nsplit, parts, ldz, ldw, ld_part;
-    size_t pack, dz, wb, db_part, part, total;
+    int64_t nsplit, parts, ldz, ldw, ld_part, ld_a;
+    tile::Choice da;
+    size_t pack, dz, wb, db_part, part, a_part, total;
     Plan(int64_t k_each, bool two, int64_t n_out, int64_t cap_m, bool shadow) {
         const int64_t K = two ? 2 * k_each : k_each, halves = two ? 2 : 1;
         ldz = pack::row8(n_out);
+        da = tile::choose(cap_m, K, ldz);
+        ld_a = (K + 3) / 4 * 4;
         // dW: large tiles where they fill half the chip or the rows are long
         // enough to split; each split at least 512 rows, one round of the CUs
         auto tiles = [&](int64_t edge) { return halves * ceil_div(k_each, edge) * ceil_div(n_out, edge); };
@@ -363,6 +351,7 @@ struct Plan {
         wb = c.take(shadow ? 0 : static_cast<size_t>(K * ldw * 2));
         db_part = c.take(static_cast<size_t>(parts * n_out * 4));
         part = c.take(nsplit > 1 ? static_cast<size_t>(nsplit * K * ld_part * 4) : 0);
+        a_part = c.take(da.nsplit > 1 ? static_cast<size_t>(da.nsplit * cap_m * ld_a * 4) : 0);
         total = round_up(c.off, 256);
     }
 };
@@ -377,7 +366,8 @@ template <class C> gnn_status launch_dw(const DwArgs &p, int odt, hipStream_t s)
 }
 
 template <class C> gnn_status launch_da(const DaArgs &p, int odt, bool shadow, hipStream_t s) {
-    const int64_t tiles = ceil_div(p.cap_m, int64_t(C::BM)) * ceil_div(p.K, int64_t(C::BN)), grid64 = round_up(tiles, wide::kXcds);
+    const int64_t tiles = ceil_div(p.cap_m, int64_t(C::BM)) * ceil_div(p.K, int64_t(C::BN));
+    const int64_t grid64 = round_up(tiles * p.nsplit, wide::kXcds);
     GNN_CHECK(grid64 <= kMaxGrid / C::kThreads, GNN_ESIZE, "update_bwd_act: cap_m exceeds the grid limit");
     const unsigned grid = static_cast<unsigned>(grid64);
     if (odt == GNN_BF16) {
@@ -437,17 +427,11 @@ gnn_status launch_tiles(const ActBwd &a, void *ws, hipStream_t s) {
     if (pl.mid) GNN_TRY(launch_dw<tile::Mid>(w, wdt, s));
     else GNN_TRY(launch_dw<tile::Big>(w, wdt, s));
     if (split || a.db) {
-        const unsigned db_blocks = a.db ? static_cast<unsigned>(ceil_div(a.n_out, int64_t(32))) : 0;
-        const unsigned dw_blocks = split ? static_cast<unsigned>(std::min<int64_t>(ceil_div(K * (pl.ld_part / 4), int64_t(kThreads)), 4096)) : 0;
-        if (a.dwdt == GNN_BF16)
-            act_reduce_kernel<uint16_t><<<db_blocks + dw_blocks, kThreads, 0, s>>>(
-                part, pl.nsplit, K, a.n_out, pl.ld_part, static_cast<uint16_t *>(a.dw), db_blocks, z.part, pl.parts, a.db);
-        else
-            act_reduce_kernel<float><<<db_blocks + dw_blocks, kThreads, 0, s>>>(
-                part, pl.nsplit, K, a.n_out, pl.ld_part, static_cast<float *>(a.dw), db_blocks, z.part, pl.parts, a.db);
-        GNN_LAUNCHED("update_bwd_act_reduce");
+        ReduceArgs r{part, pl.nsplit, K, a.n_out, pl.ld_part, nullptr, a.dw, z.part, pl.parts, a.n_out, a.db, 0};
+        r.db_blocks = a.db ? static_cast<unsigned>(ceil_div(a.n_out, int64_t(32))) : 0;
+        GNN_TRY(launch_reduce(r, a.dwdt, split, s));
     }
-    if (!a.d_a) return GNN_OK;
+    if (!a.d_a || a.cap_m == 0) return GNN_OK;
     DaArgs d{};
     d.dz = z.dz;
     d.ldz = pl.ldz;
@@ -464,28 +448,34 @@ gnn_status launch_tiles(const ActBwd &a, void *ws, hipStream_t s) {
         d.w = wb;
         d.ldw = pl.ldw;
     }
-    d.out = a.d_a;
-    d.vec = K % 4 == 0 && aligned(a.d_a, 4 * dtype_size(a.gdt));
-    switch (tile::pick(a.cap_m, K)) {
-        case tile::kBig:
-        case tile::kBig7: return launch_da<tile::Big>(d, a.gdt, a.wt != nullptr, s);
-        case tile::kMid: return launch_da<tile::Mid>(d, a.gdt, a.wt != nullptr, s);
-        default: return launch_da<tile::Small>(d, a.gdt, a.wt != nullptr, s);
+    float *a_part = reinterpret_cast<float *>(base + pl.a_part);
+    const bool a_split = pl.da.nsplit > 1;
+    d.out = a_split ? static_cast<void *>(a_part) : a.d_a;
+    d.ld = a_split ? pl.ld_a : K;
+    d.nsplit = pl.da.nsplit;
+    d.split_stride = a_split ? a.cap_m * pl.ld_a : 0;
+    d.vec = a_split || (K % 4 == 0 && aligned(a.d_a, 4 * dtype_size(a.gdt)));
+    const int adt = a_split ? static_cast<int>(GNN_F32) : a.gdt;
+    switch (pl.da.pick) {
+        case tile::kBig: GNN_TRY(launch_da<tile::Big>(d, adt, a.wt != nullptr, s)); break;
+        case tile::kBig7: GNN_TRY(launch_da<tile::Big7>(d, adt, a.wt != nullptr, s)); break;
+        case tile::kMid: GNN_TRY(launch_da<tile::Mid>(d, adt, a.wt != nullptr, s)); break;
+        default: GNN_TRY(launch_da<tile::Small>(d, adt, a.wt != nullptr, s));
     }
+    if (!a_split) return GNN_OK;
+    return launch_reduce(ReduceArgs{a_part, pl.da.nsplit, a.cap_m, K, pl.ld_a, a.m_dev, a.d_a, nullptr, 0, 0, nullptr, 0}, a.gdt,
+                         true, s);
 }
 
 }  // namespace
 
-size_t act_bwd_ws_bytes(int, int64_t k_each, bool two, int64_t n_out, int64_t cap_m, int gdt, int dwdt, int gemm_dt,
-                        bool shadow) {
-    const int64_t K = two ? 2 * k_each : k_each;
-    if (pack::small(cap_m, K, n_out, gemm_dt)) return EngineLayout(K, n_out, cap_m, gdt, dwdt, gemm_dt, shadow).total;
+size_t act_bwd_ws_bytes(int, int64_t k_each, bool two, int64_t n_out, int64_t cap_m, int, int, int gemm_dt, bool shadow) {
+    if (gemm_dt != GNN_BF16) return EngineLayout(two ? 2 * k_each : k_each, n_out, cap_m).total;
     return Plan(k_each, two, n_out, cap_m, shadow).total;
 }
 
 gnn_status launch_act_bwd(const ActBwd &a, void *ws, hipStream_t s) {
-    if (pack::small(a.cap_m, a.K(), a.n_out, a.gemm_dt)) return launch_engine(a, ws, s);
-    return launch_tiles(a, ws, s);
+    return a.gemm_dt == GNN_BF16 ? launch_tiles(a, ws, s) : launch_engine(a, ws, s);
 }
 
 }  // namespace gnn

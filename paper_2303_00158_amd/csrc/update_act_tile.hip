@@ -16,32 +16,72 @@ struct TileArgs {
     const uint16_t *wt;       // W^T, n_out rows of K values, ldw apart
     int64_t ldw;
     tile::Epilogue ep;
+    float *part;              // partial tiles of a split reduction, or null
+    int64_t nsplit, part_ld;
 };
+
+// Tile of this workgroup and its split of the reduction; false: none.
+template <class C> struct Place {
+    int64_t M, row0, col0, beg, end, split;
+    __device__ __forceinline__ bool find(const TileArgs &p) {
+        M = p.m_dev ? max(min(*p.m_dev, p.cap_m), int64_t(0)) : p.cap_m;
+        const int64_t tm = ceil_div(M, int64_t(C::BM)), tn = ceil_div(p.ep.ld, int64_t(C::BN));
+        const int64_t t = wide::xcd_item(blockIdx.x, tm * tn * p.nsplit);
+        if (t < 0) return false;
+        split = t / (tm * tn);
+        int64_t m, n;
+        tile::tile_of(t - split * (tm * tn), tm, tn, &m, &n);
+        row0 = m * C::BM;
+        col0 = n * C::BN;
+        tile::split_of(p.K, p.nsplit, split, &beg, &end);
+        return true;
+    }
+};
+
+template <class C> __device__ __forceinline__ void tile_product(const TileArgs &p, const Place<C> &at, const tile::Ring &ring, tile::Acc<C> &acc) {
+    // a split's part of [a0 || a1] starts in one half and may end in the other
+    const bool hi = p.a1 && at.beg >= p.k_each;
+    const int64_t off = at.row0 * p.lda + (hi ? at.beg - p.k_each : at.beg);
+    const tile::Operand oa{(hi ? p.a1 : p.a0) + off, p.a1 && !hi ? p.a1 + at.row0 * p.lda : nullptr, p.lda,
+                           p.a1 && !hi ? p.k_each - at.beg : at.end - at.beg, at.M - at.row0, at.end - at.beg};
+    const tile::Operand ob{p.wt + at.col0 * p.ldw + at.beg, nullptr, p.ldw, 0, p.ep.ld - at.col0, at.end - at.beg};
+    acc.clear();
+    if (at.end > at.beg)
+        tile::Product<C, false, false>(oa, ob).run(acc, ring, static_cast<int>(ceil_div(at.end - at.beg, int64_t(tile::kBK))));
+}
 
 template <class C, int ACT, class T>
 __global__ void __launch_bounds__(C::kThreads, C::PER_CU) act_tile_kernel(TileArgs p) {
     __shared__ __attribute__((aligned(16))) uint16_t st0[C::kStageElems], st1[C::kStageElems];
-    const int64_t M = p.m_dev ? min(*p.m_dev, p.cap_m) : p.cap_m;
-    const int64_t tm = ceil_div(M, int64_t(C::BM)), tn = ceil_div(p.ep.ld, int64_t(C::BN));
-    const int64_t t = wide::xcd_item(blockIdx.x, tm * tn);
-    if (t < 0) return;
-    int64_t m, n;
-    tile::tile_of(t, tm, tn, &m, &n);
-    const int64_t row0 = m * C::BM, col0 = n * C::BN;
-    const tile::Operand oa{p.a0 + row0 * p.lda, p.a1 ? p.a1 + row0 * p.lda : nullptr, p.lda, p.k_each, M - row0, p.K};
-    const tile::Operand ob{p.wt + col0 * p.ldw, nullptr, p.ldw, p.K, p.ep.ld - col0, p.K};
+    Place<C> at;
+    if (!at.find(p)) return;
     tile::Acc<C> acc;
-    acc.clear();
-    const tile::Ring ring{{st0, st1}};
-    tile::Product<C, false, false>(oa, ob).run(acc, ring, static_cast<int>(ceil_div(p.K, int64_t(tile::kBK))));
+    tile_product<C>(p, at, tile::Ring{{st0, st1}}, acc);
     const int wave = threadIdx.x >> 6;
-    tile::finish<C, ACT, T>(acc, p.ep, row0 + (wave >> 1) * 16 * C::MI, col0 + (wave & 1) * 16 * C::NI, M);
+    tile::finish<C, ACT, T>(acc, p.ep, at.row0 + (wave >> 1) * 16 * C::MI, at.col0 + (wave & 1) * 16 * C::NI, at.M);
+}
+
+// The same for a split's partial tile.
+template <class C> __global__ void __launch_bounds__(C::kThreads, C::PER_CU) act_tile_part_kernel(TileArgs p) {
+    __shared__ __attribute__((aligned(16))) uint16_t st0[C::kStageElems], st1[C::kStageElems];
+    Place<C> at;
+    if (!at.find(p)) return;
+    tile::Acc<C> acc;
+    tile_product<C>(p, at, tile::Ring{{st0, st1}}, acc);
+    const int wave = threadIdx.x >> 6;
+    const tile::Epilogue ep{nullptr, nullptr, nullptr, p.part + at.split * p.cap_m * p.part_ld, p.part_ld, true};
+    tile::finish<C, GNN_ACT_NONE, float>(acc, ep, at.row0 + (wave >> 1) * 16 * C::MI, at.col0 + (wave & 1) * 16 * C::NI, at.M);
 }
 
 template <class C> gnn_status launch_tiles(const ActFwd &a, const TileArgs &p, hipStream_t s) {
     const int64_t tiles = ceil_div(p.cap_m, int64_t(C::BM)) * ceil_div(p.ep.ld, int64_t(C::BN));
-    const int64_t grid = round_up(tiles, wide::kXcds);
+    const int64_t grid = round_up(tiles * p.nsplit, wide::kXcds);
     GNN_CHECK(grid <= kMaxGrid / C::kThreads, GNN_ESIZE, "update_fwd_act: cap_m exceeds the grid limit");
+    if (p.nsplit > 1) {
+        act_tile_part_kernel<C><<<static_cast<unsigned>(grid), C::kThreads, 0, s>>>(p);
+        GNN_LAUNCHED("update_fwd_act_part");
+        return launch_act_finish(a, p.part, p.nsplit, p.part_ld, s);
+    }
     act::with(a.act, [&](auto code) {
         constexpr int ACT = decltype(code)::value;
         if (a.odt == GNN_BF16) act_tile_kernel<C, ACT, uint16_t><<<static_cast<unsigned>(grid), C::kThreads, 0, s>>>(p);
@@ -51,20 +91,35 @@ template <class C> gnn_status launch_tiles(const ActFwd &a, const TileArgs &p, h
     return GNN_OK;
 }
 
+struct Plan {
+    tile::Choice choice;
+    int64_t part_ld;
+    size_t pack, part, total;
+    Plan(int64_t cap_m, int64_t K, int64_t n_out) : choice(tile::choose(cap_m, n_out, K)), part_ld((n_out + 3) / 4 * 4) {
+        Carver c(nullptr);
+        pack = c.take(pack::Layout(cap_m, K, n_out).total);
+        part = c.take(choice.nsplit > 1 ? static_cast<size_t>(choice.nsplit * cap_m * part_ld * 4) : 0);
+        total = round_up(c.off, 256);
+    }
+};
+
 }  // namespace
 
 size_t act_fwd_ws_bytes(int, int64_t k_each, bool two, int64_t n_out, int64_t cap_m, int gemm_dt, bool shadow) {
-    if (act_few(cap_m, gemm_dt, shadow) || pack::small(cap_m, two ? 2 * k_each : k_each, n_out, gemm_dt)) return 0;
-    return pack::Layout(cap_m, two ? 2 * k_each : k_each, n_out).total;
+    const int64_t K = two ? 2 * k_each : k_each;
+    if (act_few(cap_m, gemm_dt, shadow)) return 0;
+    if (pack::small(cap_m, K, n_out, gemm_dt)) return act_engine_ws_bytes(K, n_out, cap_m, gemm_dt);
+    return Plan(cap_m, K, n_out).total;
 }
 
 gnn_status launch_act_fwd(const ActFwd &a, void *ws, hipStream_t s) {
     if (a.cap_m == 0) return GNN_OK;
     const int64_t K = a.K();
     if (act_few(a.cap_m, a.gemm_dt, a.wt != nullptr)) return launch_act_few(a, s);
-    if (pack::small(a.cap_m, K, a.n_out, a.gemm_dt)) return launch_act_engine(a, s);
+    if (pack::small(a.cap_m, K, a.n_out, a.gemm_dt)) return launch_act_engine(a, ws, s);
+    const Plan pl(a.cap_m, K, a.n_out);
     pack::Operands o;
-    GNN_TRY(pack::prepare(a, tile::kBK, true, ws, &o, s));
+    GNN_TRY(pack::prepare(a, tile::kBK, true, static_cast<char *>(ws) + pl.pack, &o, s));
     TileArgs p{};
     p.a0 = o.a0;
     p.a1 = o.a1;
@@ -78,7 +133,10 @@ gnn_status launch_act_fwd(const ActFwd &a, void *ws, hipStream_t s) {
     const size_t osz = dtype_size(a.odt);
     p.ep = tile::Epilogue{a.bias, a.residual, a.z, a.out, a.n_out,
                           a.n_out % 4 == 0 && aligned(a.residual, 4 * osz) && aligned(a.z, 4 * osz) && aligned(a.out, 4 * osz)};
-    switch (tile::pick(a.cap_m, a.n_out)) {
+    p.part = reinterpret_cast<float *>(static_cast<char *>(ws) + pl.part);
+    p.nsplit = pl.choice.nsplit;
+    p.part_ld = pl.part_ld;
+    switch (pl.choice.pick) {
         case tile::kBig: return launch_tiles<tile::Big>(a, p, s);
         case tile::kBig7: return launch_tiles<tile::Big7>(a, p, s);
         case tile::kMid: return launch_tiles<tile::Mid>(a, p, s);

@@ -199,6 +199,33 @@ def test_forms(m, k, n, two, gemm, adt, odt, dwdt, form):
     check_backward(o, a64, w64, None, g, "none", gemm, gdt, dwdt)
 
 
+# few rows and columns over long reductions, which are split; splits that begin in
+# one half of A and end in the other
+@pytest.mark.gpu
+@pytest.mark.parametrize("live", [False, True])
+@pytest.mark.parametrize("two", [False, True])
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("m, k, n", [(130, 1088, 256), (100, 1024, 72), (129, 1100, 130), (65, 64, 4160), (100, 1031, 47), (300, 72, 2049),
+                                     (70, 2176, 1001)])
+def test_split_reductions(m, k, n, dt, two, live):
+    gen = torch.Generator().manual_seed(m + k + n)
+    gemm = gnn.GNN_BF16 if dt == BF16 else gnn.GNN_F32
+    a, b = rand(gen, m, k, dtype=dt), rand(gen, m, k, dtype=dt) if two else None
+    K = 2 * k if two else k
+    w, bias, res = rand(gen, K, n, scale=1 / math.sqrt(K)), rand(gen, n), rand(gen, m, n, dtype=dt)
+    z, g = rand(gen, m, n, dtype=dt), rand(gen, m, n, dtype=dt)
+    wt = w.t().contiguous().bfloat16() if dt == BF16 else None
+    rows = m - 30 if live else m
+    kw = {"m_dev": torch.tensor([rows], device=DEV)} if live else {}
+    a64, w64 = operands(a, b, w, wt, gemm)
+    o = forward(a, b, w, wt, bias, "gelu", gemm, dt, res, **kw)
+    check_forward(o, a64, w64, bias, res, "gelu", dt, rows)
+    assert (o["out"][rows:] == 7).all() and (o["z"][rows:] == 7).all()
+    o = backward(a, b, w, wt, z, g, "gelu", gemm, dt, **kw)
+    check_backward(o, a64, w64, z, g, "gelu", gemm, dt, dt, rows)
+    assert (o["d_a"][rows:] == 7).all()
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("dt", [F32, BF16])
 @pytest.mark.parametrize("off", [1, 2, 4, 5])
