@@ -15,7 +15,7 @@
 // cycles) under 2,048 cycles of v_mfma_f32_16x16x32_bf16; eight wavefronts of
 // 128 x 64 would read 192 KB.  Chunks are 64 deep for the copies' sake: a row's
 // part of a chunk is a whole 128-byte line (with chunks of 32, four stages of
-// them, every line came from the L2 twice: 8,192^3 took 1,000 us).
+// them, every line came from the L2 twice: 8,192^3 took 1,000 us; now 818).
 //
 // Operand layouts, in memory and in LDS:
 //  * N: rows of P (columns of Q) run along the reduction in memory.  LDS holds
@@ -32,6 +32,7 @@
 
 #include "act_dev.h"
 #include "gemm_wide_dev.h"
+#include "row_dev.h"
 
 namespace gnn {
 namespace tile {
@@ -61,12 +62,16 @@ using Mid = Cfg<4, 4, 2>;    // 128 x 128
 using Small = Cfg<2, 2, 4>;  // 64 x 64
 
 // The tile size for an output of rows x cols over a reduction of `red`, and how many
-// ways the reduction is split: the choice that takes the least time by its rounds of
-// the CUs, going by what a tile's area takes at the measured rates (8,192^3: 1.15
-// PFLOP/s in 256 x 256 tiles, 1.00 in 128 x 128, 0.70 in 64 x 64) and 3 us for its
-// first copies and its epilogue.  A split (fp32 partial tiles, added in order by
-// another kernel) costs their bytes, out and in, and a launch; each has at least
-// four chunks.
+// ways the reduction is split: the choice that takes the least time by the rounds
+// of tiles that the CUs work through.  Measured: a chunk of a tile takes `busy` us of
+// a CU that has all it holds (8,192^3: 1.34 PFLOP/s in 256 x 256 tiles, 1.12 in 128 x
+// 128, 0.72 in 64 x 64), but no less than `lone` (250 x 16,384 x 256: 289, 158 and 121
+// us); a tile takes `ends` us beside its chunks, for its first copies and its
+// epilogue, which in large tiles nothing overlaps (14,591 x 512 x 1,024 with a residual:
+// 39 us in 256 x 256 tiles, 35 in 128 x 128).  A split (fp32 partial tiles,
+// added in order by another kernel) costs their bytes, out and in, and a launch;
+// each has at least four chunks.  4,096 x 1,024 x 2,048: 43 us in 256 x 256 tiles, 24 in
+// 128 x 128, 35 in 64 x 64; 8,192 x 4,096 x 4,096: 221, 266 and 410.
 enum Pick { kBig, kBig7, kMid, kSmall };
 struct Choice {
     Pick pick;
@@ -75,25 +80,26 @@ struct Choice {
 inline Choice choose(int64_t rows, int64_t cols, int64_t red) {
     Choice best{kSmall, 1};
     double least = -1;
-    auto look = [&](auto cfg, Pick pick, double rate) {
+    auto look = [&](auto cfg, Pick pick, double busy, double lone, double ends) {
         using C = decltype(cfg);
         const int64_t chunks = std::max<int64_t>(ceil_div(red, int64_t(kBK)), 1);
         const int64_t tiles = ceil_div(rows, int64_t(C::BM)) * ceil_div(cols, int64_t(C::BN)), round = 256 * C::PER_CU;
         for (int64_t n = 1; n <= 16 && (n == 1 || (n * tiles <= round && n * 4 <= chunks)); n *= 2) {
-            const int64_t items = n * tiles;
-            const double per_cu = static_cast<double>(items / round * C::PER_CU + ceil_div(items % round, int64_t(256)));
-            const double us = 3 + 2.0 * C::BM * C::BN * kBK * static_cast<double>(ceil_div(chunks, n)) / (rate * 1e9 / 256);
-            const double t = per_cu * us + (n > 1 ? 4 + static_cast<double>(n) * rows * cols * 8 / 4e6 : 0);
+            const double each = static_cast<double>(ceil_div(chunks, n));
+            const int64_t last = ceil_div(n * tiles % round, int64_t(256));  // tiles a CU holds in the last round
+            double t = static_cast<double>(n * tiles / round * C::PER_CU) * (each * busy + ends);
+            if (last) t += each * std::max(lone, busy * last) + ends * last;
+            if (n > 1) t += 4 + static_cast<double>(n) * rows * cols * 8 / 4e6;
             if (least < 0 || t < least) {
                 least = t;
                 best = Choice{pick, n};
             }
         }
     };
-    look(Big{}, kBig, 1.15);
-    look(Big7{}, kBig7, 1.13);
-    look(Mid{}, kMid, 1.0);
-    look(Small{}, kSmall, 0.7);
+    look(Big{}, kBig, 1.6, 1.13, 20);
+    look(Big7{}, kBig7, 1.42, 1.02, 18);
+    look(Mid{}, kMid, 0.48, 0.7, 4);
+    look(Small{}, kSmall, 0.19, 0.5, 1);
     return best;
 }
 // Reduction elements [*beg, *end) of split `split`, whole chunks.
@@ -124,7 +130,8 @@ struct Operand {
 template <int W, int COPIES, bool T> struct Copier {
     __amdgpu_buffer_rsrc_t r0, r1;
     const uint16_t *x0;
-    int64_t ld, half, red, left;  // T: bytes from x0 to the operand's end
+    int64_t ld, left;  // T: bytes from x0 to the operand's end
+    int half, red;     // N
     int off[COPIES], k8;
     __device__ static __amdgpu_buffer_rsrc_t desc(const uint16_t *p, int64_t bytes) {
         return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(p), 0,
@@ -134,8 +141,6 @@ template <int W, int COPIES, bool T> struct Copier {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
         x0 = o.x0;
         ld = o.ld;
-        half = o.x1 ? o.half : o.red;
-        red = o.red;
         if constexpr (T) {
             left = o.red > 0 ? ((o.red - 1) * o.ld + o.rows) * 2 : 0;
             constexpr int kRows = 512 / W;  // reduction rows of one copy
@@ -145,6 +150,8 @@ template <int W, int COPIES, bool T> struct Copier {
                 off[i] = static_cast<int>((k * o.ld + t_unit<W>(k, u) * 8) * 2);
             }
         } else {
+            red = static_cast<int>(o.red);
+            half = o.x1 ? static_cast<int>(o.half) : red;
             const int64_t rows = min(o.rows, int64_t(W));
             auto bytes = [&](int64_t cols) { return rows > 0 ? ((rows - 1) * o.ld + cols) * 2 : 0; };
             r0 = desc(o.x0, bytes(half));
@@ -158,7 +165,7 @@ template <int W, int COPIES, bool T> struct Copier {
     // copy i of chunk c into `dst` (this operand's part of a stage)
     __device__ __forceinline__ void copy(int c, uint16_t *dst, int i) const {
 #if defined(__HIP_DEVICE_COMPILE__)  // the LDS-bit buffer load exists for the device pass only
-        const int wave = threadIdx.x >> 6;
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         if constexpr (T) {
             const int64_t at = static_cast<int64_t>(c) * kBK * ld;
             const __amdgpu_buffer_rsrc_t r = desc(x0 + at, left - at * 2);
@@ -167,7 +174,7 @@ template <int W, int COPIES, bool T> struct Copier {
             const int k0 = c * kBK;
             const bool hi = k0 >= half;
             const __amdgpu_buffer_rsrc_t r = hi ? r1 : r0;
-            const int base = static_cast<int>(hi ? k0 - half : k0) * 2;
+            const int base = (hi ? k0 - half : k0) * 2;
             const bool in = k0 + k8 < red;  // past the last column lies the next row
             __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void *)(dst + (wave + 4 * i) * 512), 16,
                                                      in ? off[i] : kOob, base, 0, 0);
@@ -209,11 +216,14 @@ template <class C> struct Acc {
 // acc += the product of two fragments, in place in the accumulation registers.
 // Written out, because the compiler's own choice of form for 256 accumulators
 // moved them between registers in every pass (532 moves beside 256 of these).
-// The wait states that it would see to: two before the instruction cover sources
-// written by a move (a fragment's usual source, an LDS read, has its own wait),
-// and settle() covers the first use of the sums.
+// The wait states that it would otherwise see to: settle() covers the first use of the
+// sums; and the two that the instruction needs behind a move into one of its
+// operands are free of charge as long as there is none, which is the case where
+// fragments come from LDS reads (they have a wait of their own) and the sums stay in
+// place: tests/test_tile_code.py holds the built code to it.  (Two wait states with
+// every instruction cost 4% of the loop.)
 __device__ __forceinline__ void mma(f32x4 &acc, const bf16x8 &x, const bf16x8 &y) {
-    asm volatile("s_nop 1\n\tv_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(x), "v"(y));
+    asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(x), "v"(y));
 }
 __device__ __forceinline__ void settle() { asm volatile("s_nop 15\n\ts_nop 15" ::: "memory"); }
 
@@ -310,98 +320,89 @@ __device__ __forceinline__ void tile_of(int64_t t, int64_t tm, int64_t tn, int64
 }
 
 // --- the epilogue ---------------------------------------------------------------
-// out = act(acc + bias) + residual for rows below M, and acc + bias to z.
-// Four columns at a time where rows and pointers allow it (vec).
+// out = act(acc + bias) + residual for rows below M, and acc + bias to z; rows of
+// `ld` elements, which the output has columns.
 struct Epilogue {
     const float *bias;
     const void *residual;
     void *z, *out;
-    int64_t ld;      // row length of residual, z and out: the output's columns
-    bool vec;
+    int64_t ld;
 };
 
-// Four elements as they lie in memory.
-template <class T> struct Raw4 {
-    uint32_t w[sizeof(T)];
-    __device__ __forceinline__ void load(const T *p) {
-        if constexpr (sizeof(T) == 2) {
-            const uint2 v = *reinterpret_cast<const uint2 *>(p);
-            w[0] = v.x;
-            w[1] = v.y;
-        } else {
-            const uint4 v = *reinterpret_cast<const uint4 *>(p);
-            w[0] = v.x;
-            w[1] = v.y;
-            w[2] = v.z;
-            w[3] = v.w;
+// Eight elements of a row, `room` of them inside it.
+template <class T> __device__ __forceinline__ void put8(T *p, int64_t room, const float (&x)[8]) {
+    if (room >= 8) {
+        row::Vec<T, 8> v;
+#pragma unroll
+        for (int e = 0; e < (sizeof(T) == 2 ? 4 : 8); ++e) {
+            if constexpr (sizeof(T) == 2) v.w[e] = wide::pack_bf16(x[2 * e], x[2 * e + 1]);
+            else v.w[e] = __float_as_uint(x[e]);
         }
-    }
-    __device__ __forceinline__ float get(int e) const {
-        if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
-        else return __uint_as_float((e & 1) ? (w[e / 2] & 0xffff0000u) : (w[e / 2] << 16));
-    }
-};
-template <class T> __device__ __forceinline__ void put4(T *p, int room, bool vec, const f32x4 &x) {
-    if (vec) {
-        store4(p, 0, make_float4(x[0], x[1], x[2], x[3]));
+        v.store(p);
     } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
+        for (int e = 0; e < 8; ++e)
             if (e < room) Elem<T>::store(p, e, x[e]);
     }
 }
 
 // The epilogue of a wavefront's part of the tile, whose origin in the output is
-// (row0, col0).  The residual's four-column groups of a row of tiles are loaded
-// before those of the row above are finished.
+// (row0, col0).  Of two neighbouring MFMA tiles' columns a lane holds four each;
+// exchanging one half with the lane 16 away gives every lane eight consecutive ones
+// of one of the two, so that an instruction moves 16 bytes a lane and 64 a row
+// of bf16 (with four columns a lane, 8 and 32).  The residual's part of a row of
+// tiles is loaded before the row above is finished.
 template <class C, int ACT, class T>
 __device__ __forceinline__ void finish(const Acc<C> &acc, const Epilogue &p, int64_t row0, int64_t col0, int64_t M) {
-    const int lane = threadIdx.x & 63;
-    const int64_t r0 = row0 + (lane & 15), c0 = col0 + (lane >> 4) * 4;
+    const int lane = threadIdx.x & 63, g = lane >> 4;
+    constexpr int kPairs = C::NI / 2;
+    const int64_t r0 = row0 + (lane & 15), c0 = col0 + (g & 1) * 16 + (g >> 1) * 8;
     const T *res = static_cast<const T *>(p.residual);
     T *z = static_cast<T *>(p.z), *out = static_cast<T *>(p.out);
-    const bool ahead = res && p.vec;
-    f32x4 bias[C::NI];
+    float bias[kPairs][8];
 #pragma unroll
-    for (int j = 0; j < C::NI; ++j)
+    for (int j = 0; j < kPairs; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) bias[j][e] = p.bias && c0 + 16 * j + e < p.ld ? p.bias[c0 + 16 * j + e] : 0.f;
-    Raw4<T> next[C::NI], now[C::NI];
+        for (int e = 0; e < 8; ++e) bias[j][e] = p.bias && c0 + 32 * j + e < p.ld ? p.bias[c0 + 32 * j + e] : 0.f;
+    row::Vec<T, 8> next[kPairs], now[kPairs];
     auto fetch = [&](int i) {
         const int64_t r = r0 + 16 * i;
 #pragma unroll
-        for (int j = 0; j < C::NI; ++j)
-            if (ahead && r < M && c0 + 16 * j < p.ld) next[j].load(res + r * p.ld + c0 + 16 * j);
+        for (int j = 0; j < kPairs; ++j)
+            if (res && r < M && c0 + 32 * j + 8 <= p.ld) next[j].load(res + r * p.ld + c0 + 32 * j);
     };
     fetch(0);
 #pragma unroll
     for (int i = 0; i < C::MI; ++i) {
         const int64_t r = r0 + 16 * i;
 #pragma unroll
-        for (int j = 0; j < C::NI; ++j) now[j] = next[j];
+        for (int j = 0; j < kPairs; ++j) now[j] = next[j];
         if (i + 1 < C::MI) fetch(i + 1);
-        if (r < M) {
 #pragma unroll
-            for (int j = 0; j < C::NI; ++j) {
-                const int64_t c = c0 + 16 * j, at = r * p.ld + c;
-                const int room = static_cast<int>(min(p.ld - c, int64_t(4)));
-                if (room <= 0) continue;
-                f32x4 x = acc.v[i][j];
+        for (int j = 0; j < kPairs; ++j) {
+            float x[8];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] += bias[j][e];
-                if (z) put4(z + at, room, p.vec, x);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = act::apply<ACT>(x[e]);
-                if (ahead) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) x[e] += now[j].get(e);
-                } else if (res) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (e < room) x[e] += Elem<T>::load(res, at + e);
-                }
-                put4(out + at, room, p.vec, x);
+            for (int q = 0; q < 4; ++q) {
+                const auto two = __builtin_amdgcn_permlane16_swap(__float_as_uint(acc.v[i][2 * j][q]),
+                                                                  __float_as_uint(acc.v[i][2 * j + 1][q]), false, false);
+                x[q] = __uint_as_float(two[0]);
+                x[q + 4] = __uint_as_float(two[1]);
             }
+            const int64_t c = c0 + 32 * j, at = r * p.ld + c, room = p.ld - c;
+            if (r >= M || room <= 0) continue;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] += bias[j][e];
+            if (z) put8(z + at, room, x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = act::apply<ACT>(x[e]);
+            if (res) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    if (room >= 8) x[e] += now[j].get(e);
+                    else if (e < room) x[e] += Elem<T>::load(res, at + e);
+                }
+            }
+            put8(out + at, room, x);
         }
     }
 }

@@ -102,14 +102,14 @@ struct DzArgs {
     int64_t ld;
     float *part;         // parts x n_out, or null (db is not wanted)
     int64_t parts;
-    bool vec;            // g's and z's rows and pointers allow eight elements at a time
 };
 
-template <class T> __device__ __forceinline__ void get8(const T *p, int64_t room, bool vec, float (&v)[8]) {
-    if (vec) {
-        const float4 a = load4(p, 0), b = load4(p, 4);
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-        v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+template <class T> __device__ __forceinline__ void get8(const T *p, int64_t room, float (&v)[8]) {
+    if (room >= 8) {
+        row::Vec<T, 8> x;
+        x.load(p);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = x.get(e);
     } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = e < room ? Elem<T>::load(p, e) : 0.f;
@@ -129,14 +129,13 @@ __global__ void __launch_bounds__(kThreads) act_dz_kernel(DzArgs p) {
     if (c < p.ld) {
         const TG *g = static_cast<const TG *>(p.g) + c;
         const TZ *z = static_cast<const TZ *>(p.z) + c;
-        const bool vec = p.vec && room >= 8;
 #pragma unroll 4
         for (int64_t i = beg + y; i < end; i += 8) {
             float v[8];
-            get8(g + i * p.n_out, room, vec, v);
+            get8(g + i * p.n_out, room, v);
             if constexpr (ACT != GNN_ACT_NONE) {
                 float zz[8];
-                get8(z + i * p.n_out, room, vec, zz);
+                get8(z + i * p.n_out, room, zz);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] *= act::slope<ACT>(zz[e]);
             }
@@ -177,7 +176,6 @@ struct DwArgs {
     int64_t cap_m, n_out;
     void *out;
     int64_t ld, split_stride, nsplit;
-    bool vec;
 };
 
 template <class C, class T> __global__ void __launch_bounds__(C::kThreads, C::PER_CU) act_dw_kernel(DwArgs p) {
@@ -203,7 +201,7 @@ template <class C, class T> __global__ void __launch_bounds__(C::kThreads, C::PE
         tile::Product<C, true, true>(oa, ob).run(acc, ring, static_cast<int>(ceil_div(rows, int64_t(tile::kBK))));
     const int wave = threadIdx.x >> 6;
     T *out = static_cast<T *>(p.out) + split * p.split_stride + (hi ? p.k_each * p.ld : 0);
-    const tile::Epilogue ep{nullptr, nullptr, nullptr, out, p.ld, p.vec};
+    const tile::Epilogue ep{nullptr, nullptr, nullptr, out, p.ld};
     tile::finish<C, GNN_ACT_NONE, T>(acc, ep, k0 + (wave >> 1) * 16 * C::MI, col0 + (wave & 1) * 16 * C::NI, p.k_each);
 }
 
@@ -218,7 +216,6 @@ struct DaArgs {
     int64_t ldw;
     void *out;
     int64_t ld, split_stride, nsplit;
-    bool vec;
 };
 
 template <class C, class T, bool TB>
@@ -242,7 +239,7 @@ __global__ void __launch_bounds__(C::kThreads, C::PER_CU) act_da_kernel(DaArgs p
     if (red > 0)
         tile::Product<C, false, TB>(oa, ob).run(acc, ring, static_cast<int>(ceil_div(red, int64_t(tile::kBK))));
     const int wave = threadIdx.x >> 6;
-    const tile::Epilogue ep{nullptr, nullptr, nullptr, static_cast<T *>(p.out) + split * p.split_stride, p.ld, p.vec};
+    const tile::Epilogue ep{nullptr, nullptr, nullptr, static_cast<T *>(p.out) + split * p.split_stride, p.ld};
     tile::finish<C, GNN_ACT_NONE, T>(acc, ep, row0 + (wave >> 1) * 16 * C::MI, col0 + (wave & 1) * 16 * C::NI, M);
 }
 
@@ -254,7 +251,7 @@ __global__ void __launch_bounds__(kThreads) act_w_rows_kernel(const float *w, in
          t += static_cast<int64_t>(gridDim.x) * kThreads) {
         const int64_t k = t / groups, n = (t - k * groups) * 8;
         float v[8];
-        get8(w + k * n_out + n, n_out - n, false, v);
+        get8(w + k * n_out + n, n_out - n, v);
         uint4 o;
         o.x = wide::pack_bf16(v[0], v[1]);
         o.y = wide::pack_bf16(v[2], v[3]);
@@ -298,12 +295,11 @@ template <class T> __global__ void __launch_bounds__(kThreads) act_reduce_kernel
         return;
     }
     const int64_t groups = a.ld / 4, rows = count(a.m_dev, a.rows);
-    const bool vec = a.cols % 4 == 0 && aligned_dev(a.out, 4 * sizeof(T));
     for (int64_t t = static_cast<int64_t>(blockIdx.x - a.db_blocks) * kThreads + threadIdx.x; t < rows * groups;
          t += static_cast<int64_t>(gridDim.x - a.db_blocks) * kThreads) {
         const int64_t r = t / groups, c = (t - r * groups) * 4;
         const float *p = a.part + r * a.ld + c;
-        tile::f32x4 s{0.f, 0.f, 0.f, 0.f};
+        float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
         for (int64_t q = 0; q < a.nsplit; ++q) {
             const float4 v = *reinterpret_cast<const float4 *>(p + q * a.rows * a.ld);
@@ -312,7 +308,16 @@ template <class T> __global__ void __launch_bounds__(kThreads) act_reduce_kernel
             s[2] += v.z;
             s[3] += v.w;
         }
-        tile::put4(static_cast<T *>(a.out) + r * a.cols + c, static_cast<int>(min(a.cols - c, int64_t(4))), vec, s);
+        T *out = static_cast<T *>(a.out) + r * a.cols + c;
+        if (a.cols - c >= 4) {
+            row::Vec<T, 4> v;
+            v.set(s);
+            v.store(out);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (e < a.cols - c) Elem<T>::store(out, e, s[e]);
+        }
     }
 }
 
@@ -397,7 +402,6 @@ gnn_status launch_tiles(const ActBwd &a, void *ws, hipStream_t s) {
     z.ld = pl.ldz;
     z.part = a.db ? reinterpret_cast<float *>(base + pl.db_part) : nullptr;
     z.parts = pl.parts;
-    z.vec = a.n_out % 4 == 0 && aligned(a.g, 4 * dtype_size(a.gdt)) && aligned(a.z, 4 * dtype_size(a.zdt));
     const unsigned dz_grid = static_cast<unsigned>(ceil_div(pl.ldz, int64_t(kStripe)) * pl.parts);
     act::with(a.act, [&](auto code) {
         with_types(a.gdt, a.zdt, [&](auto tg, auto tz) {
@@ -422,7 +426,6 @@ gnn_status launch_tiles(const ActBwd &a, void *ws, hipStream_t s) {
     w.out = split ? part : a.dw;
     w.ld = split ? pl.ld_part : a.n_out;
     w.split_stride = split ? K * pl.ld_part : 0;
-    w.vec = split || (a.n_out % 4 == 0 && aligned(a.dw, 4 * dtype_size(a.dwdt)));
     const int wdt = split ? static_cast<int>(GNN_F32) : a.dwdt;
     if (pl.mid) GNN_TRY(launch_dw<tile::Mid>(w, wdt, s));
     else GNN_TRY(launch_dw<tile::Big>(w, wdt, s));
@@ -454,7 +457,6 @@ gnn_status launch_tiles(const ActBwd &a, void *ws, hipStream_t s) {
     d.ld = a_split ? pl.ld_a : K;
     d.nsplit = pl.da.nsplit;
     d.split_stride = a_split ? a.cap_m * pl.ld_a : 0;
-    d.vec = a_split || (K % 4 == 0 && aligned(a.d_a, 4 * dtype_size(a.gdt)));
     const int adt = a_split ? static_cast<int>(GNN_F32) : a.gdt;
     switch (pl.da.pick) {
         case tile::kBig: GNN_TRY(launch_da<tile::Big>(d, adt, a.wt != nullptr, s)); break;

@@ -69,7 +69,7 @@ template <class C> __global__ void __launch_bounds__(C::kThreads, C::PER_CU) act
     tile::Acc<C> acc;
     tile_product<C>(p, at, tile::Ring{{st0, st1}}, acc);
     const int wave = threadIdx.x >> 6;
-    const tile::Epilogue ep{nullptr, nullptr, nullptr, p.part + at.split * p.cap_m * p.part_ld, p.part_ld, true};
+    const tile::Epilogue ep{nullptr, nullptr, nullptr, p.part + at.split * p.cap_m * p.part_ld, p.part_ld};
     tile::finish<C, GNN_ACT_NONE, float>(acc, ep, at.row0 + (wave >> 1) * 16 * C::MI, at.col0 + (wave & 1) * 16 * C::NI, at.M);
 }
 
@@ -130,9 +130,7 @@ gnn_status launch_act_fwd(const ActFwd &a, void *ws, hipStream_t s) {
     p.cap_m = a.cap_m;
     p.wt = o.wt;
     p.ldw = o.ldw;
-    const size_t osz = dtype_size(a.odt);
-    p.ep = tile::Epilogue{a.bias, a.residual, a.z, a.out, a.n_out,
-                          a.n_out % 4 == 0 && aligned(a.residual, 4 * osz) && aligned(a.z, 4 * osz) && aligned(a.out, 4 * osz)};
+    p.ep = tile::Epilogue{a.bias, a.residual, a.z, a.out, a.n_out};
     p.part = reinterpret_cast<float *>(static_cast<char *>(ws) + pl.part);
     p.nsplit = pl.choice.nsplit;
     p.part_ld = pl.part_ld;
