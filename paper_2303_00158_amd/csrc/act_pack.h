@@ -19,10 +19,15 @@ gnn_status launch_act_finish(const ActFwd &a, const float *part, int64_t nsplit,
 
 namespace pack {
 
-// Products so small that launches and latency are all there is, and fp32
-// ones, stay with the general engine, which reads any operand as it lies.
-inline bool small(int64_t cap_m, int64_t K, int64_t n_out, int gemm_dt) {
-    return gemm_dt != GNN_BF16 || static_cast<double>(cap_m) * static_cast<double>(K) * static_cast<double>(n_out) < double(1 << 25);
+// fp32 products, and small ones, stay with the general engine, which reads any
+// operand as it lies.  Small is below 2^25 where the tiles could do so as well (all of
+// these take 12.5 to 13.5 us either way; 512 x 1,024 x 512 13 on the tiles, 16 on
+// the engine), and below 2^28 where they would copy operands first, which is 6 us of
+// launches (1,000 x 100 x 1,000: 19 us and 13; 20,000 x 100 x 47: 20 and 13; 2,000 x 602 x
+// 256: 19.5 and 22).
+inline bool small(int64_t cap_m, int64_t K, int64_t n_out, int gemm_dt, bool copied) {
+    return gemm_dt != GNN_BF16 || static_cast<double>(cap_m) * static_cast<double>(K) * static_cast<double>(n_out) <
+                                      static_cast<double>(copied ? 1 << 28 : 1 << 25);
 }
 
 inline int64_t row8(int64_t n) { return (n + 7) / 8 * 8; }
@@ -43,6 +48,13 @@ struct Operands {
     const uint16_t *wt;        // W^T: n_out rows, ldw values apart
     int64_t ldw;
 };
+
+// Whether the tiles must have A (W) copied.
+inline bool copies_a(const ActArgs &a, int64_t chunk) {
+    return a.adt != GNN_BF16 || a.K() % 8 != 0 || (a.a_nbr && a.k_each % chunk != 0) || !aligned(a.a_self, 16) ||
+           !aligned(a.a_nbr, 16);
+}
+inline bool copies_w(const ActArgs &a) { return !a.wt || a.K() % 8 != 0 || !aligned(a.wt, 16); }
 
 // The operands of a (a1's halves of a whole number of `chunk` values), copied on s
 // where they must be.  weights: wt is wanted.

@@ -66,8 +66,7 @@ gnn_status prepare(const ActArgs &a, int64_t chunk, bool weights, void *ws, Oper
     char *base = static_cast<char *>(ws);
     *o = Operands{static_cast<const uint16_t *>(a.a_self), static_cast<const uint16_t *>(a.a_nbr), a.k_each, K, a.k_each,
                   a.wt, K};
-    if (a.adt != GNN_BF16 || K % 8 != 0 || (a.a_nbr && a.k_each % chunk != 0) || !aligned(a.a_self, 16) ||
-        !aligned(a.a_nbr, 16)) {
+    if (copies_a(a, chunk)) {
         uint16_t *out = reinterpret_cast<uint16_t *>(base + l.a);
         const unsigned grid = grid_of(a.cap_m * (ld / 8));
         if (a.adt == GNN_BF16)
@@ -83,7 +82,7 @@ gnn_status prepare(const ActArgs &a, int64_t chunk, bool weights, void *ws, Oper
         o->a1 = nullptr;
         o->k_each = o->K = o->lda = ld;
     }
-    if (!weights) return GNN_OK;
+    if (!weights || !copies_w(a)) return GNN_OK;
     if (!a.wt) {
         uint16_t *out = reinterpret_cast<uint16_t *>(base + l.w);
         pack_transpose_kernel<<<static_cast<unsigned>(ceil_div(ld, int64_t(64)) * ceil_div(a.n_out, int64_t(64))), kThreads,
@@ -91,7 +90,7 @@ gnn_status prepare(const ActArgs &a, int64_t chunk, bool weights, void *ws, Oper
         GNN_LAUNCHED("act_pack_w");
         o->wt = out;
         o->ldw = ld;
-    } else if (K % 8 != 0 || !aligned(a.wt, 16)) {
+    } else {
         uint16_t *out = reinterpret_cast<uint16_t *>(base + l.w);
         pack_rows_kernel<uint16_t><<<grid_of(a.n_out * (ld / 8)), kThreads, 0, s>>>(a.wt, nullptr, K, K, nullptr, a.n_out,
                                                                                   ld, out);
