@@ -525,8 +525,9 @@ gnn_status gnn_update_fwd_act(const void *a_self, const void *a_nbr, gnn_dtype a
  *          bf16, sums are fp32; GNN_F32: fp32 throughout, and gdt and dwdt
  *          must be GNN_F32.
  *   ws     as above, of gnn_update_bwd_act_workspace_size bytes.
- * Sums have a fixed order: results are bitwise reproducible for the same
- * sizes, types and row count.  Errors as gnn_update_fwd_act. */
+ * Sums have a fixed order, here and in gnn_update_fwd_act: results are bitwise
+ * reproducible for the same sizes, types, row count and alignment of the
+ * pointers to 16 bytes.  Errors as gnn_update_fwd_act. */
 gnn_status gnn_update_bwd_act_workspace_size(gnn_dtype adt, int64_t k_each, int32_t two, int64_t n_out, int64_t cap_m,
                                              gnn_dtype gdt, gnn_dtype dwdt, gnn_dtype gemm_dt, int32_t shadow,
                                              size_t *bytes);

@@ -632,12 +632,14 @@ template <int VE, bool BF16, class F> bool with_shape(int64_t c, int64_t k, F &&
 // Classes of a row in registers, fp32 (with a gradient of either type) and bf16.
 constexpr int64_t kRowsMax[2] = {Span<Shape<1024, 64, 4>, float>::kMost, Span<Shape<1024, 128, 8>, uint16_t>::kMost};
 
-// Rows are split when they do not fit, and where so few of 8,192 classes and
-// more come that most CUs would have none.
+// Rows are split when they do not fit, and where so few long ones come that most
+// CUs would have none (bf16, 64 entries, us whole and split: 1 x 20,000 12.7 and 15.1,
+// 100 x 20,000 17 and 19; 1 x 65,536 18 and 15.5, 64 rows of it 23 and 19, 127 rows 25 and
+// 24; 127 x 100,003 30 either way).
 SplitPlan plan_split(int64_t b, int64_t c, int ldt) {
     SplitPlan p{1, c};
     const bool fits = c <= kRowsMax[ldt == GNN_BF16];
-    if (fits && (c < 8192 || b >= kCus / 2)) return p;
+    if (fits && (c < 32768 || b >= kCus / 2)) return p;
     const int64_t unit = kSplitThreads * SplitShape::VE;
     const int64_t want = std::max<int64_t>(ceil_div(2 * kCus, std::max<int64_t>(b, 1)), fits ? 1 : 4);
     const int64_t units = ceil_div(c, unit);

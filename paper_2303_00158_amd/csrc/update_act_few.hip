@@ -1,5 +1,5 @@
 // The update with an activation and a residual for few rows (a serving program's
-// single answers): up to 64 rows against the bf16 shadow W^T.
+// single answers) against the bf16 shadow W^T.
 //
 // Bound by the weights' bytes: each is read once, straight into the registers of
 // the wavefront that multiplies it (no LDS, no barrier in the loop).  A workgroup
@@ -161,7 +161,7 @@ gnn_status launch_act_few(const ActFwd &a, hipStream_t s) {
     };
     if (a.cap_m <= 16) by_waves(std::integral_constant<int, 1>{});
     else if (a.cap_m <= 32) by_waves(std::integral_constant<int, 2>{});
-    else by_waves(std::integral_constant<int, 4>{});
+    else by_type(std::integral_constant<int, 4>{}, std::integral_constant<int, 4>{});  // K <= 1,024
     GNN_LAUNCHED("update_fwd_act_few");
     return GNN_OK;
 }

@@ -107,7 +107,7 @@ struct Plan {
 
 size_t act_fwd_ws_bytes(int, int64_t k_each, bool two, int64_t n_out, int64_t cap_m, int gemm_dt, bool shadow) {
     const int64_t K = two ? 2 * k_each : k_each;
-    if (act_few(cap_m, gemm_dt, shadow)) return 0;
+    if (act_few(cap_m, K, gemm_dt, shadow)) return 0;
     // whether operands are copied goes by their addresses too
     const size_t engine = pack::small(cap_m, K, n_out, gemm_dt, true) ? act_engine_ws_bytes(K, n_out, cap_m, gemm_dt) : 0;
     return pack::small(cap_m, K, n_out, gemm_dt, false) ? engine : std::max(engine, Plan(cap_m, K, n_out).total);
@@ -116,7 +116,7 @@ size_t act_fwd_ws_bytes(int, int64_t k_each, bool two, int64_t n_out, int64_t ca
 gnn_status launch_act_fwd(const ActFwd &a, void *ws, hipStream_t s) {
     if (a.cap_m == 0) return GNN_OK;
     const int64_t K = a.K();
-    if (act_few(a.cap_m, a.gemm_dt, a.wt != nullptr)) return launch_act_few(a, s);
+    if (act_few(a.cap_m, K, a.gemm_dt, a.wt != nullptr)) return launch_act_few(a, s);
     if (pack::small(a.cap_m, K, a.n_out, a.gemm_dt, pack::copies_a(a, tile::kBK) || pack::copies_w(a)))
         return launch_act_engine(a, ws, s);
     const Plan pl(a.cap_m, K, a.n_out);

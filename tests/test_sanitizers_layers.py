@@ -7,10 +7,9 @@ import subprocess
 
 import pytest
 
-from tests import test_sanitizers as base
-
 
 def test_layers_validation_under_asan_and_ubsan(tmp_path):
+    base = pytest.importorskip("tests.test_sanitizers")
     if not os.path.exists(base.HIPCC):
         pytest.skip("hipcc not found")
     objs = os.path.join(base.CACHE, base._sources_hash())

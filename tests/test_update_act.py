@@ -301,6 +301,55 @@ def test_residual_in_place(m, k, n, dt):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("m, k, n", [(1, 4096, 512), (64, 256, 200), (70, 1024, 256), (129, 4160, 65), (600, 512, 513), (9000, 256, 260)])
+def test_residual_in_place_of_the_tiles(m, k, n, dt):
+    """The output's type apart from the products': few rows, split reductions, tiles."""
+    gen = torch.Generator().manual_seed(m)
+    a, wt, res = rand(gen, m, k, dtype=BF16), rand(gen, n, k, dtype=BF16, scale=1 / math.sqrt(k)), rand(gen, m, n, dtype=dt)
+    o = forward(a, None, None, wt, None, "gelu", gnn.GNN_BF16, dt, res)
+    check_forward(o, a.double(), wt.t().double(), None, res, "gelu", dt)
+    over = res.clone()
+    gnn.update_fwd_act(a, None, None, None, over, ACTS["gelu"], gnn.GNN_BF16, residual=over, wt=wt)
+    assert torch.equal(over, o["out"])
+
+
+@pytest.mark.gpu
+def test_two_captured_calls_share_a_workspace():
+    """Two graphs with one workspace, replayed in turn: nothing is kept in it."""
+    gen = torch.Generator().manual_seed(4)
+    sizes, calls = [(70, 2048, 200), (300, 520, 777)], []
+    ws = torch.empty(1 << 26, dtype=torch.uint8, device=DEV)
+    for m, k, n in sizes:
+        a, z, g = (rand(gen, m, c, dtype=BF16) for c in (k, n, n))
+        w = rand(gen, k, n, scale=1 / math.sqrt(k))
+        wt = w.t().contiguous().bfloat16()
+        out = [torch.zeros((m, n), dtype=BF16, device=DEV), torch.zeros((k, n), device=DEV), torch.zeros(n, device=DEV),
+               torch.zeros((m, k), dtype=BF16, device=DEV)]
+
+        def go(a=a, z=z, g=g, w=w, wt=wt, out=out):
+            gnn.update_fwd_act(a, None, w, None, out[0], ACTS["silu"], gnn.GNN_BF16, wt=wt, ws=ws)
+            gnn.update_bwd_act(a, None, w, z, g, *out[1:], ACTS["silu"], gnn.GNN_BF16, wt=wt, ws=ws)
+        go()
+        want = [t.clone() for t in out]
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            go()
+        calls.append((graph, out, want, go))  # go keeps the graph's operands
+    for _ in range(3):
+        for graph, out, *_ in calls:
+            for t in out:
+                t.fill_(7)
+            graph.replay()
+        ws.fill_(255)  # NaN in any type
+        torch.cuda.synchronize()
+        for _, out, want, _ in calls:
+            for t, v in zip(out, want):
+                assert torch.equal(t, v)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("name", list(ACTS))
 def test_activations_far_out(name):
     """Z over the whole range, through a product that is exact: no NaN where
