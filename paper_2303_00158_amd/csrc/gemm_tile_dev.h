@@ -77,29 +77,38 @@ struct Choice {
     Pick pick;
     int64_t nsplit;
 };
+struct Pace {
+    double busy, lone, ends;
+};
+constexpr Pace kBigPace{1.6, 1.13, 20}, kBig7Pace{1.42, 1.02, 18}, kMidPace{0.48, 0.7, 4}, kSmallPace{0.19, 0.5, 1};
+// us of `tiles` tiles of `chunks` chunks, split n ways
+template <class C> inline double cost(int64_t tiles, int64_t chunks, int64_t n, const Pace &p) {
+    constexpr int64_t round = 256 * C::PER_CU;
+    const double each = static_cast<double>(ceil_div(chunks, n));
+    const int64_t last = ceil_div(n * tiles % round, int64_t(256));  // tiles a CU holds in the last round
+    double t = static_cast<double>(n * tiles / round * C::PER_CU) * (each * p.busy + p.ends);
+    if (last) t += each * std::max(p.lone, p.busy * last) + p.ends * last;
+    return t;
+}
 inline Choice choose(int64_t rows, int64_t cols, int64_t red) {
     Choice best{kSmall, 1};
     double least = -1;
-    auto look = [&](auto cfg, Pick pick, double busy, double lone, double ends) {
+    auto look = [&](auto cfg, Pick pick, const Pace &p) {
         using C = decltype(cfg);
         const int64_t chunks = std::max<int64_t>(ceil_div(red, int64_t(kBK)), 1);
         const int64_t tiles = ceil_div(rows, int64_t(C::BM)) * ceil_div(cols, int64_t(C::BN)), round = 256 * C::PER_CU;
         for (int64_t n = 1; n <= 16 && (n == 1 || (n * tiles <= round && n * 4 <= chunks)); n *= 2) {
-            const double each = static_cast<double>(ceil_div(chunks, n));
-            const int64_t last = ceil_div(n * tiles % round, int64_t(256));  // tiles a CU holds in the last round
-            double t = static_cast<double>(n * tiles / round * C::PER_CU) * (each * busy + ends);
-            if (last) t += each * std::max(lone, busy * last) + ends * last;
-            if (n > 1) t += 4 + static_cast<double>(n) * rows * cols * 8 / 4e6;
+            const double t = cost<C>(tiles, chunks, n, p) + (n > 1 ? 4 + static_cast<double>(n) * rows * cols * 8 / 4e6 : 0);
             if (least < 0 || t < least) {
                 least = t;
                 best = Choice{pick, n};
             }
         }
     };
-    look(Big{}, kBig, 1.6, 1.13, 20);
-    look(Big7{}, kBig7, 1.42, 1.02, 18);
-    look(Mid{}, kMid, 0.48, 0.7, 4);
-    look(Small{}, kSmall, 0.19, 0.5, 1);
+    look(Big{}, kBig, kBigPace);
+    look(Big7{}, kBig7, kBig7Pace);
+    look(Mid{}, kMid, kMidPace);
+    look(Small{}, kSmall, kSmallPace);
     return best;
 }
 // Reduction elements [*beg, *end) of split `split`, whole chunks.

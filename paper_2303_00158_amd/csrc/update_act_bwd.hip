@@ -339,12 +339,29 @@ struct Plan {
         ldz = pack::row8(n_out);
         da = tile::choose(cap_m, K, ldz);
         ld_a = (K + 3) / 4 * 4;
-        // dW: large tiles where they fill half the chip or the rows are long
-        // enough to split; each split at least 512 rows, one round of the CUs
-        auto tiles = [&](int64_t edge) { return halves * ceil_div(k_each, edge) * ceil_div(n_out, edge); };
-        mid = tiles(256) < 64;
-        const int64_t t = tiles(mid ? 128 : 256), slots = mid ? 512 : 256;
-        nsplit = std::max<int64_t>(1, std::min<int64_t>(slots / t, ceil_div(cap_m, int64_t(512))));
+        // dW: the tile size and the split of the rows that take the least time, as
+        // tile::choose has it, with at least four chunks a split; 128 x 128 tiles read
+        // twice as many T fragments a multiplication and are slower than their
+        // pace there, and the partials come back from the last-level cache.  With dZ,
+        // us in 256 x 256 and in 128 x 128 tiles: 8,192 x 1,024 x 1,024 54 and 44, 26,624 x
+        // 1,024 x 1,024 99 and 108, 8,192 x 2,048 x 2,048 91 and 96, 4,096 x 2,048 x 4,096 92
+        // and 80, 16,384 x 256 x 256 43 and 29.
+        const int64_t chunks = std::max<int64_t>(ceil_div(cap_m, int64_t(tile::kBK)), 1);
+        double least = -1;
+        auto look = [&](auto cfg, bool is_mid, const tile::Pace &pace) {
+            using C = decltype(cfg);
+            const int64_t t = halves * ceil_div(k_each, int64_t(C::BM)) * ceil_div(n_out, int64_t(C::BN));
+            for (int64_t n = 1; n == 1 || (n * t <= 256 * C::PER_CU && n * 4 <= chunks); n *= 2) {
+                const double us = tile::cost<C>(t, chunks, n, pace) + (n > 1 ? 4 + static_cast<double>(n) * K * n_out * 8 / 8e6 : 0);
+                if (least < 0 || us < least) {
+                    least = us;
+                    mid = is_mid;
+                    nsplit = n;
+                }
+            }
+        };
+        look(tile::Big{}, false, tile::kBigPace);
+        look(tile::Mid{}, true, tile::Pace{0.62, 0.8, 4});
         // dZ: about four workgroups to a CU, at least 32 rows each
         const int64_t stripes = ceil_div(ldz, int64_t(kStripe));
         parts = std::max<int64_t>(1, std::min<int64_t>(ceil_div(2048, stripes), ceil_div(cap_m, int64_t(32))));
