@@ -302,7 +302,7 @@ def test_residual_in_place(m, k, n, dt):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dt", [F32, BF16])
-@pytest.mark.parametrize("m, k, n", [(1, 4096, 512), (64, 256, 200), (70, 1024, 256), (129, 4160, 65), (600, 512, 513), (9000, 256, 260)])
+@pytest.mark.parametrize("m, k, n", [(1, 4096, 512), (64, 256, 200), (33, 4096, 512), (64, 1032, 777), (32, 1032, 777), (70, 1024, 256), (129, 4160, 65), (600, 512, 513), (9000, 256, 260)])
 def test_residual_in_place_of_the_tiles(m, k, n, dt):
     """The output's type apart from the products': few rows, split reductions, tiles."""
     gen = torch.Generator().manual_seed(m)
