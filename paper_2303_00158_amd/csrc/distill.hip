@@ -22,13 +22,14 @@
 // split over workgroups: one launch takes each part's maximum and sums (and
 // keeps the listed classes' logits, which a gradient in place of the logits
 // may overwrite), the next joins them and writes each part's gradient.
-#include "row_dev.h"
+#include "distill_rows.h"
 
 namespace gnn {
 
 namespace {
 
 using namespace row;
+using namespace distill;
 
 constexpr int64_t kCus = 256;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -41,7 +42,6 @@ struct Entries {
     float *w, *z;     // weight (first the teacher's value); the class's logit
     int32_t *cls;     // class, or -1; padded with -1 to a multiple of 4
 };
-__host__ __device__ inline int entries_padded(int64_t k) { return static_cast<int>((k + 1 + 3) / 4 * 4); }
 __device__ __forceinline__ Entries entries_at(float *lds, int slot, int kp) {
     float *p = lds + static_cast<int64_t>(slot) * 3 * kp;
     return Entries{p, p + kp, reinterpret_cast<int32_t *>(p + 2 * kp)};
@@ -153,58 +153,6 @@ __device__ __forceinline__ void put_entries(const Entries &en, const RowTerms &t
 // rows in registers
 // ---------------------------------------------------------------------------
 
-// A thread's share of a row of c elements, in vectors that lie in whole 128-byte
-// lines whatever the row's own address (off them a row of 100,003 bf16 classes
-// took 18% longer than one of 100,000).  `full` vectors hold elements in all of
-// the row's threads (at most NV, the same in every thread) but for the first
-// line's; the one after them is the row's end, of which some threads have a
-// part or nothing.  One uniform count in place of every vector's bounds keeps
-// those out of the registers: with bounds, 1,024 threads x 128 elements spilled
-// 154.  Where a thread's vector reaches over the row's start or end, the row's
-// first or last VE elements are loaded in its place, and those that are other
-// threads' are masked when it is used (trim): nothing waits for the load.
-template <class S, class TL> struct Span {
-    int c, head, full, rest;  // head: elements from the line to the row; rest: from the tail's place to the row's end
-    static constexpr int kLine = 128 / sizeof(TL);
-    static constexpr int64_t kMost = static_cast<int64_t>(S::T) * (S::E + S::VE) - kLine;  // longest row
-    static constexpr int kStep = S::T * S::VE;
-    __device__ __forceinline__ Span(const TL *row, int64_t c_) {
-        c = static_cast<int>(c_);
-        head = static_cast<int>((reinterpret_cast<uintptr_t>(row) & 127) / sizeof(TL));
-        full = (c + head) / kStep;
-        rest = c + head - (full * S::T + S::lane()) * S::VE;
-    }
-    __device__ __forceinline__ static uint32_t off() { return static_cast<uint32_t>(S::lane()) * S::VE; }
-    __device__ __forceinline__ int skip() const { return head - S::lane() * S::VE; }  // of the first vector, before the row
-    __device__ __forceinline__ bool first(int v) const { return v == 0 && skip() > 0; }
-    template <class T> __device__ __forceinline__ T *at(T *row, int v) const { return row - head + v * kStep + off(); }
-    // a whole vector (v < full)
-    __device__ __forceinline__ void load(Vec<TL, S::VE> &x, const TL *row, int v) const {
-        x.load(first(v) ? row : at(row, v));
-    }
-    __device__ __forceinline__ void trim(Vec<TL, S::VE> &x, int v) const {
-        if (first(v)) x.keep(0, S::VE - skip());
-    }
-    template <class T> __device__ __forceinline__ void store(const Vec<T, S::VE> &x, T *row, int v) const {
-        if (first(v)) x.store_some(row, 0, S::VE - skip());
-        else x.store(at(row, v));
-    }
-    // the row's end; rows of less than one whole vector a thread are taken
-    // element by element
-    __device__ __forceinline__ void load_tail(Vec<TL, S::VE> &x, const TL *row) const {
-        if (full == 0) x.load_some(at(row, 0), max(skip(), 0), rest, -INFINITY);
-        else x.load(rest >= S::VE ? at(row, full) : row + c - S::VE);
-    }
-    __device__ __forceinline__ void trim_tail(Vec<TL, S::VE> &x) const {
-        if (full != 0 && rest < S::VE) x.keep(S::VE - max(rest, 0), S::VE);
-    }
-    template <class T> __device__ __forceinline__ void store_tail(const Vec<T, S::VE> &x, T *row) const {
-        if (full == 0) x.store_some(at(row, 0), max(skip(), 0), rest);
-        else if (rest >= S::VE) x.store(at(row, full));
-        else if (rest > 0) x.store_some(row + c - S::VE, S::VE - rest, S::VE);
-    }
-};
-
 // A thread's running maximum and the sums relative to it.
 template <bool TWO> struct Online {
     float m = -INFINITY, sa = 0.f, sb = 0.f;
@@ -296,10 +244,6 @@ template <class S> constexpr int waves_wanted() { return S::T >= 512 ? 4 : 1; }
 // Vectors between a load and its use: a vector of 1,024 threads takes a CU's
 // share of the memory 1.6 us, in and out.
 constexpr int kLag = 2;
-// Sets of entries: a row's are read until after the next row's meeting, when a
-// thread may be at the row after that.
-constexpr int kSets = 3;
-
 // A row passes one meeting of its threads, after which its constants are known;
 // what is left of the row before (its listed classes' second store, its loss) is
 // done after the same meeting, which orders it behind that row's dense stores.
@@ -612,33 +556,14 @@ __global__ void __launch_bounds__(kLossThreads) distill_loss_kernel(const float 
     if (threadIdx.x == 0) *loss = row_scale || b == 0 ? s[0] : s[0] / static_cast<float>(b);
 }
 
-// The shape of a row of c classes in registers: at most 68 words a thread.
-// Long lists take a workgroup to a row: the sets of all its rows' entries lie in
-// LDS (64 KB hold 112 entries of 16 rows, 454 of four).
-template <class S, class F> bool if_fits(int64_t c, int64_t k, F &&go) {
-    if (c > Span<S, float>::kMost || kSets * S::kRows * entries_padded(k) * 12 > (64 << 10)) return false;
-    go(S{});
-    return true;
-}
-template <int VE, bool BF16, class F> bool with_shape(int64_t c, int64_t k, F &&go) {
-    return if_fits<Shape<16, 8, VE>>(c, k, go) || if_fits<Shape<64, 8, VE>>(c, k, go) ||
-           if_fits<Shape<64, 16, VE>>(c, k, go) || if_fits<Shape<64, 32, VE>>(c, k, go) ||
-           if_fits<Shape<64, 64, VE>>(c, k, go) || if_fits<Shape<256, 32, VE>>(c, k, go) ||
-           if_fits<Shape<256, 64, VE>>(c, k, go) ||
-           if_fits<Shape<512, 64, VE>>(c, k, go) || if_fits<Shape<1024, 64, VE>>(c, k, go) ||
-           (BF16 && if_fits<Shape<1024, BF16 ? 128 : 64, VE>>(c, k, go));
-}
-
-// Classes of a row in registers, fp32 (with a gradient of either type) and bf16.
-constexpr int64_t kRowsMax[2] = {Span<Shape<1024, 64, 4>, float>::kMost, Span<Shape<1024, 128, 8>, uint16_t>::kMost};
-
 // Rows are split when they do not fit, and where so few long ones come that most
 // CUs would have none (bf16, 64 entries, us whole and split: 1 x 20,000 12.7 and 15.1,
 // 100 x 20,000 17 and 19; 1 x 65,536 18 and 15.5, 64 rows of it 23 and 19, 127 rows 25 and
 // 24; 127 x 100,003 30 either way).
-SplitPlan plan_split(int64_t b, int64_t c, int ldt) {
+SplitPlan plan_split(int64_t b, int64_t c, int64_t k, int ldt) {
     SplitPlan p{1, c};
-    const bool fits = c <= kRowsMax[ldt == GNN_BF16];
+    const auto none = [](auto) {};
+    const bool fits = ldt == GNN_BF16 ? with_shape<uint16_t>(c, k, none) : with_shape<float>(c, k, none);
     if (fits && (c < 32768 || b >= kCus / 2)) return p;
     const int64_t unit = kSplitThreads * SplitShape::VE;
     const int64_t want = std::max<int64_t>(ceil_div(2 * kCus, std::max<int64_t>(b, 1)), fits ? 1 : 4);
@@ -654,7 +579,7 @@ size_t distill_ws_bytes(int64_t b, int64_t c, int64_t k) {
     // either type's plan: the row losses, the parts' sums, the entries' logits
     int64_t parts = 0;
     for (int dt : {GNN_F32, GNN_BF16}) {
-        const SplitPlan p = plan_split(b, c, dt);
+        const SplitPlan p = plan_split(b, c, k, dt);
         if (p.parts > 1) parts = std::max(parts, p.parts);
     }
     size_t bytes = round_up(static_cast<size_t>(std::max<int64_t>(b, 1)) * 4, 256);
@@ -667,7 +592,7 @@ gnn_status launch_distill(const DistillArgs &a, void *ws, hipStream_t s) {
     const size_t rows_bytes = round_up(static_cast<size_t>(std::max<int64_t>(a.b, 1)) * 4, 256);
     float *row_loss = a.row_loss ? a.row_loss : reinterpret_cast<float *>(base);
     if (a.b > 0) {
-        const SplitPlan p = plan_split(a.b, a.c, a.ldt);
+        const SplitPlan p = plan_split(a.b, a.c, a.k, a.ldt);
         const int entry_bytes = entries_padded(a.k) * 12;
         const bool two = a.labels && a.alpha > 0.f && a.alpha < 1.f && a.temperature != 1.f;
         auto go = [&](auto tl, auto tg, auto t2) {
@@ -683,7 +608,7 @@ gnn_status launch_distill(const DistillArgs &a, void *ws, hipStream_t s) {
                 distill_join_kernel<TL, TG, TWO><<<grid, kSplitThreads, entry_bytes, s>>>(a, p, st, row_loss);
                 return;
             }
-            with_shape<sizeof(TL) == 4 ? 4 : 8, sizeof(TL) == 2>(a.c, a.k, [&](auto shape) {
+            with_shape<TL>(a.c, a.k, [&](auto shape) {
                 using S = decltype(shape);
                 // one round of the CUs with what fits on each: workgroups walk
                 // their rows and load each ahead
