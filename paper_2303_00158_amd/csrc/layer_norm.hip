@@ -183,13 +183,15 @@ __global__ void __launch_bounds__(S::kThreads) layer_norm_bwd_kernel(BwdArgs p) 
             }
 #pragma unroll
             for (int e = 0; e < S::VE; ++e) {
-                // past the row's end g is 0, and so are q and its products
-                const float ge = og.get(e), h = (ox.get(e) - mu) * r, q = ge * wg.get(e);
+                // Past the row's end g is 0, and so are q and its product with the
+                // finite d: the row's sum takes its factor r behind (d r there is
+                // -mu r, which can be infinite in a finite row, and 0 times it NaN).
+                const float ge = og.get(e), d = ox.get(e) - mu, q = ge * wg.get(e);
                 s[0] += q;
-                s[1] = fmaf(q, h, s[1]);
+                s[1] = fmaf(q, d, s[1]);
                 if constexpr (SUMS) {
                     if (live) {
-                        sa[v * S::VE + e] = fmaf(ge, h, sa[v * S::VE + e]);
+                        sa[v * S::VE + e] = fmaf(ge, d * r, sa[v * S::VE + e]);
                         sb[v * S::VE + e] += ge;
                     }
                 }
@@ -197,7 +199,7 @@ __global__ void __launch_bounds__(S::kThreads) layer_norm_bwd_kernel(BwdArgs p) 
         }
         if (!d_x) continue;
         over(Add{}, s);
-        const float m0 = s[0] / n, m1 = s[1] / n;
+        const float m0 = s[0] / n, m1 = s[1] * r / n;
         if (!live) continue;
 #pragma unroll(kHold ? S::NV : 1)
         for (int v = 0; v < S::NV; ++v) {
