@@ -555,14 +555,17 @@ gnn_status gnn_softmax_ce(const float *logits, int64_t b, int64_t c, const int64
  *          GNN_F32 or GNN_BF16) and the classes they belong to (int64).  An
  *          entry whose index is outside [0, c) or whose value is -infinity is
  *          absent; a class may be listed more than once.
- *   With the temperature T > 0, p_i = softmax over row i's present entries of
- *   t_val / T, and the targets y_i as in gnn_softmax_ce,
+ *   With the temperature T in [1e-18, 1e18] (T^2 and 1 / T are in fp32's
+ *   range), p_i = softmax over row i's present entries of t_val / T, and the
+ *   targets y_i as in gnn_softmax_ce,
  *     soft_i = T^2 sum_e p_ie (log p_ie - log softmax(z_i / T)[t_idx_ie]),
  *              0 for a row without entries,
  *     hard_i = -log softmax(z_i)[y_i], 0 for a label outside [0, c),
  *     row_loss_i = alpha soft_i + (1 - alpha) hard_i,
  *     loss = sum_i scale_i row_loss_i.
  *   An entry whose p is 0 adds nothing, whatever its class's logit.
+ *   (soft_i is T^2 times a difference of logarithms that shrinks with T: of a
+ *   high temperature it is exact to some 2^-22 T^2, the gradient to 2^-22 T.)
  *   alpha  in [0, 1]; with 1 (0) the labels (the teacher) are not read.
  *   labels [device] int64, or NULL: no hard term; targets [device] int64 b or
  *          NULL as in gnn_softmax_ce.

@@ -695,8 +695,8 @@ gnn_status gnn_distill_topk(const void *logits, gnn_dtype ldt, int64_t b, int64_
     GNN_CHECK(act_dtype(ldt) && act_dtype(tdt) && act_dtype(gdt), GNN_EUNSUPPORTED,
               "%s: dtypes must be GNN_F32 or GNN_BF16", who);
     GNN_TRY(check_distill(b, c, k, who));
-    GNN_CHECK(temperature > 0.f && std::isfinite(temperature), GNN_EINVAL, "%s: temperature must be finite and positive",
-              who);
+    // beyond these its reciprocal or its square leaves fp32's range
+    GNN_CHECK(temperature >= 1e-18f && temperature <= 1e18f, GNN_EINVAL, "%s: temperature out of [1e-18, 1e18]", who);
     GNN_CHECK(alpha >= 0.f && alpha <= 1.f, GNN_EINVAL, "%s: alpha out of [0, 1]", who);
     GNN_CHECK(((logits && t_val && t_idx) || b == 0) && loss_out && ws, GNN_EINVAL, "%s: NULL pointer", who);
     GNN_CHECK(g_out != logits || !g_out || gdt == ldt, GNN_EINVAL, "%s: g_out may be logits only with the same dtype",
