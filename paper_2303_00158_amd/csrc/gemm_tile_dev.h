@@ -234,7 +234,15 @@ template <class C> struct Acc {
 __device__ __forceinline__ void mma(f32x4 &acc, const bf16x8 &x, const bf16x8 &y) {
     asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(x), "v"(y));
 }
-__device__ __forceinline__ void settle() { asm volatile("s_nop 15\n\ts_nop 15" ::: "memory"); }
+// Each sum passes through a statement of no instructions behind the wait, so that
+// what reads it cannot be moved in front (tests/test_tile_sums.py).
+template <class C> __device__ __forceinline__ void settle(Acc<C> &acc) {
+    asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < C::MI; ++i)
+#pragma unroll
+        for (int j = 0; j < C::NI; ++j) asm volatile("" : "+a"(acc.v[i][j]));
+}
 
 template <class C> struct Frags {
     bf16x8 a[C::MI], b[C::NI];
@@ -312,7 +320,7 @@ template <class C, bool TA, bool TB> struct Product {
             step<1>(acc, f, ring, c + 1);
         }
         wide::chunk_barrier<wide::waitcnt(0, 0)>();  // the stages are drained
-        settle();
+        settle(acc);
     }
 };
 
