@@ -487,7 +487,8 @@ gnn_status gnn_update_bwd_noalloc(const void *a_self, const void *a_nbr, gnn_dty
  *   Z = A W + b,  out = act(Z) + residual.
  * GNN_ACT_GELU is z Phi(z) with the normal distribution's Phi, _GELU_TANH its
  * form z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2, _SILU
- * z / (1 + exp(-z)); _RELU gives 0 for a NaN, as gnn_update_fwd's.
+ * z / (1 + exp(-z)), these three NaN at -infinity (-infinity times 0); _RELU
+ * gives 0 for a NaN, as gnn_update_fwd's.
  *   a_self, a_nbr, adt, k_each, m_dev, cap_m, w, wt, bias, n_out, gemm_dt: as
  *          gnn_update_fwd, and with GNN_BF16 either of w and wt may be NULL
  *          (wt is read where both are given; any K).
@@ -580,10 +581,13 @@ gnn_status gnn_softmax_ce(const float *logits, int64_t b, int64_t c, const int64
  *   ws     [device] 256-byte aligned workspace of
  *          gnn_distill_topk_workspace_size bytes; no state is kept in it
  *          between calls; calls sharing it must not overlap.
- * Sums and probabilities are fp32; every sum has a fixed order, so results
- * are bitwise reproducible.  A NaN logit, a +infinity, or a row of -infinity
- * alone makes its row's loss NaN; a -infinity logit has probability 0 (and
- * an infinite loss where the teacher's is not 0).  Errors: GNN_EINVAL for bad
+ * Sums and probabilities are fp32; every sum has a fixed order, which goes by
+ * the sizes, the types and the place of logits in its 128-byte line: for the
+ * same of these, results are bitwise reproducible.  A NaN logit, a +infinity,
+ * or a row of -infinity alone makes its row's loss NaN where the row has a
+ * term, and so does a NaN or a +infinity among the teacher's present values;
+ * a -infinity logit has probability 0 (and an infinite loss where the
+ * teacher's is not 0).  Errors: GNN_EINVAL for bad
  * sizes, temperature or alpha, NULL or misaligned (to the element) pointers;
  * GNN_EUNSUPPORTED for other dtypes; GNN_ESIZE for a small workspace. */
 #define GNN_MAX_CLASSES (1 << 20)
@@ -608,8 +612,9 @@ gnn_status gnn_distill_topk(const void *logits, gnn_dtype ldt, int64_t b, int64_
  *   y      [device] cap_m x f of ydt; may be x itself when ydt == xdt.
  *   mean, rstd  [device] fp32 cap_m each, or NULL when no backward follows.
  * The statistics are fp32: the mean first, then the squares of the distances
- * from it, so rows far from zero lose nothing.  A NaN or an infinity makes
- * its own row NaN and no other.  Errors: GNN_EINVAL for bad sizes, eps,
+ * from it, so rows far from zero lose nothing; a row's sum and its sum of
+ * squared distances have to be in fp32's range (values up to some 1e18).  A NaN
+ * or an infinity makes its own row NaN and no other.  Errors: GNN_EINVAL for bad sizes, eps,
  * NULL or misaligned (to the element) pointers; GNN_EUNSUPPORTED for other
  * dtypes. */
 gnn_status gnn_layer_norm_fwd(const void *x, gnn_dtype xdt, const int64_t *m_dev, int64_t cap_m, int64_t f,

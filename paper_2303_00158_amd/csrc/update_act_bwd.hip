@@ -10,6 +10,9 @@
 // shadow W^T, whose rows are the reduction, a T operand, so that the weights are
 // read as the forward keeps them.  (Without the shadow, W is rounded to bf16 rows
 // in the workspace, an N operand.)
+// dZ is an operand of bf16 products, so it is rounded before them: with A or W^T
+// exact in bf16, dW and dA are then off by 0.0023 in the root mean square (8,192 x 4,096 x
+// 4,096), where the rounding of a bf16 output alone is 0.0017.
 // fp32 products take the update's own kernels (gemm_bwd.hip) on an fp32 dZ.
 #include "act_pack.h"
 #include "gemm_tile_dev.h"
