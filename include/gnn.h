@@ -614,9 +614,9 @@ gnn_status gnn_distill_topk(const void *logits, gnn_dtype ldt, int64_t b, int64_
  * The statistics are fp32: the mean first, then the squares of the distances
  * from it, so rows far from zero lose nothing; a row's sum and its sum of
  * squared distances have to be in fp32's range (values up to some 1e18).  A NaN
- * or an infinity makes its own row NaN and no other.  Errors: GNN_EINVAL for bad sizes, eps,
- * NULL or misaligned (to the element) pointers; GNN_EUNSUPPORTED for other
- * dtypes. */
+ * or an infinity makes its own row NaN and no other.  Errors: GNN_EINVAL for
+ * bad sizes, eps, NULL or misaligned (to the element) pointers;
+ * GNN_EUNSUPPORTED for other dtypes. */
 gnn_status gnn_layer_norm_fwd(const void *x, gnn_dtype xdt, const int64_t *m_dev, int64_t cap_m, int64_t f,
                               const float *gamma, const float *beta, float eps, void *y, gnn_dtype ydt, float *mean,
                               float *rstd, gnn_stream s);

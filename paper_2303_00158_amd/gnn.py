@@ -729,10 +729,11 @@ def distill_topk(logits: torch.Tensor, t_val: torch.Tensor, t_idx: torch.Tensor,
                  row_scale: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None):
     """gnn_distill_topk: the loss of the student's logits (b x c) against the
     teacher's k largest (t_val, t_idx: b x k; an entry with an index outside
-    [0, c) is absent) at a temperature, mixed as alpha soft + (1 - alpha) hard
-    with the labels' cross-entropy, and its gradient g_out (may be logits
-    itself; None: the loss alone).  row_scale: each row's factor in the loss
-    (1 / b when None; 0 skips the row).  ws: workspace (allocated when None)."""
+    [0, c) is absent) at a temperature in [1e-18, 1e18], mixed as
+    alpha soft + (1 - alpha) hard with the labels' cross-entropy, and its
+    gradient g_out (may be logits itself; None: the loss alone).  row_scale:
+    each row's factor in the loss (1 / b when None; 0 skips the row).  ws:
+    workspace (allocated when None)."""
     b, c = _matrix("logits", logits)
     dev = logits.device
     _want("t_val", t_val, (b, None), _ACTIVATIONS, dev)
