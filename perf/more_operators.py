@@ -33,7 +33,7 @@ Operators, for rows i:
              key ^ (element / 2)) the four 16-bit parts of h, in their order,
              are for m and sqrt(v) of the even element and of the odd one, key =
              mix(mix(mix(seed) ^ t) ^ tensor), mix the output function of
-             SplitMix64
+             SplitMix64 (without its increment)
 
 Where the matrix products run in bf16, dz is rounded to bf16 as their operand
 and the gradients that are summed from it are kept in bf16 too.
@@ -328,16 +328,14 @@ def _signed(x):
 
 
 def _mix(x):
-    """The output function of SplitMix64 of an integer or of int64 values."""
-    one, two, three = 0x9E3779B97F4A7C15, 0xBF58476D1CE4E5B9, 0x94D049BB133111EB
+    """The output function of SplitMix64, of an integer or of int64 values."""
+    one, two = 0xBF58476D1CE4E5B9, 0x94D049BB133111EB
     if isinstance(x, int):
-        x = (x + one) % (1 << 64)
-        x = ((x ^ (x >> 30)) * two) % (1 << 64)
-        x = ((x ^ (x >> 27)) * three) % (1 << 64)
+        x = ((x ^ (x >> 30)) * one) % (1 << 64)
+        x = ((x ^ (x >> 27)) * two) % (1 << 64)
         return x ^ (x >> 31)
-    x = x + _signed(one)
-    x = (x ^ ((x >> 30) & ((1 << 34) - 1))) * _signed(two)
-    x = (x ^ ((x >> 27) & ((1 << 37) - 1))) * _signed(three)
+    x = (x ^ ((x >> 30) & ((1 << 34) - 1))) * _signed(one)
+    x = (x ^ ((x >> 27) & ((1 << 37) - 1))) * _signed(two)
     return x ^ ((x >> 31) & ((1 << 33) - 1))
 
 
