@@ -70,7 +70,7 @@ typedef int32_t gnn_status;
 typedef int32_t gnn_dtype;
 typedef int32_t gnn_agg;
 typedef int32_t gnn_loc;
-enum { GNN_F32 = 0, GNN_BF16 = 1, GNN_F16 = 2 };
+enum { GNN_F32 = 0, GNN_BF16 = 1, GNN_F16 = 2, GNN_F8E4M3 = 3 /* gnn_adamw's states only */ };
 /* GNN_AGG_SAGE_MAX: GraphSAGE with the max aggregator (Section II-A); its
  * update reads [h_self || max] as the mean model reads [h_self || mean].
  * The model-level calls (gnn_train_step and its stages) take it; the
@@ -187,6 +187,42 @@ gnn_status gnn_build_block(const gnn_graph *g, const float *gcn_norm, const int6
 gnn_status gnn_gather_features(const void *table, gnn_dtype tdt, gnn_loc loc, int64_t n_rows, int64_t dim,
                                int64_t row_stride, const int64_t *ids, const int64_t *n_ids_dev, int64_t cap_ids,
                                void *out, gnn_dtype odt, gnn_stream s);
+
+/* ------------------------------------------------------------------------
+ * A trained table (features of vertices, tokens or classes that the training
+ * moves, in place of Section III-A's given ones): lookup of its rows,
+ *   out_i = scale table[ids_i], or 0 where ids_i is outside [0, n_rows).
+ *   table  [device] n_rows x row_stride (>= dim) elements of tdt.
+ *   ids    [device] int64; n_ids_dev [device] int64 count, or NULL to use
+ *          cap_ids.  Rows of out at or past the count are left untouched.
+ *   out    [device] cap_ids x dim of odt.
+ * Types GNN_F32 and GNN_BF16; the product is fp32, rounded once.  Errors:
+ * GNN_EINVAL for bad sizes, a scale that is not finite, NULL or misaligned (to
+ * the element) pointers; GNN_EUNSUPPORTED for other dtypes. */
+gnn_status gnn_embed_fwd(const void *table, gnn_dtype tdt, int64_t n_rows, int64_t dim, int64_t row_stride,
+                         const int64_t *ids, const int64_t *n_ids_dev, int64_t cap_ids, float scale, void *out,
+                         gnn_dtype odt, gnn_stream s);
+
+/* The table's gradient from g = dLoss/dout:
+ *   d_table_v = scale sum over the i with ids_i = v of g_i.
+ *   g       [device] cap_ids x dim of gdt; ids, n_ids_dev, cap_ids as above
+ *           (cap_ids and n_rows below 2^31).  Rows of g whose id is outside
+ *           [0, n_rows), or at or past the count, are not read.
+ *   d_table [device] n_rows x dim of ddt.  accumulate == 0: overwritten, rows
+ *           that no id names with 0.  Else the sum is added to what it holds (in
+ *           fp32, rounded once), and rows that no id names are not touched: the
+ *           gradient of a table that is used in two places, or of a table
+ *           far larger than what a step names.
+ *   ws      [device] 256-byte aligned workspace of
+ *           gnn_embed_bwd_workspace_size bytes (NULL when cap_ids is 0); no state is
+ *           kept in it between calls; calls sharing it must not overlap.
+ * Sums are fp32 in an order that goes by the ids' order, cap_ids and dim alone
+ * (no atomics): results are bitwise reproducible.  Errors as gnn_embed_fwd,
+ * and GNN_ESIZE for a small workspace or sizes past the grid limit. */
+gnn_status gnn_embed_bwd_workspace_size(int64_t cap_ids, int64_t n_rows, int64_t dim, size_t *bytes);
+gnn_status gnn_embed_bwd(const void *g, gnn_dtype gdt, const int64_t *ids, const int64_t *n_ids_dev, int64_t cap_ids,
+                         int64_t dim, float scale, int64_t n_rows, int32_t accumulate, void *d_table, gnn_dtype ddt,
+                         void *ws, size_t ws_bytes, gnn_stream s);
 
 /* ------------------------------------------------------------------------
  * Aggregation (equation 1; GCN and GraphSAGE operators of Section II-A).
@@ -647,6 +683,48 @@ gnn_status gnn_layer_norm_bwd(const void *g, gnn_dtype gdt, const void *x, gnn_d
 /* Plain SGD (synchronous SGD of Section II-B on one device): w -= lr * dw
  * over n fp32 values [device]. */
 gnn_status gnn_sgd(float *w, const float *dw, int64_t n, float lr, gnn_stream s);
+
+/* AdamW over the tensors of a model, 48 of them to a launch.  For element e of
+ * each tensor, with t the number of this step (the first is 1):
+ *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
+ *   w = w (1 - lr weight_decay)
+ *       - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps).
+ * sdt GNN_F32: m and v are kept in fp32.
+ * sdt GNN_F8E4M3: what is kept is m and r = sqrt(v), in e4m3 (4 exponent and 3
+ *   mantissa bits, largest value 448), times an fp32 scale for each group of
+ *   GNN_ADAMW_GROUP elements of a tensor (the last one may be shorter), chosen so
+ *   that the group's largest magnitude is 448.  The step uses the new m and
+ *   v before they are rounded.  With x a magnitude over its scale and u its step (2^-9
+ *   below 2^-6, else an eighth of its power of two), u floor(x / u + chance) is
+ *   kept (448 at most), so that on average nothing is lost.  chance =
+ *   (bits + 1/2) / 2^16 with 16 bits of h = mix(key ^ (e / 2)): bits 0 to 15 for m of
+ *   an even e, 16 to 31 for r, 32 to 47 and 48 to 63 for m and r of an odd e; key = mix(mix(
+ *   mix(seed) ^ t) ^ number of the tensor in the call), mix as the sampler's.  A
+ *   group whose largest magnitude is below 448 2^-126 is kept as zeros.  A NaN or
+ *   an infinity among a group's new m (r) makes all of the group's m (r) NaN.
+ * Arithmetic is fp32 (bias corrections fp64, rounded once).  lr, beta1, beta2,
+ * eps: beta1 and beta2 in [0, 1), lr and eps finite and not negative.
+ *   lr_dev   [device] fp32, or NULL: read in place of lr;
+ *   step_dev [device] int64, or NULL: read in place of step, so that a captured
+ *            step goes on counting where the caller adds 1 to it.
+ * Tensors must not overlap; a tensor of 0 elements may have NULL pointers.
+ * The tensors' array [host] is read before the call returns.  Errors:
+ * GNN_EINVAL for bad counts or rates, NULL or misaligned (to the element)
+ * pointers; GNN_EUNSUPPORTED for other dtypes. */
+#define GNN_ADAMW_GROUP 256
+typedef struct gnn_adamw_tensor {
+    float *w;                 /* [device] fp32 n, updated */
+    const void *g;            /* [device] gradient, n of gdt */
+    void *m, *v;              /* [device] state, n of the call's sdt each (GNN_F8E4M3: m and sqrt(v)), updated */
+    float *m_scale, *v_scale; /* [device] fp32 ceil(n / GNN_ADAMW_GROUP) for GNN_F8E4M3; else NULL */
+    uint16_t *shadow;         /* [device] bf16 n, or NULL: written with the new w */
+    int64_t n;
+    double weight_decay;      /* finite, not negative */
+    gnn_dtype gdt;            /* GNN_F32 or GNN_BF16 */
+} gnn_adamw_tensor;
+gnn_status gnn_adamw(const gnn_adamw_tensor *tensors, int64_t count, gnn_dtype sdt, double lr, double beta1,
+                     double beta2, double eps, int64_t step, const float *lr_dev, const int64_t *step_dev,
+                     uint64_t seed, gnn_stream s);
 
 /* ------------------------------------------------------------------------
  * One whole training iteration (Section II-B, Figure 1): sample L blocks,

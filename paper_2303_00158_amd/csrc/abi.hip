@@ -111,6 +111,13 @@ gnn_status check_act(const ActArgs &a, bool weights, const char *who) {
     return GNN_OK;
 }
 
+gnn_status check_embed(int64_t cap_ids, int64_t n_rows, int64_t dim, const char *who) {
+    GNN_CHECK(dim_ok(dim), GNN_EINVAL, "%s: dim out of [1, %d]", who, GNN_MAX_DIM);
+    GNN_CHECK(n_rows >= 1 && n_rows < (1ll << 31), GNN_EINVAL, "%s: n_rows out of [1, 2^31)", who);
+    GNN_CHECK(cap_ids >= 0 && cap_ids < (1ll << 31), GNN_EINVAL, "%s: cap_ids out of [0, 2^31)", who);
+    return GNN_OK;
+}
+
 gnn_status check_graph(const gnn_graph *g, const char *who) {
     GNN_CHECK(g, GNN_EINVAL, "%s: graph is NULL", who);
     GNN_CHECK(g->n >= 0 && g->nnz >= 0, GNN_EINVAL, "%s: negative graph size", who);
@@ -300,6 +307,48 @@ gnn_status gnn_gather_features(const void *table, gnn_dtype tdt, gnn_loc loc, in
     GNN_TRY(device_view(table, loc, &t, who));
     return launch_gather(t, tdt, dim, row_stride, ids, n_ids_dev, cap_ids, out, odt, loc == GNN_LOC_HOST_PINNED,
                          stream_of(s));
+}
+
+gnn_status gnn_embed_fwd(const void *table, gnn_dtype tdt, int64_t n_rows, int64_t dim, int64_t row_stride,
+                         const int64_t *ids, const int64_t *n_ids_dev, int64_t cap_ids, float scale, void *out,
+                         gnn_dtype odt, gnn_stream s) {
+    clear_error();
+    const char *who = "gnn_embed_fwd";
+    GNN_CHECK(act_dtype(tdt) && act_dtype(odt), GNN_EUNSUPPORTED, "%s: dtypes must be GNN_F32 or GNN_BF16", who);
+    GNN_TRY(check_embed(cap_ids, n_rows, dim, who));
+    GNN_CHECK(row_stride >= dim && row_stride < (1ll << 32), GNN_EINVAL, "%s: bad row_stride", who);
+    GNN_CHECK(std::isfinite(scale), GNN_EINVAL, "%s: scale must be finite", who);
+    GNN_CHECK((table && ids && out) || cap_ids == 0, GNN_EINVAL, "%s: NULL pointer", who);
+    GNN_CHECK(out != table || cap_ids == 0, GNN_EINVAL, "%s: out must not be the table", who);
+    GNN_CHECK(aligned(table, dtype_size(tdt)) && aligned(out, dtype_size(odt)) && aligned(ids, 8) && aligned(n_ids_dev, 8),
+              GNN_EINVAL, "%s: misaligned data", who);
+    return launch_embed_fwd(table, tdt, n_rows, dim, row_stride, ids, n_ids_dev, cap_ids, scale, out, odt, stream_of(s));
+}
+
+gnn_status gnn_embed_bwd_workspace_size(int64_t cap_ids, int64_t n_rows, int64_t dim, size_t *bytes) {
+    clear_error();
+    const char *who = "gnn_embed_bwd_workspace_size";
+    GNN_CHECK(bytes, GNN_EINVAL, "%s: bytes is NULL", who);
+    GNN_TRY(check_embed(cap_ids, n_rows, dim, who));
+    *bytes = cap_ids ? embed_bwd_ws_bytes(cap_ids, n_rows, dim) : 0;
+    return GNN_OK;
+}
+
+gnn_status gnn_embed_bwd(const void *g, gnn_dtype gdt, const int64_t *ids, const int64_t *n_ids_dev, int64_t cap_ids,
+                         int64_t dim, float scale, int64_t n_rows, int32_t accumulate, void *d_table, gnn_dtype ddt,
+                         void *ws, size_t ws_bytes, gnn_stream s) {
+    clear_error();
+    const char *who = "gnn_embed_bwd";
+    GNN_CHECK(act_dtype(gdt) && act_dtype(ddt), GNN_EUNSUPPORTED, "%s: dtypes must be GNN_F32 or GNN_BF16", who);
+    GNN_TRY(check_embed(cap_ids, n_rows, dim, who));
+    GNN_CHECK(std::isfinite(scale), GNN_EINVAL, "%s: scale must be finite", who);
+    GNN_CHECK(((g && ids) || cap_ids == 0) && d_table, GNN_EINVAL, "%s: NULL pointer", who);
+    GNN_CHECK(d_table != g, GNN_EINVAL, "%s: d_table must not be g", who);
+    GNN_CHECK(aligned(g, dtype_size(gdt)) && aligned(d_table, dtype_size(ddt)) && aligned(ids, 8) && aligned(n_ids_dev, 8),
+              GNN_EINVAL, "%s: misaligned data", who);
+    if (cap_ids) GNN_TRY(check_ws(ws, ws_bytes, embed_bwd_ws_bytes(cap_ids, n_rows, dim), who));
+    return launch_embed_bwd(g, gdt, ids, n_ids_dev, cap_ids, dim, scale, n_rows, accumulate != 0, d_table, ddt, ws,
+                            stream_of(s));
 }
 
 gnn_status gnn_aggregate_fwd(const gnn_block *b, gnn_agg kind, const void *h_src, gnn_dtype hdt, int64_t f,
@@ -766,6 +815,36 @@ gnn_status gnn_sgd(float *w, const float *dw, int64_t n, float lr, gnn_stream s)
     GNN_CHECK((w && dw) || n == 0, GNN_EINVAL, "gnn_sgd: NULL pointer");
     GNN_CHECK(aligned(w, 4) && aligned(dw, 4), GNN_EINVAL, "gnn_sgd: misaligned data");
     return launch_sgd(w, dw, n, lr, stream_of(s));
+}
+
+gnn_status gnn_adamw(const gnn_adamw_tensor *tensors, int64_t count, gnn_dtype sdt, double lr, double beta1,
+                     double beta2, double eps, int64_t step, const float *lr_dev, const int64_t *step_dev,
+                     uint64_t seed, gnn_stream s) {
+    clear_error();
+    const char *who = "gnn_adamw";
+    GNN_CHECK(sdt == GNN_F32 || sdt == GNN_F8E4M3, GNN_EUNSUPPORTED, "%s: states must be GNN_F32 or GNN_F8E4M3", who);
+    GNN_CHECK(count >= 0 && count < (1ll << 31) && (tensors || count == 0), GNN_EINVAL, "%s: bad tensors", who);
+    GNN_CHECK(beta1 >= 0 && beta1 < 1 && beta2 >= 0 && beta2 < 1, GNN_EINVAL, "%s: beta1 and beta2 must be in [0, 1)", who);
+    GNN_CHECK(lr_dev || (lr >= 0 && std::isfinite(lr)), GNN_EINVAL, "%s: lr must be finite and not negative", who);
+    GNN_CHECK(eps >= 0 && std::isfinite(eps), GNN_EINVAL, "%s: eps must be finite and not negative", who);
+    GNN_CHECK(step_dev || step >= 1, GNN_EINVAL, "%s: the first step is 1", who);
+    GNN_CHECK(aligned(lr_dev, 4) && aligned(step_dev, 8), GNN_EINVAL, "%s: misaligned data", who);
+    const size_t ss = sdt == GNN_F32 ? 4 : 1;
+    for (int64_t i = 0; i < count; ++i) {
+        const gnn_adamw_tensor &t = tensors[i];
+        const long long at = static_cast<long long>(i);
+        GNN_CHECK(act_dtype(t.gdt), GNN_EUNSUPPORTED, "%s: tensor %lld: gdt must be GNN_F32 or GNN_BF16", who, at);
+        GNN_CHECK(t.n >= 0 && t.n < (1ll << 34), GNN_EINVAL, "%s: tensor %lld: n out of [0, 2^34)", who, at);
+        GNN_CHECK(t.weight_decay >= 0 && std::isfinite(t.weight_decay), GNN_EINVAL,
+                  "%s: tensor %lld: weight_decay must be finite and not negative", who, at);
+        if (t.n == 0) continue;
+        GNN_CHECK(t.w && t.g && t.m && t.v && (sdt == GNN_F32 || (t.m_scale && t.v_scale)), GNN_EINVAL,
+                  "%s: tensor %lld: NULL pointer", who, at);
+        GNN_CHECK(aligned(t.w, 4) && aligned(t.g, dtype_size(t.gdt)) && aligned(t.m, ss) && aligned(t.v, ss) &&
+                      aligned(t.m_scale, 4) && aligned(t.v_scale, 4) && aligned(t.shadow, 2),
+                  GNN_EINVAL, "%s: tensor %lld: misaligned data", who, at);
+    }
+    return launch_adamw(tensors, count, sdt, lr, beta1, beta2, eps, step, lr_dev, step_dev, seed, stream_of(s));
 }
 
 gnn_status gnn_train_step_layout(const gnn_model *m, int64_t graph_n, int64_t batch, gnn_step_layout *out) {

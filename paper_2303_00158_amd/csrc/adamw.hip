@@ -1,0 +1,295 @@
+// The AdamW step over many tensors in one launch:
+//   m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2,
+//   w = w (1 - lr decay) - lr m / (1 - b1^t) / (sqrt(v / (1 - b2^t)) + eps)
+// and, where it is kept, the bf16 copy of w.
+//
+// Bound by memory: w, m and v once in and out and g once in.  A workgroup takes
+// a chunk of one tensor, found among the records in the kernel's arguments, so
+// that a model's small tensors share a launch with its large ones.
+//
+// States in 8 bits: m and r = sqrt(v) are e4m3 values times an fp32 scale for
+// each group of 256 elements, which a wavefront holds at once (four a lane), so
+// that a group's largest values meet in registers and nothing is read twice.
+// The root is kept and not v itself, since its values span half as many
+// octaves: the smallest value above 0 is 2^-18 of a group's largest root, of v
+// 2^-36.  Rounding is by chance: to nearest, a change below half a step would be lost
+// every time, and with b2 = 0.999 v changes by a thousandth a step, where
+// e4m3's steps are a sixteenth and an eighth.  The chance is a hash of seed,
+// step, tensor and element, as the sampler's draws are, so a step is
+// reproducible bit for bit.
+#include <cmath>
+
+#include "internal.h"
+#include "row_dev.h"
+#include "sampler_dev.h"
+
+namespace gnn {
+
+namespace {
+
+using samp::mix64;
+
+constexpr int kThreads = 256;
+constexpr int kGroup = GNN_ADAMW_GROUP;  // elements that share a scale: four to each lane of a wavefront
+static_assert(kGroup == 256, "a wavefront holds a group, four elements a lane");
+constexpr int kGroups = 4;               // groups of a wavefront
+constexpr int64_t kChunk = (kThreads / 64) * kGroups * kGroup;
+constexpr int kMost = 48;                // tensors of a launch: their records fit the 4 KB of its arguments
+constexpr float kTop = 448.f;            // the largest e4m3 value, 0x7e
+
+struct Record {
+    float *w;
+    const void *g;
+    void *m, *v;
+    float *m_scale, *v_scale;
+    uint16_t *shadow;
+    int64_t n;
+    float decay;
+    uint32_t begin;  // the tensor's first chunk in the launch; bit 31: g is bf16
+};
+
+struct Args {
+    Record r[kMost];
+    int count;
+    int base;        // number of r[0] in the call
+    float b1, nb1, b2, nb2, eps;
+    float c1, c2;    // lr / (1 - b1^t), 1 / sqrt(1 - b2^t)
+    float lr;
+    uint64_t key;    // mix(mix(seed) ^ t), or mix(seed) with the step on the device
+    double beta1, beta2;
+    const float *lr_dev;
+    const int64_t *step_dev;
+};
+static_assert(sizeof(Args) <= 4096, "kernel arguments");
+
+// What goes by the learning rate and the step.
+struct Rates {
+    float lr, c1, c2;
+    uint64_t key;
+};
+__host__ __device__ inline double one_less_power(double beta, int64_t t) {
+    return beta > 0 ? -expm1(static_cast<double>(t) * log(beta)) : 1.0;
+}
+__device__ __forceinline__ Rates rates_of(const Args &a) {
+    Rates x{a.lr_dev ? *a.lr_dev : a.lr, a.c1, a.c2, a.key};
+    if (a.step_dev) {
+        const int64_t t = *a.step_dev;
+        x.c1 = static_cast<float>(1.0 / one_less_power(a.beta1, t));
+        x.c2 = static_cast<float>(1.0 / sqrt(one_less_power(a.beta2, t)));
+        x.key = mix64(a.key ^ static_cast<uint64_t>(t));
+    }
+    if (a.lr_dev || a.step_dev) x.c1 = a.step_dev ? x.lr * x.c1 : x.lr * a.c1;
+    return x;
+}
+
+// One element: m, v and w are replaced; the root of v is returned.
+__device__ __forceinline__ float move(const Args &a, const Rates &x, float keep, float g, float &m, float &v, float &w) {
+    m = fmaf(a.b1, m, a.nb1 * g);
+    v = fmaf(a.b2, v, a.nb2 * (g * g));
+    const float root = sqrtf(v);
+    w = fmaf(w, keep, -(x.c1 * (m / fmaf(root, x.c2, a.eps))));
+    return root;
+}
+
+// |x| times `inverse` as the magnitude of an e4m3 value: below 2^-6 whole steps of
+// 2^-9, above eight steps to an octave; `chance` of a step (in 2^-16) is added.
+__device__ __forceinline__ uint32_t code_of(float x, float inverse, uint32_t chance) {
+    const float t = fabsf(x) * inverse;
+    const int e = max(static_cast<int>(__float_as_uint(t) >> 23) - 130, -9);
+    const float u = (static_cast<float>(chance) + 0.5f) * 0x1p-16f;
+    const uint32_t q = static_cast<uint32_t>(ldexpf(t, -e) + u);
+    return min(static_cast<uint32_t>((e + 9) << 3) + q, 126u);
+}
+template <int B> __device__ __forceinline__ float value_of(uint32_t codes) {
+    return __builtin_amdgcn_cvt_f32_fp8(static_cast<int>(codes), B);
+}
+
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) x = max(x, static_cast<uint32_t>(__shfl_xor(static_cast<int>(x), o, 64)));
+    return x;
+}
+// The scale of a group from its largest magnitude's bits (a NaN's are above all others) and
+// its reciprocal.  Below fp32's normal range both are 0; a scale that is
+// not finite makes what it scales NaN.
+__device__ __forceinline__ float scale_of(uint32_t top, float *inverse) {
+    const float s = __uint_as_float(top) / kTop;
+    *inverse = s >= 0x1p-126f ? 1.f / s : 0.f;
+    return s < 0x1p-126f ? 0.f : s;
+}
+
+// Four elements from p, `room` of them there; the others are 0.
+template <class T> __device__ __forceinline__ void get4(const T *p, int64_t room, float (&x)[4]) {
+    if (room >= 4) {
+        row::Vec<T, 4> v;
+        v.load(p);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = v.get(e);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = e < room ? Elem<T>::load(p, e) : 0.f;
+    }
+}
+template <class T> __device__ __forceinline__ void put4(T *p, int64_t room, const float (&x)[4]) {
+    row::Vec<T, 4> v;
+    v.set(x);
+    v.store_upto(p, room);
+}
+struct __attribute__((packed, aligned(1))) Word {
+    uint32_t x;
+};
+__device__ __forceinline__ uint32_t get_codes(const uint8_t *p, int64_t room) {
+    if (room >= 4) return reinterpret_cast<const Word *>(p)->x;
+    uint32_t x = 0;
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+        if (e < room) x |= static_cast<uint32_t>(p[e]) << (8 * e);
+    return x;
+}
+__device__ __forceinline__ void put_codes(uint8_t *p, int64_t room, uint32_t x) {
+    if (room >= 4) {
+        reinterpret_cast<Word *>(p)->x = x;
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+        if (e < room) p[e] = static_cast<uint8_t>(x >> (8 * e));
+}
+
+// Groups [first, first + kGroups) of tensor r, number `tensor` of the call.
+template <bool EIGHT, class TG>
+__device__ __forceinline__ void do_groups(const Args &a, const Rates &x, const Record &r, int tensor, int64_t first) {
+    const int lane = threadIdx.x & 63;
+    const float keep = 1.f - x.lr * r.decay;
+    float g[kGroups][4], w[kGroups][4], m[kGroups][4], v[kGroups][4];
+    uint32_t mc[kGroups], vc[kGroups];
+    float ms[kGroups], vs[kGroups];
+#pragma unroll
+    for (int k = 0; k < kGroups; ++k) {
+        const int64_t at = (first + k) * kGroup + lane * 4, room = r.n - at;
+        get4(static_cast<const TG *>(r.g) + at, room, g[k]);
+        get4(static_cast<const float *>(r.w) + at, room, w[k]);
+        if constexpr (EIGHT) {
+            mc[k] = get_codes(static_cast<const uint8_t *>(r.m) + at, room);
+            vc[k] = get_codes(static_cast<const uint8_t *>(r.v) + at, room);
+            const bool there = (first + k) * kGroup < r.n;
+            ms[k] = there ? r.m_scale[first + k] : 0.f;
+            vs[k] = there ? r.v_scale[first + k] : 0.f;
+        } else {
+            get4(static_cast<const float *>(r.m) + at, room, m[k]);
+            get4(static_cast<const float *>(r.v) + at, room, v[k]);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kGroups; ++k) {
+        const int64_t at = (first + k) * kGroup + lane * 4, room = r.n - at;
+        if ((first + k) * kGroup >= r.n) break;
+        if constexpr (EIGHT) {
+            const float mv[4] = {value_of<0>(mc[k]), value_of<1>(mc[k]), value_of<2>(mc[k]), value_of<3>(mc[k])};
+            const float rv[4] = {value_of<0>(vc[k]), value_of<1>(vc[k]), value_of<2>(vc[k]), value_of<3>(vc[k])};
+            float root[4];
+            uint32_t m_top = 0, r_top = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float old = rv[e] * vs[k];
+                m[k][e] = mv[e] * ms[k];
+                v[k][e] = old * old;
+                root[e] = move(a, x, keep, g[k][e], m[k][e], v[k][e], w[k][e]);
+                if (e < room) {
+                    m_top = max(m_top, __float_as_uint(m[k][e]) & 0x7fffffffu);
+                    r_top = max(r_top, __float_as_uint(root[e]) & 0x7fffffffu);
+                }
+            }
+            float m_inv, r_inv;
+            const float m_s = scale_of(wave_max(m_top), &m_inv), r_s = scale_of(wave_max(r_top), &r_inv);
+            uint32_t mo = 0, ro = 0;
+#pragma unroll
+            for (int e = 0; e < 4; e += 2) {
+                const uint64_t h = mix64(mix64(x.key ^ static_cast<uint64_t>(tensor)) ^ static_cast<uint64_t>((at + e) / 2));
+#pragma unroll
+                for (int o = 0; o < 2; ++o) {
+                    const float mm = m[k][e + o];
+                    const uint32_t c = static_cast<uint32_t>(h >> (32 * o));
+                    mo |= (code_of(mm, m_inv, c & 0xffffu) | (__float_as_uint(mm) >> 31 << 7)) << (8 * (e + o));
+                    ro |= code_of(root[e + o], r_inv, c >> 16) << (8 * (e + o));
+                }
+            }
+            put_codes(static_cast<uint8_t *>(r.m) + at, room, mo);
+            put_codes(static_cast<uint8_t *>(r.v) + at, room, ro);
+            if (lane == 0) {
+                r.m_scale[first + k] = m_s;
+                r.v_scale[first + k] = r_s;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) move(a, x, keep, g[k][e], m[k][e], v[k][e], w[k][e]);
+            put4(static_cast<float *>(r.m) + at, room, m[k]);
+            put4(static_cast<float *>(r.v) + at, room, v[k]);
+        }
+        put4(r.w + at, room, w[k]);
+        if (r.shadow) put4(r.shadow + at, room, w[k]);
+    }
+}
+
+template <bool EIGHT> __global__ void __launch_bounds__(kThreads) adamw_kernel(Args a) {
+    // the last record that begins at or before this workgroup's chunk
+    int lo = 0, hi = a.count - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if ((a.r[mid].begin & 0x7fffffffu) <= blockIdx.x) lo = mid;
+        else hi = mid - 1;
+    }
+    const Record &r = a.r[lo];
+    const int64_t first = (static_cast<int64_t>(blockIdx.x - (r.begin & 0x7fffffffu)) * (kThreads / 64) + (threadIdx.x >> 6)) * kGroups;
+    const Rates x = rates_of(a);
+    if (r.begin >> 31) do_groups<EIGHT, uint16_t>(a, x, r, a.base + lo, first);
+    else do_groups<EIGHT, float>(a, x, r, a.base + lo, first);
+}
+
+}  // namespace
+
+gnn_status launch_adamw(const gnn_adamw_tensor *t, int64_t count, int sdt, double lr, double beta1, double beta2, double eps,
+                        int64_t step, const float *lr_dev, const int64_t *step_dev, uint64_t seed, hipStream_t s) {
+    Args a{};
+    a.b1 = static_cast<float>(beta1);
+    a.nb1 = static_cast<float>(1.0 - beta1);
+    a.b2 = static_cast<float>(beta2);
+    a.nb2 = static_cast<float>(1.0 - beta2);
+    a.eps = static_cast<float>(eps);
+    a.lr = static_cast<float>(lr);
+    a.beta1 = beta1;
+    a.beta2 = beta2;
+    a.lr_dev = lr_dev;
+    a.step_dev = step_dev;
+    a.key = mix64(seed);
+    if (!step_dev) {
+        a.c1 = static_cast<float>((lr_dev ? 1.0 : lr) / one_less_power(beta1, step));
+        a.c2 = static_cast<float>(1.0 / std::sqrt(one_less_power(beta2, step)));
+        a.key = mix64(a.key ^ static_cast<uint64_t>(step));
+    }
+    int64_t chunks = 0;
+    auto launch = [&]() -> gnn_status {
+        if (a.count == 0) return GNN_OK;
+        if (sdt == GNN_F32) adamw_kernel<false><<<static_cast<unsigned>(chunks), kThreads, 0, s>>>(a);
+        else adamw_kernel<true><<<static_cast<unsigned>(chunks), kThreads, 0, s>>>(a);
+        GNN_LAUNCHED("adamw");
+        chunks = 0;
+        a.count = 0;
+        return GNN_OK;
+    };
+    for (int64_t i = 0; i < count; ++i) {
+        const int64_t need = ceil_div(t[i].n, kChunk);
+        // a launch's records are consecutive tensors
+        if (a.count == kMost || chunks + need > kMaxGrid / kThreads) GNN_TRY(launch());
+        if (a.count == 0) a.base = static_cast<int>(i);
+        a.r[a.count++] = Record{t[i].w, t[i].g, t[i].m, t[i].v, t[i].m_scale, t[i].v_scale, t[i].shadow, t[i].n,
+                                static_cast<float>(t[i].weight_decay),
+                                static_cast<uint32_t>(chunks) | (t[i].gdt == GNN_BF16 ? 0x80000000u : 0u)};
+        chunks += need;
+        // empty tensors alone make no grid
+        if (chunks == 0) a.count = 0;
+    }
+    return launch();
+}
+
+}  // namespace gnn

@@ -278,6 +278,15 @@ gnn_status launch_layer_norm_bwd(const void *g, int gdt, const void *x, int xdt,
                                  int64_t f, const float *gamma, const float *mean, const float *rstd,
                                  const void *d_res, void *d_x, float *dgamma, float *dbeta, void *ws, hipStream_t s);
 gnn_status launch_sgd(float *w, const float *dw, int64_t n, float lr, hipStream_t s);
+// The AdamW step over many tensors (adamw.hip).
+gnn_status launch_adamw(const gnn_adamw_tensor *t, int64_t count, int sdt, double lr, double beta1, double beta2, double eps,
+                        int64_t step, const float *lr_dev, const int64_t *step_dev, uint64_t seed, hipStream_t s);
+// Lookup of a trained table's rows and the table's gradient (embed.hip).
+gnn_status launch_embed_fwd(const void *table, int tdt, int64_t rows, int64_t dim, int64_t stride, const int64_t *ids,
+                            const int64_t *n_dev, int64_t cap, float scale, void *out, int odt, hipStream_t s);
+size_t embed_bwd_ws_bytes(int64_t cap, int64_t rows, int64_t dim);
+gnn_status launch_embed_bwd(const void *g, int gdt, const int64_t *ids, const int64_t *n_dev, int64_t cap, int64_t dim,
+                            float scale, int64_t rows, bool add, void *d_table, int ddt, void *ws, hipStream_t s);
 size_t sampler_ws_bytes(int64_t graph_n, int64_t cap_dst, int32_t fanout);
 gnn_status launch_sampler_ws_init(void *ws, int64_t graph_n, hipStream_t s);
 // Builds the block's CSR part (ids, row pointer, columns, norms).  With csc

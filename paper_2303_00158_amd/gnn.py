@@ -7,6 +7,7 @@ library has not been built the first call raises: there is no fallback path.
 """
 from __future__ import annotations
 
+import bisect
 import ctypes
 import os
 from typing import List, Optional, Sequence
@@ -18,16 +19,18 @@ LIB_PATH = os.path.join(_HERE, "libgnn.so")
 
 GNN_OK, GNN_EINVAL, GNN_ESIZE, GNN_EHIP, GNN_EUNSUPPORTED, GNN_EDEVICE = 0, -1, -2, -3, -4, -5
 GNN_DEVERR_WAIT, GNN_DEVERR_RANGE = 1, 2
-GNN_F32, GNN_BF16, GNN_F16 = 0, 1, 2
+GNN_F32, GNN_BF16, GNN_F16, GNN_F8E4M3 = 0, 1, 2, 3
 GNN_AGG_SAGE_MEAN, GNN_AGG_GCN_SYM, GNN_AGG_SAGE_MAX = 0, 1, 2
 GNN_LOC_DEVICE, GNN_LOC_HOST_PINNED = 0, 1
 GNN_ACT_NONE, GNN_ACT_RELU, GNN_ACT_GELU, GNN_ACT_GELU_TANH, GNN_ACT_SILU = 0, 1, 2, 3, 4
 GNN_MAX_LAYERS = 4
 GNN_MAX_DIM = 65536
 GNN_MAX_CLASSES, GNN_MAX_TOP = 1 << 20, 1024
+GNN_ADAMW_GROUP = 256
 
 _i64, _i32, _u64, _f32, _vp, _sz = (ctypes.c_int64, ctypes.c_int32, ctypes.c_uint64, ctypes.c_float,
                                     ctypes.c_void_p, ctypes.c_size_t)
+_f64 = ctypes.c_double
 
 
 class GnnError(RuntimeError):
@@ -50,6 +53,11 @@ class Model(ctypes.Structure):
                 ("dims", _i32 * (GNN_MAX_LAYERS + 1)), ("fanouts", _i32 * GNN_MAX_LAYERS),
                 ("w", _vp * GNN_MAX_LAYERS), ("b", _vp * GNN_MAX_LAYERS),
                 ("dw", _vp * GNN_MAX_LAYERS), ("db", _vp * GNN_MAX_LAYERS), ("wt", _vp * GNN_MAX_LAYERS)]
+
+
+class AdamwTensor(ctypes.Structure):
+    _fields_ = [("w", _vp), ("g", _vp), ("m", _vp), ("v", _vp), ("m_scale", _vp), ("v_scale", _vp), ("shadow", _vp),
+                ("n", _i64), ("weight_decay", _f64), ("gdt", _i32)]
 
 
 _ML = GNN_MAX_LAYERS
@@ -79,6 +87,9 @@ _SIGNATURES = {
     "gnn_sampler_workspace_init": (_i32, [_vp, _sz, _i64, _vp]),
     "gnn_build_block": (_i32, [_P(Graph), _vp, _vp, _vp, _i32, _u64, _u64, _i32, _i32, _P(Block), _vp, _sz, _vp]),
     "gnn_gather_features": (_i32, [_vp, _i32, _i32, _i64, _i64, _i64, _vp, _vp, _i64, _vp, _i32, _vp]),
+    "gnn_embed_fwd": (_i32, [_vp, _i32, _i64, _i64, _i64, _vp, _vp, _i64, _f32, _vp, _i32, _vp]),
+    "gnn_embed_bwd_workspace_size": (_i32, [_i64, _i64, _i64, _P(_sz)]),
+    "gnn_embed_bwd": (_i32, [_vp, _i32, _vp, _vp, _i64, _i64, _f32, _i64, _i32, _vp, _i32, _vp, _sz, _vp]),
     "gnn_aggregate_fwd": (_i32, [_P(Block), _i32, _vp, _i32, _i64, _vp, _i32, _vp]),
     "gnn_aggregate_fwd_dedup": (_i32, [_P(Block), _i32, _vp, _i32, _i64, _vp, _i32, _vp]),
     "gnn_aggregate_bwd": (_i32, [_P(Block), _i32, _vp, _i64, _vp, _i32, _vp, _vp]),
@@ -117,6 +128,7 @@ _SIGNATURES = {
     "gnn_layer_norm_bwd": (_i32, [_vp, _i32, _vp, _i32, _vp, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz,
                                   _vp]),
     "gnn_sgd": (_i32, [_vp, _vp, _i64, _f32, _vp]),
+    "gnn_adamw": (_i32, [_P(AdamwTensor), _i64, _i32, _f64, _f64, _f64, _f64, _i64, _vp, _vp, _u64, _vp]),
     "gnn_model_sync_shadow": (_i32, [_P(Model), _vp]),
     "gnn_train_step_layout": (_i32, [_P(Model), _i64, _i64, _P(StepLayout)]),
     "gnn_train_step_workspace_size": (_i32, [_P(Model), _i64, _i64, _P(_sz)]),
@@ -753,6 +765,155 @@ def distill_topk(logits: torch.Tensor, t_val: torch.Tensor, t_idx: torch.Tensor,
              _ptr(row_scale), _ptr(g_out), dtype_code(g_out.dtype) if g_out is not None else GNN_F32, _ptr(row_loss),
              _ptr(loss_out), _ptr(ws), ws.numel())
     return loss_out, g_out
+
+
+# ---------------------------------------------------------------------------
+# a trained table, and the optimizer's step
+# ---------------------------------------------------------------------------
+
+def embed_fwd(table: torch.Tensor, ids: torch.Tensor, out: torch.Tensor, scale: float = 1.0,
+              n_ids_dev: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """gnn_embed_fwd: out_i = scale table[ids_i], 0 where ids_i is outside the
+    table.  The table's rows may lie apart (any stride(0) >= dim); n_ids_dev
+    (int64, one value): how many ids there are, all of them when None."""
+    dev = table.device
+    if table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1):
+        raise ValueError(f"table: shape {tuple(table.shape)}, strides {table.stride()}, expected a matrix of dense rows")
+    rows, dim = table.shape
+    stride = table.stride(0) if rows > 1 else dim
+    if stride < dim:
+        raise ValueError(f"table: strides {table.stride()}, expected rows that do not overlap")
+    if table.dtype not in _ACTIVATIONS or not table.is_cuda:
+        raise ValueError(f"table: {table.dtype} on {dev}, expected fp32 or bf16 on a GPU")
+    _want("ids", ids, (None,), _INT64, dev)
+    _want("out", out, (ids.numel(), dim), _ACTIVATIONS, dev)
+    _want("n_ids_dev", n_ids_dev, (1,), _INT64, dev)
+    _enqueue(lib().gnn_embed_fwd, dev, stream, _ptr(table), dtype_code(table.dtype), rows, dim, stride, _ptr(ids),
+             _ptr(n_ids_dev), ids.numel(), float(scale), _ptr(out), dtype_code(out.dtype))
+    return out
+
+
+def embed_bwd_workspace(cap_ids: int, n_rows: int, dim: int, device, stream=None) -> torch.Tensor:
+    """A workspace for gnn_embed_bwd with these sizes."""
+    nb = _sz()
+    _check(lib().gnn_embed_bwd_workspace_size(cap_ids, n_rows, dim, ctypes.byref(nb)))
+    return _scratch(nb.value, device, stream)
+
+
+def embed_bwd(g: torch.Tensor, ids: torch.Tensor, d_table: torch.Tensor, scale: float = 1.0, accumulate: bool = False,
+              n_ids_dev: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """gnn_embed_bwd: the gradient of embed_fwd's table from g = dLoss/dout, in
+    place of what d_table held (rows that no id names are 0) or, with
+    accumulate, added to it (rows that no id names are not touched).  ws:
+    workspace (allocated when None)."""
+    n_rows, dim = _matrix("d_table", d_table)
+    dev = d_table.device
+    _want("ids", ids, (None,), _INT64, dev)
+    n = ids.numel()
+    _want("g", g, (n, dim), _ACTIVATIONS, dev)
+    _want("n_ids_dev", n_ids_dev, (1,), _INT64, dev)
+    if ws is None:
+        ws = embed_bwd_workspace(n, n_rows, dim, dev, stream)
+    _want("ws", ws, (None,), (torch.uint8,), dev)
+    _enqueue(lib().gnn_embed_bwd, dev, stream, _ptr(g), dtype_code(g.dtype), _ptr(ids), _ptr(n_ids_dev), n, dim,
+             float(scale), n_rows, int(accumulate), _ptr(d_table), dtype_code(d_table.dtype), _ptr(ws), ws.numel())
+    return d_table
+
+
+class AdamW:
+    """AdamW over the tensors of a model (gnn_adamw): step() moves every tensor
+    of ``params`` by its gradient in ``grads`` (the same buffers at every step).
+
+    params        fp32 tensors, any shapes, dense.
+    grads         a gradient for each, fp32 or bf16.
+    weight_decay  one number, or one for each tensor.
+    state_dtype   torch.float32, or torch.float8_e4m3fn: m and sqrt(v) in 8
+                  bits with a scale for each GNN_ADAMW_GROUP elements.
+    m, v, m_scale, v_scale  the states (lists; zeros when None).
+    shadows       bf16 tensors (or None) that each step writes with the new
+                  values, as the bf16 products read them.
+    seed          of the 8-bit states' rounding.
+
+    A step of the same inputs, seed and step number is reproducible bit for
+    bit.  ``steps`` counts the steps that step() counted by itself."""
+
+    def __init__(self, params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], weight_decay=0.0,
+                 betas=(0.9, 0.999), eps: float = 1e-8, state_dtype: torch.dtype = torch.float32, m=None, v=None,
+                 m_scale=None, v_scale=None, shadows=None, seed: int = 0):
+        params, grads = list(params), list(grads)
+        if not params:
+            raise ValueError("params: none given")
+        if state_dtype not in (torch.float32, torch.float8_e4m3fn):
+            raise ValueError(f"state_dtype: {state_dtype}, expected torch.float32 or torch.float8_e4m3fn")
+        eight = state_dtype == torch.float8_e4m3fn
+        self.device, n = params[0].device, len(params)
+        if not eight and (m_scale is not None or v_scale is not None):
+            raise ValueError("m_scale, v_scale: given for fp32 states")
+
+        def each(name, given, make):
+            given = [make(p) for p in params] if given is None else list(given)
+            if len(given) != n:
+                raise ValueError(f"{name}: {len(given)} given for {n} tensors")
+            return given
+
+        def zeros(p):
+            return torch.zeros(p.shape, dtype=torch.uint8, device=p.device).view(state_dtype) if eight else torch.zeros_like(p)
+
+        def groups(p):
+            return torch.zeros(-(-p.numel() // GNN_ADAMW_GROUP), dtype=torch.float32, device=p.device)
+        self.params, self.grads = params, each("grads", grads, None)
+        self.m, self.v = each("m", m, zeros), each("v", v, zeros)
+        self.m_scale = each("m_scale", m_scale, groups) if eight else [None] * n
+        self.v_scale = each("v_scale", v_scale, groups) if eight else [None] * n
+        self.shadows = each("shadows", shadows, lambda p: None)
+        decay = [float(weight_decay)] * n if isinstance(weight_decay, (int, float)) else [float(x) for x in weight_decay]
+        if len(decay) != n:
+            raise ValueError(f"weight_decay: {len(decay)} given for {n} tensors")
+        self.betas, self.eps, self.seed, self.steps = (float(betas[0]), float(betas[1])), float(eps), int(seed), 0
+        self.state_dtype = state_dtype
+        written, read = [], []
+        self._c = (AdamwTensor * n)()
+        for i, p in enumerate(params):
+            shape, scales = p.shape, (-(-p.numel() // GNN_ADAMW_GROUP),)
+            for name, t, want, types in ((f"params[{i}]", p, shape, _FP32), (f"grads[{i}]", self.grads[i], shape, _ACTIVATIONS),
+                                         (f"m[{i}]", self.m[i], shape, (state_dtype,)),
+                                         (f"v[{i}]", self.v[i], shape, (state_dtype,)),
+                                         (f"m_scale[{i}]", self.m_scale[i], scales, _FP32),
+                                         (f"v_scale[{i}]", self.v_scale[i], scales, _FP32),
+                                         (f"shadows[{i}]", self.shadows[i], shape, (torch.bfloat16,))):
+                _want(name, t, want, types, self.device)
+                if t is not None and t.numel():
+                    span = (t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), name)
+                    (read if name.startswith("grads") else written).append(span)
+            self._c[i] = AdamwTensor(_ptr(p), _ptr(self.grads[i]), _ptr(self.m[i]), _ptr(self.v[i]), _ptr(self.m_scale[i]),
+                                     _ptr(self.v_scale[i]), _ptr(self.shadows[i]), p.numel(), decay[i],
+                                     dtype_code(self.grads[i].dtype))
+        # what one tensor's step writes is no other's (gradients may be shared)
+        written.sort()
+        for a, b in zip(written, written[1:]):
+            if b[0] < a[1]:
+                raise ValueError(f"{a[2]} and {b[2]} overlap")
+        starts = [a[0] for a in written]
+        for a in read:
+            at = bisect.bisect_right(starts, a[0]) - 1
+            if (at >= 0 and written[at][1] > a[0]) or (at + 1 < len(written) and starts[at + 1] < a[1]):
+                raise ValueError(f"{a[2]} overlaps what the step writes")
+
+    def step(self, lr: float = 0.0, step: Optional[int] = None, lr_dev: Optional[torch.Tensor] = None,
+             step_dev: Optional[torch.Tensor] = None, stream=None) -> None:
+        """Enqueue one step.  step: its number (the first is 1; counted here
+        when None).  lr_dev (fp32) and step_dev (int64), one value each on the
+        GPU, are read in place of lr and step: what a captured step goes by
+        when it is replayed."""
+        _want("lr_dev", lr_dev, (1,), _FP32, self.device)
+        _want("step_dev", step_dev, (1,), _INT64, self.device)
+        count = step is None and step_dev is None
+        number = self.steps + 1 if count else (0 if step is None else int(step))
+        _enqueue(lib().gnn_adamw, self.device, stream, self._c, len(self.params),
+                 GNN_F32 if self.state_dtype == torch.float32 else GNN_F8E4M3, float(lr), *self.betas, self.eps, number,
+                 _ptr(lr_dev), _ptr(step_dev), self.seed & 0xFFFFFFFFFFFFFFFF)
+        if count:
+            self.steps = number
 
 
 # ---------------------------------------------------------------------------

@@ -1,0 +1,425 @@
+"""The AdamW step over many tensors, states in fp32 and in 8 bits, against the
+formulas in 64 bits."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+from paper_2303_00158_amd import gnn
+
+DEV = "cuda:0"
+F32, BF16, E4M3 = torch.float32, torch.bfloat16, torch.float8_e4m3fn
+U = 2.0 ** -24  # half a step of fp32, relative
+GROUP, TOP = gnn.GNN_ADAMW_GROUP, 448.0
+LR, B1, B2, EPS = 1e-2, 0.9, 0.99, 1e-8
+
+
+def f32(x):
+    return torch.tensor(x, dtype=F32).double().item()
+
+
+def mix(x):
+    x = ((x ^ (x >> 30)) * 0xBF58476D1CE4E5B9) % 2 ** 64
+    x = ((x ^ (x >> 27)) * 0x94D049BB133111EB) % 2 ** 64
+    return x ^ (x >> 31)
+
+
+def mix_of(x):
+    """mix of int64 values"""
+    def signed(c):
+        return c - 2 ** 64 if c >> 63 else c
+    x = (x ^ ((x >> 30) & (2 ** 34 - 1))) * signed(0xBF58476D1CE4E5B9)
+    x = (x ^ ((x >> 27) & (2 ** 37 - 1))) * signed(0x94D049BB133111EB)
+    return x ^ ((x >> 31) & (2 ** 33 - 1))
+
+
+def chances(n, tensor, seed, t):
+    """(for m, for r) of each element"""
+    key = mix(mix(mix(seed) ^ t) ^ tensor)
+    e = torch.arange(n, device=DEV)
+    h = mix_of((e // 2) ^ (key - 2 ** 64 if key >> 63 else key))
+    at = 32 * (e % 2)
+    return [(((h >> (at + o)) & 0xffff).double() + 0.5) / 65536 for o in (0, 16)]
+
+
+def decode(codes, scale):
+    n = codes.numel()
+    return codes.float().double().reshape(-1) * scale.double().repeat_interleave(GROUP)[:n]
+
+
+def exact(w, g, m, v, t, decay, lr=LR, betas=(B1, B2), eps=EPS):
+    """New w, m and v in 64 bits, and how far fp32 may be off."""
+    w, g, m, v = (x.double().reshape(-1) for x in (w, g, m, v))
+    b1, b2 = betas
+    m2, v2 = b1 * m + (1 - b1) * g, b2 * v + (1 - b2) * g * g
+    # factors rounded, products and sums rounded
+    off_m = 4 * U * ((b1 * m).abs() + ((1 - b1) * g).abs())
+    off_v = 5 * U * v2
+    c1, c2 = lr / (1 - b1 ** t), 1 / math.sqrt(1 - b2 ** t)
+    den = v2.sqrt() * c2 + eps
+    moved = c1 * m2 / den
+    # half of v's relative error; root, its factor, eps, denominator, quotient, c1, product
+    off_moved = c1 * off_m / den + moved.abs() * 12 * U
+    kept = w * (1 - lr * decay)
+    off_w = off_moved + kept.abs() * 4 * U + 2 * U * (kept - moved).abs()
+    return (kept - moved, m2, v2), (off_w * 1.01 + 1e-37, off_m * 1.01 + 1e-37, off_v * 1.01 + 1e-37)
+
+
+def within(got, want, bound, what):
+    off = (got.double().reshape(-1) - want).abs()
+    bad = ~(off <= bound)
+    assert not bad.any(), f"{what}: {int(bad.sum())} of {bad.numel()} off, most {float((off / bound).max()):.3g} times the bound"
+
+
+def rand(gen, *shape, dtype=F32, scale=1.0):
+    return (torch.randn(shape, generator=gen) * scale).to(dtype).to(DEV)
+
+
+def misaligned(t, off):
+    buf = torch.empty(t.numel() + 64, dtype=torch.uint8, device=t.device).view(t.dtype) if t.element_size() == 1 else \
+        torch.empty(t.numel() + 64, dtype=t.dtype, device=t.device)
+    v = buf[off:off + t.numel()].view(t.shape)
+    v.copy_(t)
+    return v
+
+
+SHAPES = [(1,), (3,), (4,), (5,), (255,), (256,), (257,), (511,), (1023, 1), (33, 31), (4095,), (4096,), (4097,), (8192,), (200, 256), (47,),
+          (16_385,), (100_003,)]
+
+
+def model(gen, shapes, gdts, off=0):
+    params = [misaligned(rand(gen, *s), (off + i) % 4 if off else 0) for i, s in enumerate(shapes)]
+    # sizes of gradients differ by orders of magnitude
+    grads = [misaligned((rand(gen, *s) * torch.exp(2 * rand(gen, *s))).to(gdts[i % len(gdts)]), (off + 2 * i) % 5 if off else 0)
+             for i, s in enumerate(shapes)]
+    return params, grads
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("gdts", [(F32,), (BF16,), (F32, BF16)])
+@pytest.mark.parametrize("off", [0, 1])
+def test_steps_with_fp32_states(gdts, off):
+    gen = torch.Generator().manual_seed(off)
+    params, grads = model(gen, SHAPES, gdts, off)
+    decays = [0.1 * (i % 3) for i in range(len(params))]
+    shadows = [misaligned(torch.zeros(s, dtype=BF16, device=DEV), off) if i % 2 else None for i, s in enumerate(SHAPES)]
+    opt = gnn.AdamW(params, grads, decays, (B1, B2), EPS, shadows=shadows,
+                    m=[misaligned(torch.zeros(s, device=DEV), off) for s in SHAPES])
+    for t in range(1, 5):
+        before = [[x.clone() for x in xs] for xs in (params, opt.m, opt.v)]
+        opt.step(LR)
+        assert opt.steps == t
+        for i, g in enumerate(grads):
+            w, m, v = (b[i] for b in before)
+            want, bound = exact(w, g, m, v, t, decays[i])
+            for got, x, b, what in zip((params[i], opt.m[i], opt.v[i]), want, bound, "wmv"):
+                within(got, x, b, f"{what} of tensor {i}, step {t}")
+            if shadows[i] is not None:
+                assert torch.equal(shadows[i], params[i].to(BF16))
+        for g in grads:
+            g.mul_(-0.7)
+
+
+def check_8bit(x, codes, scale, chance, what):
+    """x: what was to be stored, in 64 bits, each group's largest at 448."""
+    n = x.numel()
+    groups = -(-n // GROUP)
+    pad = torch.zeros(groups * GROUP, dtype=torch.float64, device=DEV)
+    pad[:n] = x.abs()
+    top = pad.view(groups, GROUP).amax(1)
+    assert ((scale.double() - top / TOP).abs() <= 12 * U * top / TOP).all(), what
+    y = x.abs() / scale.double().repeat_interleave(GROUP)[:n]
+    step = torch.exp2(torch.floor(torch.log2(y.clamp(min=2.0 ** -6))) - 3)
+    got = codes.float().double().reshape(-1)
+    assert (torch.signbit(got) == torch.signbit(x))[x.abs() > 12 * U * scale.double().repeat_interleave(GROUP)[:n]].all(), what
+    # one of the two neighbours: fp32's own errors are a few U of up to 16 steps
+    assert ((got.abs() - y).abs() <= step * (1 + 2.0 ** -15)).all(), what
+    # and the one that chance says, unless it was that close
+    q = y / step + chance
+    want = (torch.floor(q) * step).clamp(max=TOP)
+    near = (q - torch.round(q)).abs() <= 2.0 ** -15
+    assert (got.abs() == want)[~near].all(), what
+    assert near.double().mean() <= 2.0 ** -13 or n < 100_000, what
+    return (got.abs() - y) / step
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("gdt", [F32, BF16])
+@pytest.mark.parametrize("off", [0, 1])
+def test_steps_with_8bit_states(gdt, off):
+    gen = torch.Generator().manual_seed(10 + off)
+    params, grads = model(gen, SHAPES, (gdt,), off)
+    # a state's own sign and size decide; gradients that nearly cancel it lose digits, so both have one sign here
+    grads = [g.abs_() for g in grads]
+    seed = 99
+    opt = gnn.AdamW(params, grads, 0.1, (B1, B2), EPS, state_dtype=E4M3, seed=seed,
+                    m=[misaligned(torch.zeros(s, dtype=torch.uint8, device=DEV), off).view(E4M3) for s in SHAPES],
+                    shadows=[torch.zeros(s, dtype=BF16, device=DEV) for s in SHAPES])
+    for t in range(1, 5):
+        w0 = [p.clone() for p in params]
+        m0 = [decode(a, b) for a, b in zip(opt.m, opt.m_scale)]
+        r0 = [decode(a, b) for a, b in zip(opt.v, opt.v_scale)]
+        opt.step(LR)
+        for i, g in enumerate(grads):
+            (w, m, v), (bw, _, _) = exact(w0[i], g, m0[i], r0[i] ** 2, t, 0.1)
+            within(params[i], w, bw + 8 * U * (w - w0[i].double().reshape(-1)).abs(), f"w of tensor {i}, step {t}")
+            assert torch.equal(opt.shadows[i], params[i].to(BF16))
+            cm, cr = chances(g.numel(), i, seed, t)
+            parts = [check_8bit(m, opt.m[i], opt.m_scale[i], cm, f"m of tensor {i}, step {t}"),
+                     check_8bit(v.sqrt(), opt.v[i], opt.v_scale[i], cr, f"r of tensor {i}, step {t}")]
+            if g.numel() > 50_000:
+                # a rounding by chance is off by less than a step, none on average: 6 of the mean's deviations of at most 1/2
+                for p in parts:
+                    assert abs(float(p.mean())) <= 6 * 0.5 / math.sqrt(p.numel())
+        for g in grads:
+            g.mul_(0.6)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("sdt", [F32, E4M3])
+@pytest.mark.parametrize("count", [47, 48, 49, 96, 145])
+def test_many_tensors(count, sdt):
+    """More tensors than one launch takes, empty ones among them: each moves
+    as it does alone."""
+    gen = torch.Generator().manual_seed(count)
+    shapes = [((i * 37) % 300 if i % 5 else 0,) for i in range(count)]
+    params, grads = model(gen, shapes, (F32, BF16))
+    # alone, a tensor's number is another, which the 8-bit rounding goes by: the first step's w does not depend on it
+    apart = [p.clone() for p in params]
+    opt = gnn.AdamW(params, grads, 0.05, (B1, B2), EPS, state_dtype=sdt, seed=3)
+    opt.step(LR)
+    for i in range(count):
+        one = gnn.AdamW([apart[i]], [grads[i]], 0.05, (B1, B2), EPS, state_dtype=sdt)
+        one.step(LR)
+        assert torch.equal(apart[i], params[i]), i
+        if sdt == F32:
+            assert torch.equal(one.m[0], opt.m[i]) and torch.equal(one.v[0], opt.v[i]), i
+        elif shapes[i][0]:
+            assert torch.equal(one.m_scale[0], opt.m_scale[i]) and torch.equal(one.v_scale[0], opt.v_scale[i]), i
+            cm, _ = chances(shapes[i][0], i, 3, 1)
+            check_8bit(0.1 * grads[i].double(), opt.m[i], opt.m_scale[i], cm, f"m of tensor {i}")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("sdt", [F32, E4M3])
+def test_the_same_bits_at_any_alignment_and_again(sdt):
+    gen = torch.Generator().manual_seed(4)
+    base, grads = model(gen, [(70_001,)], (BF16,))
+    runs = []
+    for off in (0, 0, 1, 3):
+        p, g = misaligned(base[0], off), misaligned(grads[0], off)
+        opt = gnn.AdamW([p], [g], 0.01, (B1, B2), EPS, state_dtype=sdt, seed=7)
+        for _ in range(3):
+            opt.step(LR)
+        runs.append((p, opt.m[0].view(torch.uint8), opt.v[0].view(torch.uint8)))
+    for r in runs[1:]:
+        assert all(torch.equal(x, y) for x, y in zip(r, runs[0]))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("sdt", [F32, E4M3])
+def test_a_captured_step_counts_on(sdt):
+    gen = torch.Generator().manual_seed(6)
+    shapes = [(300, 7), (4097,), (1,)]
+    made = [model(torch.Generator().manual_seed(6), shapes, (F32,)) for _ in range(2)]
+    opts = [gnn.AdamW(p, g, 0.1, (B1, B2), EPS, state_dtype=sdt, seed=1) for p, g in made]
+    lr, t = torch.tensor([LR], device=DEV), torch.tensor([1], device=DEV)
+    lr2, t2 = lr.clone(), t.clone()
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        opts[0].step(lr_dev=lr, step_dev=t)
+        t.add_(1)
+    for k in range(5):
+        for g, h in zip(made[0][1], made[1][1]):
+            x = rand(gen, *g.shape)
+            g.copy_(x)
+            h.copy_(x)
+        lr.fill_(LR / (k + 1))
+        lr2.fill_(LR / (k + 1))
+        graph.replay()
+        opts[1].step(lr_dev=lr2, step_dev=t2)
+        t2.add_(1)
+        torch.cuda.synchronize()
+        for a, b in zip(*(o.params for o in opts)):
+            assert torch.equal(a, b), k
+        for name in ("m", "v"):
+            for a, b in zip(*(getattr(o, name) for o in opts)):
+                assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)), (k, name)
+    assert int(t) == 6
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("given", ["lr", "step", "both"])
+def test_rates_on_the_device_are_those_of_the_host(given):
+    gen = torch.Generator().manual_seed(2)
+    made = [model(torch.Generator().manual_seed(2), [(5000,)], (F32,)) for _ in range(2)]
+    opts = [gnn.AdamW(p, g, 0.1, (B1, B2), EPS) for p, g in made]
+    for t in (1, 2, 3, 1000, 10 ** 9):
+        x = rand(gen, 5000)
+        for p, g in made:
+            g[0].copy_(x)
+        opts[0].step(LR, t)
+        opts[1].step(0.0 if given != "step" else LR, None if given != "lr" else t,
+                     lr_dev=torch.tensor([LR], device=DEV) if given != "step" else None,
+                     step_dev=torch.tensor([t], device=DEV) if given != "lr" else None)
+        # three factors are rounded on the way to c1 instead of one
+        w, w2 = made[0][0][0], made[1][0][0]
+        moved = LR / (1 - B1 ** t) * 40
+        assert float((w - w2).abs().max()) <= 8 * U * (moved + float(w.abs().max())), t
+        w2.copy_(w)
+    assert opts[1].steps == 0
+
+
+@pytest.mark.gpu
+def test_edges_of_the_rates():
+    """beta 0, eps and lr 0, zero gradients."""
+    w, g = torch.ones(1000, device=DEV), torch.linspace(-1, 1, 1000, device=DEV)
+    opt = gnn.AdamW([w], [g], 0.0, (0.0, 0.0), 0.0)
+    opt.step(0.5)
+    # a quotient of equal numbers: the gradient's sign (0 / 0 where it is 0)
+    assert ((w - (1 - 0.5 * torch.sign(g)))[g != 0].abs() <= 1e-6).all() and torch.equal(opt.m[0], g)
+    w.fill_(1.0)
+    opt = gnn.AdamW([w], [g], 0.5)
+    opt.step(0.0)
+    assert (w == 1).all()
+    zero = torch.zeros(1000, device=DEV)
+    for sdt in (F32, E4M3):
+        w.fill_(2.0)
+        opt = gnn.AdamW([w], [zero], 0.5, state_dtype=sdt)
+        for _ in range(3):
+            opt.step(0.25)
+        assert ((w - 2 * 0.875 ** 3).abs() <= 1e-6).all()
+        assert (opt.m[0].float() == 0).all() and (opt.v[0].float() == 0).all()
+
+
+@pytest.mark.gpu
+def test_values_that_are_not_finite():
+    for sdt in (F32, E4M3):
+        for bad in (math.nan, math.inf):
+            w, g = torch.ones(600, device=DEV), torch.full((600,), 0.5, device=DEV)
+            g[300] = bad
+            opt = gnn.AdamW([w], [g], state_dtype=sdt)
+            opt.step(0.1)
+            ok = torch.arange(600, device=DEV) != 300
+            assert w[300].isnan() and ((w[ok] - 0.9).abs() < 1e-6).all(), (sdt, bad)
+            m = opt.m[0].double() if sdt == F32 else decode(opt.m[0], opt.m_scale[0])
+            r = opt.v[0].double() if sdt == F32 else decode(opt.v[0], opt.v_scale[0])
+            if sdt == F32:
+                assert m[ok].isfinite().all() and r[ok].isfinite().all()
+            else:
+                # the second group of 256
+                mine = (torch.arange(600, device=DEV) // GROUP) == 1
+                assert not m[mine].isfinite().any() and m[~mine].isfinite().all()
+                assert not r[mine].isfinite().any() and r[~mine].isfinite().all()
+
+
+@pytest.mark.gpu
+def test_tiny_and_huge_groups_in_8_bits():
+    for size in (1e-44, 1e-39, 1e-37, 3e-36, 1e-30, 1.0, 1e18):
+        w, g = torch.ones(512, device=DEV), torch.full((512,), size, device=DEV)
+        g[256:] = 0
+        opt = gnn.AdamW([w], [g], betas=(0.5, 0.5), eps=0.0 if size > 1e-15 else 1e-8, state_dtype=E4M3)
+        opt.step(0.1)
+        m, r = decode(opt.m[0], opt.m_scale[0]), decode(opt.v[0], opt.v_scale[0])
+        assert (m[256:] == 0).all() and (r[256:] == 0).all() and opt.m_scale[0][1] == 0
+        if size / 2 >= 448 * 2.0 ** -126:
+            # a group of equal values: all of them 448
+            assert ((m[:256] - size / 2).abs() <= 4 * U * size).all(), size
+        else:
+            assert (m == 0).all() and opt.m_scale[0][0] == 0, size
+
+
+@pytest.mark.gpu
+def test_offsets_past_32_bits():
+    n = (1 << 32) + 257
+    w, g = torch.zeros(n, device=DEV), torch.zeros(n, dtype=BF16, device=DEV)
+    at = [0, 1 << 31, (1 << 32) - 1, 1 << 32, n - 1]
+    g[at] = 1.0
+    opt = gnn.AdamW([w], [g], state_dtype=E4M3)
+    opt.step(0.5)
+    assert int((w != 0).sum()) == len(at) and ((w[at] + 0.5).abs() < 1e-6).all()
+    assert (opt.m[0].view(torch.uint8)[at] == 0x7e).all()
+
+
+@pytest.mark.gpu
+def test_on_another_stream():
+    gen = torch.Generator().manual_seed(9)
+    p, g = model(gen, [(100_000,)], (F32,))
+    q = [p[0].clone()]
+    a, b = gnn.AdamW(p, g), gnn.AdamW(q, g)
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        a.step(LR)
+        b.step(LR, stream=stream)
+    torch.cuda.synchronize()
+    assert torch.equal(p[0], q[0])
+
+
+# --- refusals ---------------------------------------------------------------
+
+BUF = ctypes.create_string_buffer(1 << 16)
+P = (ctypes.addressof(BUF) + 255) // 256 * 256  # any address: a refused call reads nothing
+
+
+@pytest.mark.parametrize("change, code, what", [
+    (dict(sdt=1), gnn.GNN_EUNSUPPORTED, "states"), (dict(count=-1), gnn.GNN_EINVAL, "tensors"),
+    (dict(tensors=None), gnn.GNN_EINVAL, "tensors"), (dict(b1=1.0), gnn.GNN_EINVAL, "beta"),
+    (dict(b2=-0.1), gnn.GNN_EINVAL, "beta"), (dict(b2=math.nan), gnn.GNN_EINVAL, "beta"),
+    (dict(lr=-1.0), gnn.GNN_EINVAL, "lr"), (dict(lr=math.inf), gnn.GNN_EINVAL, "lr"),
+    (dict(eps=-1e-9), gnn.GNN_EINVAL, "eps"), (dict(eps=math.nan), gnn.GNN_EINVAL, "eps"),
+    (dict(step=0), gnn.GNN_EINVAL, "step"), (dict(lr_dev=P + 2), gnn.GNN_EINVAL, "misaligned"),
+    (dict(step_dev=P + 4), gnn.GNN_EINVAL, "misaligned"),
+    (dict(t=dict(gdt=2)), gnn.GNN_EUNSUPPORTED, "gdt"), (dict(t=dict(n=-1)), gnn.GNN_EINVAL, "n out"),
+    (dict(t=dict(n=1 << 34)), gnn.GNN_EINVAL, "n out"), (dict(t=dict(weight_decay=-0.1)), gnn.GNN_EINVAL, "decay"),
+    (dict(t=dict(weight_decay=math.nan)), gnn.GNN_EINVAL, "decay"), (dict(t=dict(w=None)), gnn.GNN_EINVAL, "NULL"),
+    (dict(t=dict(g=None)), gnn.GNN_EINVAL, "NULL"), (dict(t=dict(m=None)), gnn.GNN_EINVAL, "NULL"),
+    (dict(t=dict(v=None)), gnn.GNN_EINVAL, "NULL"), (dict(sdt=3, t=dict(m_scale=None)), gnn.GNN_EINVAL, "NULL"),
+    (dict(t=dict(w=P + 2)), gnn.GNN_EINVAL, "misaligned"), (dict(t=dict(g=P + 1)), gnn.GNN_EINVAL, "misaligned"),
+    (dict(t=dict(m=P + 1)), gnn.GNN_EINVAL, "misaligned"), (dict(t=dict(shadow=P + 1)), gnn.GNN_EINVAL, "misaligned"),
+    (dict(sdt=3, t=dict(v_scale=P + 2)), gnn.GNN_EINVAL, "misaligned"),
+])
+def test_refusals(change, code, what):
+    t = dict(w=P, g=P + 1024, m=P + 2048, v=P + 3072, m_scale=P + 4096, v_scale=P + 4160, shadow=None, n=10, weight_decay=0.0,
+             gdt=0) | change.pop("t", {})
+    tensors = (gnn.AdamwTensor * 2)(gnn.AdamwTensor(n=0), gnn.AdamwTensor(*t.values()))
+    a = dict(tensors=tensors, count=2, sdt=0, lr=0.1, b1=0.9, b2=0.99, eps=1e-8, step=1, lr_dev=None, step_dev=None, seed=0) | change
+    got = gnn.lib().gnn_adamw(*a.values(), None)
+    assert got == code and what in gnn.lib().gnn_last_error().decode()
+
+
+def test_nothing_to_do_is_no_error():
+    assert gnn.lib().gnn_adamw(None, 0, 0, 0.1, 0.9, 0.99, 1e-8, 1, None, None, 0, None) == gnn.GNN_OK
+    empty = (gnn.AdamwTensor * 60)(*(gnn.AdamwTensor(n=0) for _ in range(60)))
+    assert gnn.lib().gnn_adamw(empty, 60, 3, 0.1, 0.9, 0.99, 1e-8, 1, None, None, 0, None) == gnn.GNN_OK
+
+
+def test_the_binding_refuses_what_is_not_on_a_gpu():
+    with pytest.raises(ValueError, match="GPU"):
+        gnn.AdamW([torch.zeros(4)], [torch.zeros(4)])
+    with pytest.raises(ValueError, match="none given"):
+        gnn.AdamW([], [])
+
+
+@pytest.mark.gpu
+def test_the_binding_refuses_wrong_tensors():
+    w, g = torch.zeros(512, device=DEV), torch.zeros(512, device=DEV)
+    for args, kw in (([w], [g[:4]]), {}), (([w], [g.half()]), {}), (([w.bfloat16()], [g]), {}), (([w], [g, g]), {}), \
+            (([w, w], [g, g]), {}), (([w, w[5:]], [g, g[5:]]), {}), (([w], [w]), {}), (([w], [w[::2]]), {}), \
+            (([w], [g], [0.1, 0.2]), {}), (([w], [g]), dict(m=[g], v=[g])), (([w], [g]), dict(state_dtype=BF16)), \
+            (([w], [g]), dict(m_scale=[g[:2]])), (([w], [g]), dict(state_dtype=E4M3, m=[g])), \
+            (([w], [g]), dict(state_dtype=E4M3, m_scale=[g[:1]])), (([w], [g]), dict(shadows=[g])):
+        with pytest.raises(ValueError):
+            gnn.AdamW(*args, **kw)
+    # one gradient may serve two tensors
+    gnn.AdamW([w, torch.zeros_like(w)], [g, g]).step(0.1)
+    opt = gnn.AdamW([w], [g])
+    with pytest.raises(ValueError):
+        opt.step(0.1, lr_dev=g[:2])
+    with pytest.raises(ValueError):
+        opt.step(0.1, step_dev=g[:1])
+    with pytest.raises(gnn.GnnError, match="step"):
+        opt.step(0.1, 0)
+    assert opt.steps == 0

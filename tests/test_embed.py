@@ -1,0 +1,360 @@
+"""Lookup of a trained table's rows and the table's gradient."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+from paper_2303_00158_amd import gnn
+
+DEV = "cuda:0"
+F32, BF16 = torch.float32, torch.bfloat16
+U = 2.0 ** -24  # half a step of fp32, relative
+
+
+def half_step(dt):
+    return torch.finfo(dt).eps / 2
+
+
+def rand(gen, *shape, dtype=F32, scale=1.0):
+    return (torch.randn(shape, generator=gen) * scale).to(dtype).to(DEV)
+
+
+def misaligned(t, off):
+    """t's values at an address `off` elements past an aligned one."""
+    buf = torch.empty(t.numel() + 64, dtype=t.dtype, device=t.device)
+    v = buf[off:off + t.numel()].view(t.shape)
+    v.copy_(t)
+    return v
+
+
+def make_ids(gen, law, n, rows):
+    if law == "same":
+        return torch.full((n,), rows // 2, device=DEV)
+    if law == "absent":
+        return torch.full((n,), -1, device=DEV)
+    if law == "last":  # the largest valid id, and the first one past it
+        return torch.tensor([rows - 1, rows], device=DEV).repeat(n)[:n]
+    if law == "distinct":
+        return torch.randperm(max(rows, n), generator=gen)[:n].to(DEV)  # ids past the table among them
+    if law == "sorted":
+        return torch.sort(torch.randint(0, rows, (n,), generator=gen))[0].to(DEV)
+    ids = (rows ** torch.rand(n, generator=gen).double()).long() - 1
+    ids = ids.clamp(0, rows - 1)
+    ids[torch.rand(n, generator=gen) < 0.06] = torch.tensor([-1, rows, 2 ** 62, -2 ** 63])[n % 4]
+    return ids.to(DEV)
+
+
+def lookup(table, ids, scale, odt):
+    there = (ids >= 0) & (ids < table.shape[0])
+    rows = table[torch.where(there, ids, 0)].float() * torch.tensor(scale, dtype=F32).item()
+    return torch.where(there[:, None], rows, 0.0).to(odt)
+
+
+def gradient64(g, ids, rows, scale, before):
+    """The gradient, and how far fp32 sums of its terms may be off: each of
+    n terms passes through at most n additions, the scale and what was there
+    before through one rounding each."""
+    there = torch.nonzero((ids >= 0) & (ids < rows))[:, 0]
+    scale = torch.tensor(scale, dtype=F32).double().item()
+    sums = torch.zeros((rows, g.shape[1]), dtype=torch.float64, device=DEV)
+    sizes, count = torch.zeros_like(sums), torch.zeros(rows, dtype=torch.float64, device=DEV)
+    sums.index_put_((ids[there],), g[there].double(), accumulate=True)
+    sizes.index_put_((ids[there],), g[there].double().abs(), accumulate=True)
+    count.index_put_((ids[there],), torch.ones(len(there), dtype=torch.float64, device=DEV), accumulate=True)
+    want = sums * scale
+    off = sizes * abs(scale) * (count[:, None] + 2) * U * 1.01
+    if before is not None:
+        want = want + before.double()
+        off = off + U * want.abs() * 1.01
+    return want, off
+
+
+def check_gradient(got, g, ids, scale, before):
+    want, off = gradient64(g, ids, got.shape[0], scale, before)
+    named = torch.zeros(got.shape[0], dtype=torch.bool, device=DEV)
+    named[ids[(ids >= 0) & (ids < got.shape[0])]] = True
+    # rows without a term: as they were, or exactly 0
+    rest = got[~named]
+    assert torch.equal(rest, before[~named] if before is not None else torch.zeros_like(rest))
+    bound = off + half_step(got.dtype) * (want.abs() + off) * 1.01 + 1e-37
+    bad = ~((got.double() - want).abs() <= bound)
+    assert not bad.any(), f"{int(bad.sum())} of {bad.numel()} off, most {float(((got.double() - want).abs() / bound).max()):.3g} times the bound"
+
+
+DIMS = [1, 2, 3, 4, 7, 8, 16, 31, 33, 64, 100, 128, 255, 256, 257, 511, 512, 602, 1001, 1024, 4096, 4100, 8193, 65_536]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tdt, odt", [(F32, F32), (BF16, BF16), (F32, BF16), (BF16, F32)])
+@pytest.mark.parametrize("dim", DIMS)
+def test_lookup(dim, tdt, odt):
+    gen = torch.Generator().manual_seed(dim)
+    rows = max(3, 40_000 // dim)
+    table = rand(gen, rows, dim, dtype=tdt)
+    for n in (1, 2, 5, 67, 1000) if dim < 5000 else (1, 9):
+        ids = make_ids(gen, "zipf", n, rows)
+        out = torch.full((n, dim), 7.0, dtype=odt, device=DEV)
+        assert gnn.embed_fwd(table, ids, out, math.sqrt(dim)) is out
+        assert torch.equal(out, lookup(table, ids, math.sqrt(dim), odt)), n
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("dim, stride", [(7, 8), (16, 24), (100, 101), (256, 260), (1001, 1024)])
+def test_lookup_strided_and_misaligned(dim, stride, dt):
+    gen = torch.Generator().manual_seed(dim)
+    table = misaligned(rand(gen, 50, stride, dtype=dt), 3)[:, 1:dim + 1] if stride > dim else None
+    ids = make_ids(gen, "zipf", 333, 50)
+    out = misaligned(torch.zeros((333, dim), dtype=dt, device=DEV), 1)
+    gnn.embed_fwd(table, ids, out, -0.25)
+    assert torch.equal(out, lookup(table, ids, -0.25, dt))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", [F32, BF16])
+def test_lookup_by_a_device_count(dt):
+    gen = torch.Generator().manual_seed(5)
+    table, ids = rand(gen, 300, 100, dtype=dt), make_ids(gen, "zipf", 500, 300)
+    for n in (0, 1, 77, 500, 600, -3):
+        out = torch.full((500, 100), 7.0, dtype=dt, device=DEV)
+        gnn.embed_fwd(table, ids, out, 2.0, n_ids_dev=torch.tensor([n], device=DEV))
+        live = min(max(n, 0), 500)
+        assert torch.equal(out[:live], lookup(table, ids[:live], 2.0, dt)) and (out[live:] == 7).all(), n
+
+
+@pytest.mark.gpu
+def test_lookup_of_none_and_of_other_rows_values():
+    table = torch.full((4, 8), math.nan, device=DEV)
+    table[1], table[2, 3] = 1.5, math.inf
+    out = torch.empty((0, 8), device=DEV)
+    gnn.embed_fwd(table, torch.empty(0, dtype=torch.int64, device=DEV), out)
+    out = torch.empty((3, 8), device=DEV)
+    gnn.embed_fwd(table, torch.tensor([1, -1, 2], device=DEV), out, 2.0)
+    assert (out[0] == 3).all() and (out[1] == 0).all() and out[2, 3] == math.inf and out[2, 0].isnan()
+
+
+LAWS = ["zipf", "same", "distinct", "sorted", "absent", "last"]
+COUNTS = [1, 2, 31, 32, 33, 65, 1000, 8191, 8192, 8193, 20_000, 70_000]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("add", [False, True])
+@pytest.mark.parametrize("law", LAWS)
+@pytest.mark.parametrize("n", COUNTS)
+def test_gradient(n, law, add):
+    gen = torch.Generator().manual_seed(n)
+    for rows, dim, dt in ((1, 5, F32), (2, 64, BF16), (257, 100, F32), (5003, 33, BF16)):
+        ids, g = make_ids(gen, law, n, rows), rand(gen, n, dim, dtype=dt)
+        before = rand(gen, rows, dim, dtype=dt)
+        d = before.clone()
+        assert gnn.embed_bwd(g, ids, d, 1.5, accumulate=add) is d
+        check_gradient(d, g, ids, 1.5, before if add else None)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("add", [False, True])
+@pytest.mark.parametrize("gdt, ddt", [(F32, F32), (BF16, BF16), (F32, BF16), (BF16, F32)])
+@pytest.mark.parametrize("dim", DIMS)
+def test_gradient_widths(dim, gdt, ddt, add):
+    gen = torch.Generator().manual_seed(dim)
+    n = max(3, min(3000, 2_000_000 // dim))
+    rows = max(2, n // 5)
+    ids, g = make_ids(gen, "zipf", n, rows), misaligned(rand(gen, n, dim, dtype=gdt), dim % 3)
+    before = misaligned(rand(gen, rows, dim, dtype=ddt), dim % 5)
+    d = misaligned(before, (dim + 1) % 4)
+    gnn.embed_bwd(g, ids, d, math.sqrt(dim), accumulate=add)
+    check_gradient(d, g, ids, math.sqrt(dim), before if add else None)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows", [255, 256, 257, 65_535, 65_536, 65_537, 2_449_029, (1 << 24) - 1, 1 << 24, (1 << 24) + 1])
+@pytest.mark.parametrize("n", [100, 9000])
+def test_gradient_of_tables_at_the_digits_edges(rows, n):
+    gen = torch.Generator().manual_seed(rows)
+    ids, g = make_ids(gen, "zipf", n, rows), rand(gen, n, 4)
+    ids[:3] = torch.tensor([rows - 1, rows, 0], device=DEV)
+    d = torch.full((rows, 4), 7.0, device=DEV)
+    gnn.embed_bwd(g, ids, d)
+    check_gradient(d, g, ids, 1.0, None)
+
+
+@pytest.mark.gpu
+def test_gradient_by_a_device_count():
+    gen = torch.Generator().manual_seed(8)
+    ids, g = make_ids(gen, "zipf", 9000, 400), rand(gen, 9000, 20)
+    for n in (0, 1, 33, 5000, 9000, 9001, -1):
+        live = min(max(n, 0), 9000)
+        g2 = g.clone()
+        g2[live:] = math.nan  # not read
+        for before in (None, rand(gen, 400, 20)):
+            d = torch.full((400, 20), 7.0, device=DEV) if before is None else before.clone()
+            gnn.embed_bwd(g2, ids, d, 1.0, accumulate=before is not None, n_ids_dev=torch.tensor([n], device=DEV))
+            check_gradient(d, g[:live], ids[:live], 1.0, before)
+
+
+@pytest.mark.gpu
+def test_absent_rows_are_not_read_and_no_ids_at_all():
+    g = torch.full((5, 8), math.nan, device=DEV)
+    g[3] = 1.0
+    d = torch.full((6, 8), 7.0, device=DEV)
+    gnn.embed_bwd(g, torch.tensor([-1, 6, 2 ** 40, 4, -7], device=DEV), d)
+    assert (d[4] == 1).all() and (d[[0, 1, 2, 3, 5]] == 0).all()
+    none = torch.empty(0, dtype=torch.int64, device=DEV)
+    gnn.embed_bwd(torch.empty((0, 8), device=DEV), none, d, accumulate=True)
+    assert (d[4] == 1).all()
+    gnn.embed_bwd(torch.empty((0, 8), device=DEV), none, d)
+    assert (d == 0).all()
+    # a value that is not finite stays in the rows that are named with it
+    g[3, 2] = math.inf
+    gnn.embed_bwd(g, torch.tensor([-1, 1, -1, 4, -1], device=DEV), d)
+    assert d[4, 2] == math.inf and d[1].isnan().all() and (d[[0, 2, 3, 5]] == 0).all()
+
+
+@pytest.mark.gpu
+def test_the_gradient_is_the_lookups_adjoint_and_its_differences():
+    gen = torch.Generator().manual_seed(3)
+    table, ids, g = rand(gen, 50, 12), make_ids(gen, "zipf", 400, 50), rand(gen, 400, 12)
+    d, out = torch.empty_like(table), torch.empty((400, 12), device=DEV)
+
+    def loss(t):
+        return float((gnn.embed_fwd(t, ids, out, 3.0).double() * g.double()).sum())
+    gnn.embed_bwd(g, ids, d, 3.0)
+    # each product's factors and sums: as many roundings as a row has terms, of sizes up to 3 |g| max|table|
+    size = 3 * float(g.abs().double().sum()) * float(table.abs().max())
+    off = abs(loss(table) - float((d.double() * table.double()).sum()))
+    assert off <= 402 * U * size
+    # the loss is linear in the table, so a difference of any size is its slope: the products' roundings remain
+    for v, c in ((0, 0), (1, 5), (7, 11), (49, 3)):
+        up, down = table.clone(), table.clone()
+        up[v, c] += 0.5
+        down[v, c] -= 0.5
+        slope = (loss(up) - loss(down)) / float(up[v, c].double() - down[v, c].double())
+        assert abs(slope - float(d[v, c])) <= 402 * U * 3 * float(g.abs().sum()), (v, c)
+
+
+@pytest.mark.gpu
+def test_offsets_past_32_bits():
+    rows, dim = 2_200_003, 1024  # 2.25e9 values
+    table = torch.zeros((rows, dim), dtype=BF16, device=DEV)
+    ids = torch.tensor([rows - 1, 0, 2_097_153, 1_048_577, rows - 1], device=DEV)
+    gen = torch.Generator().manual_seed(1)
+    table[ids[:4]] = rand(gen, 4, dim, dtype=BF16)
+    out = torch.empty((5, dim), dtype=BF16, device=DEV)
+    gnn.embed_fwd(table, ids, out, 1.0)
+    assert torch.equal(out, table[ids])
+    g = rand(gen, 5, dim, dtype=BF16)
+    gnn.embed_bwd(g, ids, table, 1.0)
+    want = torch.stack([(g[0].double() + g[4].double()), g[1].double(), g[2].double(), g[3].double()])
+    got = table[ids[:4]].double()
+    assert ((got - want).abs() <= want.abs() * 2.0 ** -8 * 1.01 + 1e-30).all()
+    assert int((table != 0).any(1).sum()) == 4
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [700, 30_000])
+def test_the_same_bits_again_also_from_a_graph_on_another_stream(n):
+    gen = torch.Generator().manual_seed(n)
+    ids, g, table = make_ids(gen, "zipf", n, 900), rand(gen, n, 100, dtype=BF16), rand(gen, 900, 100)
+    first, out = torch.empty((900, 100), device=DEV), torch.empty((n, 100), device=DEV)
+    gnn.embed_bwd(g, ids, first)
+    stream = torch.cuda.Stream()
+    d, ws = torch.empty_like(first), gnn.embed_bwd_workspace(n, 900, 100, DEV)
+    ws.fill_(0xff)
+    torch.cuda.synchronize()
+    gnn.embed_bwd(g, ids, d, ws=ws, stream=stream)
+    stream.synchronize()
+    assert torch.equal(d, first)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        gnn.embed_fwd(table, ids, out, 2.0)
+        gnn.embed_bwd(g, ids, d, ws=ws)
+    for k in range(4):
+        g.mul_(-1.0)
+        ids.copy_(ids.roll(1))
+        gnn.embed_bwd(g, ids, first)
+        d.fill_(5.0)
+        ws.fill_(k)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(d, first) and torch.equal(out, lookup(table, ids, 2.0, F32)), k
+
+
+# --- refusals ---------------------------------------------------------------
+
+def call(name, *args):
+    code = getattr(gnn.lib(), name)(*args)
+    return code, gnn.lib().gnn_last_error().decode()
+
+
+BUF = ctypes.create_string_buffer(1 << 16)
+P = (ctypes.addressof(BUF) + 255) // 256 * 256  # any address: a refused call reads nothing
+
+
+@pytest.mark.parametrize("change, code, what", [
+    (dict(tdt=2), gnn.GNN_EUNSUPPORTED, "dtypes"), (dict(odt=7), gnn.GNN_EUNSUPPORTED, "dtypes"),
+    (dict(rows=0), gnn.GNN_EINVAL, "n_rows"), (dict(rows=1 << 31), gnn.GNN_EINVAL, "n_rows"),
+    (dict(dim=0), gnn.GNN_EINVAL, "dim"), (dict(dim=65_537, stride=65_537), gnn.GNN_EINVAL, "dim"),
+    (dict(stride=7), gnn.GNN_EINVAL, "row_stride"), (dict(cap=-1), gnn.GNN_EINVAL, "cap_ids"),
+    (dict(cap=1 << 31), gnn.GNN_EINVAL, "cap_ids"), (dict(scale=math.inf), gnn.GNN_EINVAL, "scale"),
+    (dict(scale=math.nan), gnn.GNN_EINVAL, "scale"), (dict(table=None), gnn.GNN_EINVAL, "NULL"),
+    (dict(ids=None), gnn.GNN_EINVAL, "NULL"), (dict(out=None), gnn.GNN_EINVAL, "NULL"),
+    (dict(table=P + 2), gnn.GNN_EINVAL, "misaligned"), (dict(ids=P + 4), gnn.GNN_EINVAL, "misaligned"),
+    (dict(count=P + 4), gnn.GNN_EINVAL, "misaligned"), (dict(out=P), gnn.GNN_EINVAL, "must not be"),
+])
+def test_lookup_refusals(change, code, what):
+    a = dict(table=P, tdt=0, rows=10, dim=8, stride=8, ids=P, count=None, cap=4, scale=1.0, out=P + 1024, odt=0) | change
+    got = call("gnn_embed_fwd", *a.values(), None)
+    assert got[0] == code and what in got[1]
+
+
+@pytest.mark.parametrize("change, code, what", [
+    (dict(gdt=2), gnn.GNN_EUNSUPPORTED, "dtypes"), (dict(ddt=3), gnn.GNN_EUNSUPPORTED, "dtypes"),
+    (dict(rows=0), gnn.GNN_EINVAL, "n_rows"), (dict(dim=0), gnn.GNN_EINVAL, "dim"),
+    (dict(cap=-1), gnn.GNN_EINVAL, "cap_ids"), (dict(cap=1 << 31), gnn.GNN_EINVAL, "cap_ids"),
+    (dict(scale=math.nan), gnn.GNN_EINVAL, "scale"), (dict(g=None), gnn.GNN_EINVAL, "NULL"),
+    (dict(ids=None), gnn.GNN_EINVAL, "NULL"), (dict(d=None), gnn.GNN_EINVAL, "NULL"),
+    (dict(d=P), gnn.GNN_EINVAL, "must not be"), (dict(g=P + 1), gnn.GNN_EINVAL, "misaligned"),
+    (dict(d=P + 1025), gnn.GNN_EINVAL, "misaligned"), (dict(ws=None), gnn.GNN_EINVAL, "ws"),
+    (dict(ws=P + 64), gnn.GNN_EINVAL, "ws"), (dict(bytes=16), gnn.GNN_ESIZE, "workspace"),
+])
+def test_gradient_refusals(change, code, what):
+    a = dict(g=P, gdt=0, ids=P, count=None, cap=4, dim=8, scale=1.0, rows=10, add=0, d=P + 1024, ddt=0, ws=P, bytes=1 << 40) | change
+    got = call("gnn_embed_bwd", *a.values(), None)
+    assert got[0] == code and what in got[1]
+
+
+def test_workspace_sizes():
+    nb = ctypes.c_size_t()
+    assert call("gnn_embed_bwd_workspace_size", 0, 10, 8, ctypes.byref(nb))[0] == gnn.GNN_OK and nb.value == 0
+    assert call("gnn_embed_bwd_workspace_size", 1, 10, 8, ctypes.byref(nb))[0] == gnn.GNN_OK and nb.value > 0
+    assert call("gnn_embed_bwd_workspace_size", 1, 10, 8, None)[0] == gnn.GNN_EINVAL
+    assert call("gnn_embed_bwd_workspace_size", 1, 0, 8, ctypes.byref(nb))[0] == gnn.GNN_EINVAL
+
+
+def test_the_binding_refuses_what_is_not_on_a_gpu():
+    t, ids = torch.zeros(4, 8), torch.zeros(3, dtype=torch.int64)
+    with pytest.raises(ValueError, match="GPU"):
+        gnn.embed_fwd(t, ids, torch.zeros(3, 8))
+    with pytest.raises(ValueError, match="GPU"):
+        gnn.embed_bwd(torch.zeros(3, 8), ids, t)
+    with pytest.raises(ValueError, match="table"):
+        gnn.embed_fwd(torch.zeros(8, 4).t(), ids, torch.zeros(3, 8))
+
+
+@pytest.mark.gpu
+def test_the_binding_refuses_wrong_tensors():
+    t, ids, out = torch.zeros((4, 8), device=DEV), torch.zeros(3, dtype=torch.int64, device=DEV), torch.zeros((3, 8), device=DEV)
+    for bad in (dict(ids=ids.int()), dict(out=out[:2]), dict(out=out.half()), dict(ids=ids.cpu()), dict(out=torch.zeros((3, 16), device=DEV)[:, ::2]),
+                dict(table=t.half()), dict(table=t[:1].expand(4, 8)), dict(table=t[0])):
+        a = dict(table=t, ids=ids, out=out) | bad
+        with pytest.raises(ValueError):
+            gnn.embed_fwd(**a)
+    g = torch.zeros((3, 8), device=DEV)
+    for bad in (dict(g=g[:, :4]), dict(ids=ids[:2]), dict(d_table=t.half()), dict(d_table=t.t()), dict(n_ids_dev=ids), dict(ws=t)):
+        a = dict(g=g, ids=ids, d_table=t) | bad
+        with pytest.raises(ValueError):
+            gnn.embed_bwd(**a)
+    small = torch.empty(256, dtype=torch.uint8, device=DEV)
+    with pytest.raises(gnn.GnnError, match="workspace"):
+        gnn.embed_bwd(g, ids, t, ws=small)
