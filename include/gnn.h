@@ -634,6 +634,48 @@ gnn_status gnn_distill_topk(const void *logits, gnn_dtype ldt, int64_t b, int64_
                             const int64_t *targets, const float *row_scale, void *g_out, gnn_dtype gdt,
                             float *row_loss, float *loss_out, void *ws, size_t ws_bytes, gnn_stream s);
 
+/* The last layer and its loss in one call, for many classes: the softmax
+ * cross-entropy of the logits Z = A Wt^T + b (equation 2 with the loss of Section
+ * II-B) and its gradients, computed in pieces of the classes, so that neither the
+ * logits nor their gradient exist as a whole:
+ *   lse_i = log sum_c exp(z_ic),  row_loss_i = lse_i - z_i[y_i],
+ *   loss = sum_i s_i row_loss_i,  dZ = s (exp(z - lse) - onehot(y)),
+ *   dwt = dZ^T A,  db = column sums of dZ,  d_a = dZ Wt.
+ *   a      [device] b x k of adt (GNN_F32 or GNN_BF16); b >= 0.
+ *   wt     [device] c x k of wdt (GNN_F32 or GNN_BF16): a row for each class, as
+ *          the shadow W^T of a layer or an embedding table lies;
+ *          c <= GNN_MAX_CLASSES, k <= GNN_MAX_DIM.
+ *   bias   [device] fp32 c, or NULL.
+ *   labels, targets, row_scale (s_i, 1 / b when NULL): as in gnn_distill_topk.  A row
+ *          whose scale is 0 or whose label is outside [0, c) takes no part,
+ *          whatever its values: its loss is 0, its row of d_a is 0 (as long as wt is
+ *          finite), and it adds nothing to dwt and db.
+ *   gemm_dt GNN_BF16: the products' operands (dZ among them) are rounded to
+ *          bf16, sums are fp32; GNN_F32: fp32 throughout, and gdt and dwdt must be
+ *          GNN_F32.
+ *   row_loss [device] fp32 b, or NULL.  loss_out [device] fp32 scalar.
+ *   d_a    [device] b x k of gdt (GNN_F32 or GNN_BF16), or NULL; it may be a
+ *          itself when gdt == adt.
+ *   dwt    [device] c x k of dwdt (GNN_F32 or GNN_BF16), or NULL; overwritten.
+ *   db     [device] fp32 c, or NULL; dZ is summed unrounded.
+ *   ws     [device] 256-byte aligned workspace of
+ *          gnn_update_ce_workspace_size bytes (grads: any gradient is wanted); no
+ *          state is kept in it between calls; calls sharing it must not
+ *          overlap.
+ * Logits, sums and probabilities are fp32; every sum has a fixed order that goes by
+ * sizes, types and alignment of the pointers to 16 bytes: for the same of these,
+ * results are bitwise reproducible.  In a row that takes part, a NaN or +infinity
+ * among the logits, or -infinity in all of them, makes its loss NaN.  Errors:
+ * GNN_EINVAL for bad sizes, NULL or misaligned (to the element) pointers;
+ * GNN_EUNSUPPORTED for other dtypes; GNN_ESIZE for a small workspace or sizes
+ * past the grid limit. */
+gnn_status gnn_update_ce_workspace_size(int64_t b, int64_t k, int64_t c, gnn_dtype gemm_dt, int32_t grads,
+                                        size_t *bytes);
+gnn_status gnn_update_ce(const void *a, gnn_dtype adt, int64_t b, int64_t k, const void *wt, gnn_dtype wdt,
+                         const float *bias, int64_t c, const int64_t *labels, const int64_t *targets,
+                         const float *row_scale, gnn_dtype gemm_dt, float *row_loss, float *loss_out, void *d_a,
+                         gnn_dtype gdt, void *dwt, gnn_dtype dwdt, float *db, void *ws, size_t ws_bytes, gnn_stream s);
+
 /* ------------------------------------------------------------------------
  * Layer normalisation of the rows of an activation matrix, between the
  * layers of a deep or residual model.  With mu_i and v_i the mean and the

@@ -111,6 +111,14 @@ gnn_status check_act(const ActArgs &a, bool weights, const char *who) {
     return GNN_OK;
 }
 
+gnn_status check_ce(int64_t b, int64_t k, int64_t c, int gemm_dt, const char *who) {
+    GNN_CHECK(act_dtype(gemm_dt), GNN_EUNSUPPORTED, "%s: dtypes must be GNN_F32 or GNN_BF16", who);
+    GNN_CHECK(b >= 0 && b <= kMaxGrid / 256, GNN_EINVAL, "%s: bad b", who);
+    GNN_CHECK(dim_ok(k), GNN_EINVAL, "%s: k out of [1, %d]", who, GNN_MAX_DIM);
+    GNN_CHECK(c >= 1 && c <= GNN_MAX_CLASSES, GNN_EINVAL, "%s: c out of [1, %d]", who, GNN_MAX_CLASSES);
+    return GNN_OK;
+}
+
 gnn_status check_embed(int64_t cap_ids, int64_t n_rows, int64_t dim, const char *who) {
     GNN_CHECK(dim_ok(dim), GNN_EINVAL, "%s: dim out of [1, %d]", who, GNN_MAX_DIM);
     GNN_CHECK(n_rows >= 1 && n_rows < (1ll << 31), GNN_EINVAL, "%s: n_rows out of [1, 2^31)", who);
@@ -759,6 +767,41 @@ gnn_status gnn_distill_topk(const void *logits, gnn_dtype ldt, int64_t b, int64_
     const DistillArgs a{logits, ldt, b, c, t_val, tdt, t_idx, k, temperature, alpha, labels, targets, row_scale, g_out,
                         gdt, row_loss, loss_out};
     return launch_distill(a, ws, stream_of(s));
+}
+
+gnn_status gnn_update_ce_workspace_size(int64_t b, int64_t k, int64_t c, gnn_dtype gemm_dt, int32_t grads,
+                                        size_t *bytes) {
+    clear_error();
+    const char *who = "gnn_update_ce_workspace_size";
+    GNN_CHECK(bytes, GNN_EINVAL, "%s: bytes is NULL", who);
+    GNN_TRY(check_ce(b, k, c, gemm_dt, who));
+    *bytes = update_ce_ws_bytes(b, k, c, gemm_dt, grads != 0);
+    return GNN_OK;
+}
+
+gnn_status gnn_update_ce(const void *a, gnn_dtype adt, int64_t b, int64_t k, const void *wt, gnn_dtype wdt,
+                         const float *bias, int64_t c, const int64_t *labels, const int64_t *targets,
+                         const float *row_scale, gnn_dtype gemm_dt, float *row_loss, float *loss_out, void *d_a,
+                         gnn_dtype gdt, void *dwt, gnn_dtype dwdt, float *db, void *ws, size_t ws_bytes, gnn_stream s) {
+    clear_error();
+    const char *who = "gnn_update_ce";
+    GNN_CHECK(act_dtype(adt) && act_dtype(wdt) && act_dtype(gdt) && act_dtype(dwdt), GNN_EUNSUPPORTED,
+              "%s: dtypes must be GNN_F32 or GNN_BF16", who);
+    GNN_TRY(check_ce(b, k, c, gemm_dt, who));
+    GNN_CHECK(gemm_dt == GNN_BF16 || ((!d_a || gdt == GNN_F32) && (!dwt || dwdt == GNN_F32)), GNN_EUNSUPPORTED,
+              "%s: GNN_F32 products need gdt and dwdt GNN_F32", who);
+    GNN_CHECK(((a && labels) || b == 0) && wt && loss_out, GNN_EINVAL, "%s: NULL pointer", who);
+    GNN_CHECK(!dwt || (dwt != wt && dwt != a && dwt != d_a), GNN_EINVAL, "%s: dwt must not be an input or d_a", who);
+    GNN_CHECK(!d_a || (d_a != wt && (d_a != a || gdt == adt)), GNN_EINVAL,
+              "%s: d_a must not be wt, and may be a only with the same dtype", who);
+    GNN_CHECK(aligned(a, dtype_size(adt)) && aligned(wt, dtype_size(wdt)) && aligned(bias, 4) && aligned(labels, 8) &&
+                  aligned(targets, 8) && aligned(row_scale, 4) && aligned(row_loss, 4) && aligned(loss_out, 4) &&
+                  aligned(d_a, dtype_size(gdt)) && aligned(dwt, dtype_size(dwdt)) && aligned(db, 4),
+              GNN_EINVAL, "%s: misaligned data", who);
+    GNN_TRY(check_ws(ws, ws_bytes, update_ce_ws_bytes(b, k, c, gemm_dt, d_a || dwt || db), who));
+    const CeArgs args{a, adt, b, k, wt, wdt, bias, c, labels, targets, row_scale, gemm_dt, row_loss, loss_out, d_a, gdt, dwt,
+                      dwdt, db};
+    return launch_update_ce(args, ws, stream_of(s));
 }
 
 gnn_status gnn_layer_norm_fwd(const void *x, gnn_dtype xdt, const int64_t *m_dev, int64_t cap_m, int64_t f,

@@ -82,18 +82,22 @@ __device__ __forceinline__ Rates rates_of(const Args &a) {
     return x;
 }
 
-// One element: m, v and w are replaced; the root of v is returned.
+// One element: m, v and w are replaced; the root of v is returned.  Every product and sum
+// is rounded by itself, so that what is stored in 8 bits does not go by which of them the
+// compiler would join (the step is bound by memory either way).
 __device__ __forceinline__ float move(const Args &a, const Rates &x, float keep, float g, float &m, float &v, float &w) {
-    m = fmaf(a.b1, m, a.nb1 * g);
-    v = fmaf(a.b2, v, a.nb2 * (g * g));
+#pragma clang fp contract(off)
+    m = a.b1 * m + a.nb1 * g;
+    v = a.b2 * v + a.nb2 * (g * g);
     const float root = sqrtf(v);
-    w = fmaf(w, keep, -(x.c1 * (m / fmaf(root, x.c2, a.eps))));
+    w = w * keep - x.c1 * (m / (root * x.c2 + a.eps));
     return root;
 }
 
 // |x| times `inverse` as the magnitude of an e4m3 value: below 2^-6 whole steps of
 // 2^-9, above eight steps to an octave; `chance` of a step (in 2^-16) is added.
 __device__ __forceinline__ uint32_t code_of(float x, float inverse, uint32_t chance) {
+#pragma clang fp contract(off)
     const float t = fabsf(x) * inverse;
     const int e = max(static_cast<int>(__float_as_uint(t) >> 23) - 130, -9);
     const float u = (static_cast<float>(chance) + 0.5f) * 0x1p-16f;

@@ -1,0 +1,35 @@
+// The softmax cross-entropy of an update with many classes, in pieces of the
+// classes (class_loss.hip), and the matrix products of a piece (class_loss_engine.hip
+// in fp32, class_loss_tile.hip in bf16).
+#pragma once
+
+#include "internal.h"
+
+namespace gnn {
+namespace closs {
+
+// C = X Y over a reduction of R: rows of X and columns of Y reduced.  An operand is N
+// where its output rows (columns) run along the reduction in memory, T where the
+// reduction runs down the rows of the matrix.  Operands are of one type (fp32 or
+// bf16), aligned to 16 bytes with rows of whole 16 bytes; what lies behind
+// the output's rows and columns in them is zero or not stored.
+struct Product {
+    const void *x, *y;
+    int64_t ldx, ldy;
+    int64_t M, N, R;       // output rows and columns; reduction (N operands: a multiple of 16 bytes)
+    int64_t Ry;            // reduction rows that a T operand y has (at most R)
+    void *out;
+    int odt;               // GNN_F32 or GNN_BF16
+    int64_t ld;            // of out
+    int64_t nsplit, split_stride;  // a split of the reduction writes to out + split * split_stride (then fp32)
+    bool add;              // to what out holds (fp32)
+};
+enum Kind { kNN, kTT, kNT };
+
+int64_t splits_f32(Kind kind, int64_t M, int64_t N, int64_t R, bool may_split);
+gnn_status product_f32(Kind kind, const Product &p, hipStream_t s);
+int64_t splits_bf16(Kind kind, int64_t M, int64_t N, int64_t R, bool may_split);
+gnn_status product_bf16(Kind kind, const Product &p, hipStream_t s);
+
+}  // namespace closs
+}  // namespace gnn

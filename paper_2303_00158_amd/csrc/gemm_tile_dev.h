@@ -70,7 +70,7 @@ using Small = Cfg<2, 2, 4>;  // 64 x 64
 // epilogue, which in large tiles nothing overlaps (14,591 x 512 x 1,024 with a residual:
 // 39 us in 256 x 256 tiles, 35 in 128 x 128).  A split (fp32 partial tiles,
 // added in order by another kernel) costs their bytes, out and in, and a launch;
-// each has at least four chunks.  4,096 x 1,024 x 2,048: 43 us in 256 x 256 tiles, 24 in
+// each has at least four chunks, and there are at most `splits`.  4,096 x 1,024 x 2,048: 43 us in 256 x 256 tiles, 24 in
 // 128 x 128, 35 in 64 x 64; 8,192 x 4,096 x 4,096: 221, 266 and 410.
 enum Pick { kBig, kBig7, kMid, kSmall };
 struct Choice {
@@ -90,14 +90,14 @@ template <class C> inline double cost(int64_t tiles, int64_t chunks, int64_t n, 
     if (last) t += each * std::max(p.lone, p.busy * last) + p.ends * last;
     return t;
 }
-inline Choice choose(int64_t rows, int64_t cols, int64_t red) {
+inline Choice choose(int64_t rows, int64_t cols, int64_t red, int64_t splits = 16) {
     Choice best{kSmall, 1};
     double least = -1;
     auto look = [&](auto cfg, Pick pick, const Pace &p) {
         using C = decltype(cfg);
         const int64_t chunks = std::max<int64_t>(ceil_div(red, int64_t(kBK)), 1);
         const int64_t tiles = ceil_div(rows, int64_t(C::BM)) * ceil_div(cols, int64_t(C::BN)), round = 256 * C::PER_CU;
-        for (int64_t n = 1; n <= 16 && (n == 1 || (n * tiles <= round && n * 4 <= chunks)); n *= 2) {
+        for (int64_t n = 1; n <= splits && (n == 1 || (n * tiles <= round && n * 4 <= chunks)); n *= 2) {
             const double t = cost<C>(tiles, chunks, n, p) + (n > 1 ? 4 + static_cast<double>(n) * rows * cols * 8 / 4e6 : 0);
             if (least < 0 || t < least) {
                 least = t;

@@ -278,6 +278,27 @@ gnn_status launch_layer_norm_bwd(const void *g, int gdt, const void *x, int xdt,
                                  int64_t f, const float *gamma, const float *mean, const float *rstd,
                                  const void *d_res, void *d_x, float *dgamma, float *dbeta, void *ws, hipStream_t s);
 gnn_status launch_sgd(float *w, const float *dw, int64_t n, float lr, hipStream_t s);
+// The softmax cross-entropy of an update with many classes (class_loss.hip).
+struct CeArgs {
+    const void *a;
+    int adt;
+    int64_t b, k;
+    const void *wt;
+    int wdt;
+    const float *bias;
+    int64_t c;
+    const int64_t *labels, *targets;
+    const float *row_scale;
+    int gemm_dt;
+    float *row_loss, *loss_out;
+    void *d_a;
+    int gdt;
+    void *dwt;
+    int dwdt;
+    float *db;
+};
+size_t update_ce_ws_bytes(int64_t b, int64_t k, int64_t c, int gemm_dt, bool grads);
+gnn_status launch_update_ce(const CeArgs &a, void *ws, hipStream_t s);
 // The AdamW step over many tensors (adamw.hip).
 gnn_status launch_adamw(const gnn_adamw_tensor *t, int64_t count, int sdt, double lr, double beta1, double beta2, double eps,
                         int64_t step, const float *lr_dev, const int64_t *step_dev, uint64_t seed, hipStream_t s);

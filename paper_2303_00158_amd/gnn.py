@@ -123,6 +123,9 @@ _SIGNATURES = {
     "gnn_distill_topk_workspace_size": (_i32, [_i64, _i64, _i64, _P(_sz)]),
     "gnn_distill_topk": (_i32, [_vp, _i32, _i64, _i64, _vp, _i32, _vp, _i64, _f32, _f32, _vp, _vp, _vp, _vp, _i32, _vp,
                                 _vp, _vp, _sz, _vp]),
+    "gnn_update_ce_workspace_size": (_i32, [_i64, _i64, _i64, _i32, _i32, _P(_sz)]),
+    "gnn_update_ce": (_i32, [_vp, _i32, _i64, _i64, _vp, _i32, _vp, _i64, _vp, _vp, _vp, _i32, _vp, _vp, _vp, _i32, _vp,
+                             _i32, _vp, _vp, _sz, _vp]),
     "gnn_layer_norm_fwd": (_i32, [_vp, _i32, _vp, _i64, _i64, _vp, _vp, _f32, _vp, _i32, _vp, _vp, _vp]),
     "gnn_layer_norm_bwd_workspace_size": (_i32, [_i64, _i64, _P(_sz)]),
     "gnn_layer_norm_bwd": (_i32, [_vp, _i32, _vp, _i32, _vp, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz,
@@ -765,6 +768,49 @@ def distill_topk(logits: torch.Tensor, t_val: torch.Tensor, t_idx: torch.Tensor,
              _ptr(row_scale), _ptr(g_out), dtype_code(g_out.dtype) if g_out is not None else GNN_F32, _ptr(row_loss),
              _ptr(loss_out), _ptr(ws), ws.numel())
     return loss_out, g_out
+
+
+def update_ce_workspace(a: torch.Tensor, wt: torch.Tensor, gemm_dtype: int, grads: bool = True,
+                        stream=None) -> torch.Tensor:
+    """A workspace for update_ce on operands of these shapes (grads: any
+    gradient is wanted)."""
+    nb = _sz()
+    _check(lib().gnn_update_ce_workspace_size(a.shape[0], a.shape[1], wt.shape[0], gemm_dtype, int(grads),
+                                              ctypes.byref(nb)))
+    return _scratch(nb.value, a.device, stream)
+
+
+def update_ce(a: torch.Tensor, wt: torch.Tensor, bias: Optional[torch.Tensor], labels: torch.Tensor,
+              loss_out: torch.Tensor, gemm_dtype: int, row_loss: Optional[torch.Tensor] = None,
+              d_a: Optional[torch.Tensor] = None, dwt: Optional[torch.Tensor] = None,
+              db: Optional[torch.Tensor] = None, targets: Optional[torch.Tensor] = None,
+              row_scale: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """gnn_update_ce: the softmax cross-entropy of the logits a wt^T + bias (a:
+    b x k; wt: a row of k for each class) and those of its gradients that are
+    given, without the logits in memory.  row_scale: each row's factor in the
+    loss (1 / b when None; 0, or a label outside the classes, leaves a row
+    out).  d_a may be a itself.  ws: workspace (allocated when None)."""
+    b, k = _matrix("a", a)
+    dev = a.device
+    _want("wt", wt, (None, k), _ACTIVATIONS, dev)
+    c = wt.shape[0]
+    _want("bias", bias, (c,), _FP32, dev)
+    _want("loss_out", loss_out, (1,) if loss_out.dim() else (), _FP32, dev)
+    _want("row_loss", row_loss, (b,), _FP32, dev)
+    _want("d_a", d_a, (b, k), _ACTIVATIONS, dev)
+    _want("dwt", dwt, (c, k), _ACTIVATIONS, dev)
+    _want("db", db, (c,), _FP32, dev)
+    _want("row_scale", row_scale, (b,), _FP32, dev)
+    _want("targets", targets, (b,), _INT64, dev)
+    _want("labels", labels, (None if targets is not None else b,), _INT64, dev)
+    if ws is None:
+        ws = update_ce_workspace(a, wt, gemm_dtype, d_a is not None or dwt is not None or db is not None, stream)
+    _want("ws", ws, (None,), (torch.uint8,), dev)
+    _enqueue(lib().gnn_update_ce, dev, stream, _ptr(a), dtype_code(a.dtype), b, k, _ptr(wt), dtype_code(wt.dtype),
+             _ptr(bias), c, _ptr(labels), _ptr(targets), _ptr(row_scale), gemm_dtype, _ptr(row_loss), _ptr(loss_out),
+             _ptr(d_a), dtype_code(d_a.dtype) if d_a is not None else GNN_F32, _ptr(dwt),
+             dtype_code(dwt.dtype) if dwt is not None else GNN_F32, _ptr(db), _ptr(ws), ws.numel())
+    return loss_out
 
 
 # ---------------------------------------------------------------------------
