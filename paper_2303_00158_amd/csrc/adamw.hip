@@ -117,7 +117,7 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t x) {
 // its reciprocal.  Below fp32's normal range both are 0; a scale that is
 // not finite makes what it scales NaN.
 __device__ __forceinline__ float scale_of(uint32_t top, float *inverse) {
-    const float s = __uint_as_float(top) / kTop;
+    const float s = __uint_as_float(top) * (1.f / kTop);
     *inverse = s >= 0x1p-126f ? 1.f / s : 0.f;
     return s < 0x1p-126f ? 0.f : s;
 }

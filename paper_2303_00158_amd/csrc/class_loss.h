@@ -23,8 +23,38 @@ struct Product {
     int64_t ld;            // of out
     int64_t nsplit, split_stride;  // a split of the reduction writes to out + split * split_stride (then fp32)
     bool add;              // to what out holds (fp32)
+    const float *factor;   // [device] one factor of the product, or null
 };
 enum Kind { kNN, kTT, kNT };
+
+// What the rows of A bring along, and what is known of them.
+struct RowState {
+    int32_t *label;   // -1: the row takes no part
+    float *weight;    // 0 then
+    float *top, *sum; // of the classes so far: largest logit, sum of exp(z - top)
+    float *z_label;
+    float *lse;
+};
+
+// Logits of a piece on the matrix cores without keeping them: classes c0 .. c0 + N
+// of the M rows, x = A, y = the piece's rows of Wt (both N, reduction R).
+struct LogitArgs {
+    const uint16_t *x, *y;
+    int64_t ldx, ldy, M, N, R, c0;
+    const float *bias;     // of the piece's first class, or null
+    RowState rows;
+    // sums: a wavefront's columns' largest logit and sum for each row
+    float2 *part;          // strips x M
+    // dZ over *scale
+    uint16_t *dz;          // rows of ld
+    int64_t ld;
+    const float *scale;    // [device] the largest weight
+    float *db_part;        // strips of rows x ld, or null
+};
+int64_t logit_strips(int64_t M, int64_t N, int64_t R);      // column strips of part
+int64_t logit_row_strips(int64_t M, int64_t N, int64_t R);  // row strips of db_part
+gnn_status logit_sums(const LogitArgs &a, hipStream_t s);
+gnn_status logit_dz(const LogitArgs &a, hipStream_t s);
 
 int64_t splits_f32(Kind kind, int64_t M, int64_t N, int64_t R, bool may_split);
 gnn_status product_f32(Kind kind, const Product &p, hipStream_t s);

@@ -4,9 +4,17 @@
 //   dZ = s (exp(z - lse) - onehot(y)),  dWt = dZ^T A,  db = sum_i dZ,  dA = dZ Wt.
 //
 // Bound by the matrix products: 2 b K C operations for the loss, 6 b K C with the
-// gradients, and 2 b K C more where there is more than one piece, whose logits are then
-// computed twice, once for the rows' sums and once for dZ.  Only one piece of
-// Z and dZ exists at a time, so memory goes by b, not by b C.
+// gradients, and 2 b K C more because the logits are computed twice, once for the rows'
+// sums and once for dZ (in fp32 only where there is more than one piece).  Only one
+// piece of dZ (fp32: of Z and dZ, in one place) exists at a time, so memory goes by b, not by b C.
+// bf16 logits stay in the tiles' accumulators (class_loss_tile.hip).
+//
+// dZ is an operand of the products behind it, so bf16 rounds it, and it is rounded over the
+// largest row weight, which the products' ends multiply back: with a common weight
+// of 1 / b in it, the entries of unlikely labels, all of them near -1 / b, would be
+// off by one and the same rounding, and their gradients with them (3,840 rows of 100,003
+// classes: 0.0037 of the gradients' norm that way, 0.0024 this way; a bf16
+// output's own rounding is 0.0017).
 #include "class_loss.h"
 #include "gemm_engine.h"
 #include "loss_dev.h"
@@ -27,14 +35,6 @@ unsigned grid_of(int64_t n) {
 // ---------------------------------------------------------------------------
 // rows: labels and weights, operands in the products' type
 // ---------------------------------------------------------------------------
-struct RowState {
-    int32_t *label;   // -1: the row takes no part
-    float *weight;    // 0 then
-    float *top, *sum; // of the pieces so far: largest logit, sum of exp(z - top)
-    float *z_label;
-    float *lse;
-};
-
 __global__ void __launch_bounds__(kThreads) class_rows_kernel(CeArgs a, RowState r) {
     const int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
     if (i >= a.b) return;
@@ -84,11 +84,25 @@ gnn_status pack(const void *in, int idt, int64_t rows, int64_t K, int64_t ld, co
 }
 
 // ---------------------------------------------------------------------------
-// a piece of the logits
+// rows' sums and losses
 // ---------------------------------------------------------------------------
-// T threads to a row: the piece's largest logit and its sum join the row's.
-template <int T> __global__ void __launch_bounds__(kThreads) class_sums_kernel(const float *z, int64_t b, int64_t cols, int64_t ld, int64_t c0,
-                                                                              const float *bias, RowState r) {
+// A row's largest logit and sum with those of more classes, and behind the last ones its loss.
+__device__ __forceinline__ void join_row(const RowState &r, int64_t i, float top, float sum, bool last, float *row_loss) {
+    const float old = r.top[i], now = fmaxf(old, top), from = now == -INFINITY ? 0.f : now;
+    const float before = r.sum[i];
+    sum = (old == now ? before : before * expf(old - from)) + (top == now ? sum : sum * expf(top - from));
+    r.sum[i] = sum;
+    r.top[i] = now;
+    if (!last) return;
+    const float lse = now + logf(sum);
+    r.lse[i] = lse;
+    row_loss[i] = r.label[i] < 0 ? 0.f : lse - r.z_label[i];
+}
+
+// From a piece of logits, T threads to a row.
+template <int T>
+__global__ void __launch_bounds__(kThreads) class_sums_kernel(const float *z, int64_t b, int64_t cols, int64_t ld, int64_t c0, const float *bias,
+                                                              RowState r, bool last, float *row_loss) {
     constexpr int kRows = kThreads / T;
     __shared__ float sh[2][kThreads / 64];
     const int lane = threadIdx.x % T;
@@ -104,7 +118,7 @@ template <int T> __global__ void __launch_bounds__(kThreads) class_sums_kernel(c
 #pragma unroll
         for (int w = 0; w < T / 64; ++w) top = fmaxf(top, sh[0][w]);
     }
-    const float old = r.top[i], now = fmaxf(old, top), from = now == -INFINITY ? 0.f : now;
+    const float from = top == -INFINITY ? 0.f : top;
     float sum = 0.f;
     for (int64_t c = lane; c < cols; c += T) sum += expf(zi[c] + (bias ? bias[c0 + c] : 0.f) - from);
     sum = loss::wave_sum(sum);
@@ -116,59 +130,84 @@ template <int T> __global__ void __launch_bounds__(kThreads) class_sums_kernel(c
         for (int w = 0; w < T / 64; ++w) sum += sh[1][w];
     }
     if (lane != 0) return;
-    const float before = r.sum[i];
-    r.sum[i] = (old == now || before == 0.f ? before : before * expf(old - from)) + sum;
-    r.top[i] = now;
     const int64_t y = r.label[i] - c0;
     if (r.label[i] >= 0 && y >= 0 && y < cols) r.z_label[i] = zi[y] + (bias ? bias[c0 + y] : 0.f);
+    join_row(r, i, top, sum, last, row_loss);
 }
 
-__global__ void __launch_bounds__(kThreads) class_loss_kernel(CeArgs a, RowState r, float *row_loss) {
-    const int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-    if (i >= a.b) return;
-    const float lse = r.top[i] + logf(r.sum[i]);
-    r.lse[i] = lse;
-    row_loss[i] = r.label[i] < 0 ? 0.f : lse - r.z_label[i];
+// From the tiles' strips: 16 rows of a workgroup, each strip of a row to one of 16 threads.
+__global__ void __launch_bounds__(kThreads) class_join_kernel(const float2 *part, int64_t strips, int64_t b, RowState r, bool last, float *row_loss) {
+    __shared__ float2 sh[16][17];
+    const int x = threadIdx.x & 15, y = threadIdx.x >> 4;
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * 16 + x;
+    float top = -INFINITY, sum = 0.f;
+    auto take = [&](float2 v) {
+        const float now = fmaxf(top, v.x), from = now == -INFINITY ? 0.f : now;
+        sum = (top == now ? sum : sum * expf(top - from)) + (v.x == now ? v.y : v.y * expf(v.x - from));
+        top = now;
+    };
+    if (i < b) {
+#pragma unroll 4
+        for (int64_t p = y; p < strips; p += 16) take(part[p * b + i]);
+    }
+    sh[y][x] = make_float2(top, sum);
+    __syncthreads();
+    if (y != 0 || i >= b) return;
+#pragma unroll
+    for (int k = 1; k < 16; ++k) take(sh[k][x]);
+    join_row(r, i, top, sum, last, row_loss);
 }
 
-// The weighted sum of the rows' losses, in a fixed order.
-__global__ void __launch_bounds__(1024) class_total_kernel(const float *row_loss, const float *weight, int64_t b, float *loss) {
-    __shared__ float sh[16];
-    float s = 0.f;
-    for (int64_t i = threadIdx.x; i < b; i += 1024)
-        if (weight[i] != 0.f) s += row_loss[i] * weight[i];
+// The weighted sum of the rows' losses, in a fixed order, and the largest weight.
+__global__ void __launch_bounds__(1024) class_total_kernel(const float *row_loss, const float *weight, int64_t b, float *loss, float *scale) {
+    __shared__ float sh[2][16];
+    float s = 0.f, most = 0.f;
+    for (int64_t i = threadIdx.x; i < b; i += 1024) {
+        const float w = weight[i];
+        if (w != 0.f) s += row_loss[i] * w;
+        most = fmaxf(most, fabsf(w));
+    }
     s = loss::wave_sum(s);
-    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = s;
+    most = loss::wave_max(most);
+    if ((threadIdx.x & 63) == 0) {
+        sh[0][threadIdx.x >> 6] = s;
+        sh[1][threadIdx.x >> 6] = most;
+    }
     __syncthreads();
     if (threadIdx.x != 0) return;
-    float t = 0.f;
+    s = most = 0.f;
 #pragma unroll
-    for (int w = 0; w < 16; ++w) t += sh[w];
-    *loss = t;
+    for (int w = 0; w < 16; ++w) {
+        s += sh[0][w];
+        most = fmaxf(most, sh[1][w]);
+    }
+    *loss = s;
+    // (no weights, or so small that their reciprocal leaves fp32: dZ as it is)
+    *scale = most >= 0x1p-100f ? most : 1.f;
 }
 
-// dZ of a piece from its logits (in place where it is fp32), zeros in the columns up to ld,
-// and the column sums of a part of the rows.
+// dZ of a piece in place of its logits, zeros in the columns up to ld, and the column sums
+// of a part of the rows.
 constexpr int kStripe = 256;  // columns of a workgroup: 64 threads of 4, times 4 rows
-template <class T>
-__global__ void __launch_bounds__(kThreads) class_dz_kernel(const float *z, int64_t ldz, T *dz, int64_t ld, int64_t b, int64_t cols, int64_t c0,
-                                                            const float *bias, RowState r, float *part, int64_t parts) {
+__global__ void __launch_bounds__(kThreads) class_dz_kernel(float *z, int64_t ld, int64_t b, int64_t cols, int64_t c0, const float *bias, RowState r,
+                                                            const float *scale, float *part, int64_t parts) {
     __shared__ float sh[4][kStripe];
     const int64_t stripes = ceil_div(ld, int64_t(kStripe)), stripe = blockIdx.x % stripes, p = blockIdx.x / stripes;
     const int64_t per = ceil_div(b, parts), beg = min(b, p * per), end = min(b, beg + per);
     const int x = (threadIdx.x & 63) * 4, y = threadIdx.x >> 6;
     const int64_t c = stripe * kStripe + x;
+    const float inverse = 1.f / *scale;
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
     if (c < ld) {
         float bs[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) bs[e] = bias && c + e < cols ? bias[c0 + c + e] : 0.f;
         for (int64_t i = beg + y; i < end; i += 4) {
-            const float w = r.weight[i], lse = r.lse[i];
+            const float w = r.weight[i] * inverse, lse = r.lse[i];
             const int64_t label = r.label[i] - c0;
             float v[4] = {0.f, 0.f, 0.f, 0.f};
             if (w != 0.f) {
-                const float4 zz = *reinterpret_cast<const float4 *>(z + i * ldz + c);
+                const float4 zz = *reinterpret_cast<const float4 *>(z + i * ld + c);
                 v[0] = zz.x;
                 v[1] = zz.y;
                 v[2] = zz.z;
@@ -179,9 +218,7 @@ __global__ void __launch_bounds__(kThreads) class_dz_kernel(const float *z, int6
             }
 #pragma unroll
             for (int e = 0; e < 4; ++e) sum[e] += v[e];
-            row::Vec<T, 4> o;
-            o.set(v);
-            o.store(dz + i * ld + c);
+            *reinterpret_cast<float4 *>(z + i * ld + c) = make_float4(v[0], v[1], v[2], v[3]);
         }
     }
     if (!part) return;
@@ -189,20 +226,29 @@ __global__ void __launch_bounds__(kThreads) class_dz_kernel(const float *z, int6
     for (int e = 0; e < 4; ++e) sh[y][x + e] = sum[e];
     __syncthreads();
     const int64_t col = stripe * kStripe + threadIdx.x;
-    if (col >= cols) return;
+    if (col >= ld) return;
     float t = 0.f;
 #pragma unroll
     for (int k = 0; k < 4; ++k) t += sh[k][threadIdx.x];
-    part[p * cols + col] = t;
+    part[p * ld + col] = t;
 }
 
-__global__ void __launch_bounds__(kThreads) class_db_kernel(const float *part, int64_t parts, int64_t cols, float *db) {
-    const int64_t c = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-    if (c >= cols) return;
+// db of a piece: 32 columns of a workgroup, every eighth part to a thread.
+__global__ void __launch_bounds__(kThreads) class_db_kernel(const float *part, int64_t parts, int64_t ld, int64_t cols, const float *scale, float *db) {
+    __shared__ float sh[8][32];
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+    const int64_t c = static_cast<int64_t>(blockIdx.x) * 32 + x;
     float t = 0.f;
-#pragma unroll 8
-    for (int64_t p = 0; p < parts; ++p) t += part[p * cols + c];
-    db[c] = t;
+    if (c < cols)
+#pragma unroll 4
+        for (int64_t p = y; p < parts; p += 8) t += part[p * ld + c];
+    sh[y][x] = t;
+    __syncthreads();
+    if (y != 0 || c >= cols) return;
+    t = 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) t += sh[k][x];
+    db[c] = t * *scale;
 }
 
 // out = the partials in their order; rows of `ld` to rows of `cols`
@@ -230,25 +276,26 @@ gnn_status reduce(const float *part, int64_t nsplit, int64_t rows, int64_t cols,
 // ---------------------------------------------------------------------------
 // the call's buffers
 // ---------------------------------------------------------------------------
-constexpr int64_t kPiece = 1 << 27;  // logits of a piece, about
+constexpr int64_t kPiece = 1 << 27;  // values of a piece's dZ, about
 constexpr int64_t kPieceCols = 256;  // its columns: a multiple of these
+constexpr int64_t kSumsPieces = 8;   // such pieces that the bf16 sums take at once: a strip has 32 columns or more, its
+                                     // part 8 bytes a row, so that theirs fit in a piece of dZ
 
 int64_t row_of(int64_t n) { return (n + 7) / 8 * 8; }
 
 struct Plan {
     bool bf;
-    int64_t ldk, piece, pieces, parts;
-    int64_t da_splits, dw_splits_of[2];  // of a full piece and of the last one
-    size_t label, weight, top, sum, z_label, lse, row_loss, a, w, z, dz, db, dw_part, da_part, total;
+    int64_t ldk, piece, pieces, sums_piece, parts[2];
+    int64_t da_splits, dw_splits[2];  // of a full piece and of the last one
+    size_t label, weight, top, sum, z_label, lse, row_loss, scale, a, w, z, db, dw_part, da_part, total;
     Plan(int64_t b, int64_t k, int64_t c, int gemm_dt, bool grads) {
         bf = gemm_dt == GNN_BF16;
         ldk = row_of(k);
-        const int64_t all = static_cast<int64_t>(round_up(static_cast<size_t>(c), kPieceCols));
-        piece = std::min(all, std::max<int64_t>(kPiece / std::max<int64_t>(b, 1) / kPieceCols * kPieceCols, kPieceCols));
+        piece = std::min(row_of(c), std::max<int64_t>(kPiece / std::max<int64_t>(b, 1) / kPieceCols * kPieceCols, kPieceCols));
         pieces = ceil_div(c, piece);
+        sums_piece = std::min(row_of(c), bf ? kSumsPieces * piece : piece);
         const size_t es = bf ? 2 : 4;
-        const int64_t width = std::min(piece, row_of(c));
-        parts = std::max<int64_t>(1, std::min<int64_t>(ceil_div(2048, ceil_div(width, int64_t(kStripe))), ceil_div(b, int64_t(16))));
+        const int64_t last = row_of(c - (pieces - 1) * piece);
         auto splits = [&](Kind kind, int64_t m, int64_t n, int64_t r) {
             return bf ? splits_bf16(kind, m, n, r, true) : splits_f32(kind, m, n, r, true);
         };
@@ -261,19 +308,29 @@ struct Plan {
         z_label = rows();
         lse = rows();
         row_loss = rows();
+        scale = cv.take(4);
         a = cv.take(static_cast<size_t>(b * ldk) * es);
-        w = cv.take(static_cast<size_t>(width * ldk) * es);
-        z = cv.take(static_cast<size_t>(b * width) * 4);
-        dz = db = dw_part = da_part = 0;
-        da_splits = dw_splits_of[0] = dw_splits_of[1] = 1;
+        w = cv.take(static_cast<size_t>(piece * ldk) * es);
+        // one after the other: the sums' strips, dZ (bf16); logits and dZ (fp32)
+        int64_t strips = 0;
+        if (bf && b > 0)
+            for (const int64_t step : {piece, sums_piece})
+                for (int64_t c0 = 0; c0 < c; c0 += step) strips = std::max(strips, logit_strips(b, std::min(step, c - c0), ldk));
+        z = cv.take(std::max(static_cast<size_t>(b * strips) * 8, bf && !grads ? size_t(0) : static_cast<size_t>(b * piece) * es));
+        db = dw_part = da_part = 0;
+        da_splits = dw_splits[0] = dw_splits[1] = parts[0] = parts[1] = 1;
         if (grads) {
-            const int64_t last = row_of(c - (pieces - 1) * piece);
-            da_splits = splits(kNT, b, k, width);
-            dw_splits_of[0] = splits(kTT, width, k, b);
-            dw_splits_of[1] = splits(kTT, last, k, b);
-            dz = bf ? cv.take(static_cast<size_t>(b * width) * 2) : z;
-            db = cv.take(static_cast<size_t>(parts * width) * 4);
-            const int64_t dw = std::max(dw_splits_of[0] > 1 ? dw_splits_of[0] * width : 0, dw_splits_of[1] > 1 ? dw_splits_of[1] * last : 0);
+            const int64_t width[2] = {piece, last};
+            int64_t most = 0, dw = 0;
+            for (int i = 0; i < 2; ++i) {
+                parts[i] = bf ? logit_row_strips(b, width[i], ldk)
+                              : std::max<int64_t>(1, std::min<int64_t>(ceil_div(2048, ceil_div(width[i], int64_t(kStripe))), ceil_div(b, int64_t(16))));
+                most = std::max(most, parts[i] * width[i]);
+                dw_splits[i] = splits(kTT, width[i], k, b);
+                if (dw_splits[i] > 1) dw = std::max(dw, dw_splits[i] * width[i]);
+            }
+            da_splits = splits(kNT, b, k, piece);
+            db = cv.take(static_cast<size_t>(most) * 4);
             dw_part = cv.take(static_cast<size_t>(dw * ldk) * 4);
             da_part = cv.take(da_splits > 1 || pieces > 1 ? static_cast<size_t>(da_splits * b * ldk) * 4 : 0);
         }
@@ -293,88 +350,115 @@ gnn_status launch_update_ce(const CeArgs &a, void *ws, hipStream_t s) {
     const size_t es = dtype_size(gdt);
     auto f = [&](size_t at) { return reinterpret_cast<float *>(base + at); };
     const RowState r{reinterpret_cast<int32_t *>(base + pl.label), f(pl.weight), f(pl.top), f(pl.sum), f(pl.z_label), f(pl.lse)};
-    float *row_loss = a.row_loss ? a.row_loss : f(pl.row_loss);
-    if (a.b > 0) {
+    float *row_loss = a.row_loss ? a.row_loss : f(pl.row_loss), *scale = f(pl.scale), *z = f(pl.z);
+    const bool any = a.b > 0;
+    if (any) {
         class_rows_kernel<<<static_cast<unsigned>(ceil_div(a.b, int64_t(kThreads))), kThreads, 0, s>>>(a, r);
         GNN_LAUNCHED("update_ce_rows");
     }
     const void *A = a.a;
     int64_t lda = a.k;
     const bool rows16 = a.k * static_cast<int64_t>(es) % 16 == 0;
-    if (a.b > 0 && (a.dwt || a.adt != gdt || !rows16 || !aligned(a.a, 16))) {
+    if (any && (a.dwt || a.adt != gdt || !rows16 || !aligned(a.a, 16))) {
         GNN_TRY(pack(a.a, a.adt, a.b, a.k, pl.ldk, r.label, base + pl.a, gdt, s));
         A = base + pl.a;
         lda = pl.ldk;
     }
-    const bool copy_w = a.wdt != gdt || !rows16 || !aligned(a.wt, 16);
-    float *z = f(pl.z);
     // the weights' rows [c0, c0 + cols) as the products read them
-    auto weights = [&](int64_t c0, int64_t cols, const void **w, int64_t *ldw) -> gnn_status {
-        const char *from = static_cast<const char *>(a.wt) + c0 * a.k * static_cast<int64_t>(dtype_size(a.wdt));
-        *w = from;
-        *ldw = a.k;
+    const bool copy_w = a.wdt != gdt || !rows16 || !aligned(a.wt, 16);
+    const void *w = nullptr;
+    int64_t ldw = 0;
+    auto weights = [&](int64_t c0, int64_t cols) -> gnn_status {
+        w = static_cast<const char *>(a.wt) + c0 * a.k * static_cast<int64_t>(dtype_size(a.wdt));
+        ldw = a.k;
         if (!copy_w) return GNN_OK;
-        *w = base + pl.w;
-        *ldw = pl.ldk;
-        return pack(from, a.wdt, cols, a.k, pl.ldk, nullptr, base + pl.w, gdt, s);
+        GNN_TRY(pack(w, a.wdt, cols, a.k, pl.ldk, nullptr, base + pl.w, gdt, s));
+        w = base + pl.w;
+        ldw = pl.ldk;
+        return GNN_OK;
     };
-    auto product = [&](Kind kind, const Product &p) { return gdt == GNN_BF16 ? product_bf16(kind, p, s) : product_f32(kind, p, s); };
-    auto logits = [&](const void *w, int64_t ldw, int64_t cols) {
-        const int64_t K = std::min(lda, ldw), ld = row_of(cols);
-        return product(kNN, Product{A, w, lda, ldw, a.b, cols, K, K, z, GNN_F32, ld, 1, 0, false});
+    auto product = [&](Kind kind, const Product &p) { return pl.bf ? product_bf16(kind, p, s) : product_f32(kind, p, s); };
+    auto logits = [&](int64_t cols) {
+        const int64_t K = std::min(lda, ldw);
+        return product(kNN, Product{A, w, lda, ldw, a.b, cols, K, K, z, GNN_F32, row_of(cols), 1, 0, false, nullptr});
     };
-    if (a.b > 0) {
-        for (int64_t q = 0; q < pl.pieces; ++q) {
-            const int64_t c0 = q * pl.piece, cols = std::min(pl.piece, a.c - c0), ld = row_of(cols);
-            const void *w;
-            int64_t ldw;
-            GNN_TRY(weights(c0, cols, &w, &ldw));
-            GNN_TRY(logits(w, ldw, cols));
-            if (cols <= 1024) class_sums_kernel<64><<<static_cast<unsigned>(ceil_div(a.b, int64_t(4))), kThreads, 0, s>>>(z, a.b, cols, ld, c0, a.bias, r);
-            else class_sums_kernel<256><<<static_cast<unsigned>(a.b), kThreads, 0, s>>>(z, a.b, cols, ld, c0, a.bias, r);
-            GNN_LAUNCHED("update_ce_sums");
+    auto tile_args = [&](int64_t c0, int64_t cols) {
+        return LogitArgs{static_cast<const uint16_t *>(A), static_cast<const uint16_t *>(w), lda, ldw, a.b, cols, std::min(lda, ldw), c0,
+                         a.bias ? a.bias + c0 : nullptr, r, reinterpret_cast<float2 *>(z), reinterpret_cast<uint16_t *>(z), row_of(cols), scale,
+                         a.db ? f(pl.db) : nullptr};
+    };
+    // (copies of the weights are a piece's)
+    const int64_t step = copy_w ? pl.piece : pl.sums_piece;
+    for (int64_t c0 = 0; any && c0 < a.c; c0 += step) {
+        const int64_t cols = std::min(step, a.c - c0);
+        const bool last = c0 + cols == a.c;
+        GNN_TRY(weights(c0, cols));
+        if (pl.bf) {
+            const LogitArgs t = tile_args(c0, cols);
+            GNN_TRY(logit_sums(t, s));
+            class_join_kernel<<<static_cast<unsigned>(ceil_div(a.b, int64_t(16))), kThreads, 0, s>>>(t.part, logit_strips(a.b, cols, t.R), a.b, r, last,
+                                                                                                  row_loss);
+            GNN_LAUNCHED("update_ce_join");
+            continue;
         }
-        class_loss_kernel<<<static_cast<unsigned>(ceil_div(a.b, int64_t(kThreads))), kThreads, 0, s>>>(a, r, row_loss);
-        GNN_LAUNCHED("update_ce_loss");
+        GNN_TRY(logits(cols));
+        const int64_t ld = row_of(cols);
+        if (cols <= 1024)
+            class_sums_kernel<64><<<static_cast<unsigned>(ceil_div(a.b, int64_t(4))), kThreads, 0, s>>>(z, a.b, cols, ld, c0, a.bias, r, last, row_loss);
+        else class_sums_kernel<256><<<static_cast<unsigned>(a.b), kThreads, 0, s>>>(z, a.b, cols, ld, c0, a.bias, r, last, row_loss);
+        GNN_LAUNCHED("update_ce_sums");
     }
-    class_total_kernel<<<1, 1024, 0, s>>>(row_loss, r.weight, a.b, a.loss_out);
+    class_total_kernel<<<1, 1024, 0, s>>>(row_loss, r.weight, a.b, a.loss_out, scale);
     GNN_LAUNCHED("update_ce_total");
     if (!grads) return GNN_OK;
-    void *dz = base + pl.dz;
     for (int64_t q = 0; q < pl.pieces; ++q) {
         const int64_t c0 = q * pl.piece, cols = std::min(pl.piece, a.c - c0), ld = row_of(cols);
-        const void *w;
-        int64_t ldw;
-        if (pl.pieces > 1 || a.d_a) GNN_TRY(weights(c0, cols, &w, &ldw));
-        if (a.b > 0) {
-            if (pl.pieces > 1) GNN_TRY(logits(w, ldw, cols));
-            const unsigned grid = static_cast<unsigned>(ceil_div(ld, int64_t(kStripe)) * pl.parts);
-            float *part = a.db ? f(pl.db) : nullptr;
-            if (pl.bf) class_dz_kernel<<<grid, kThreads, 0, s>>>(z, ld, static_cast<uint16_t *>(dz), ld, a.b, cols, c0, a.bias, r, part, pl.parts);
-            else class_dz_kernel<<<grid, kThreads, 0, s>>>(z, ld, static_cast<float *>(dz), ld, a.b, cols, c0, a.bias, r, part, pl.parts);
+        const int which = q + 1 < pl.pieces ? 0 : 1;
+        // (a single piece's weights are still there, and in fp32 its logits)
+        const bool again = pl.pieces > 1;
+        if (any && again) GNN_TRY(weights(c0, cols));
+        if (any && pl.bf) {
+            GNN_TRY(logit_dz(tile_args(c0, cols), s));
+        } else if (any) {
+            if (again) GNN_TRY(logits(cols));
+            class_dz_kernel<<<static_cast<unsigned>(ceil_div(ld, int64_t(kStripe)) * pl.parts[which]), kThreads, 0, s>>>(
+                z, ld, a.b, cols, c0, a.bias, r, scale, a.db ? f(pl.db) : nullptr, pl.parts[which]);
             GNN_LAUNCHED("update_ce_dz");
         }
         if (a.db) {
-            class_db_kernel<<<static_cast<unsigned>(ceil_div(cols, int64_t(kThreads))), kThreads, 0, s>>>(f(pl.db), a.b > 0 ? pl.parts : 0, cols, a.db + c0);
+            class_db_kernel<<<static_cast<unsigned>(ceil_div(cols, int64_t(32))), kThreads, 0, s>>>(f(pl.db), any ? pl.parts[which] : 0, ld, cols, scale,
+                                                                                                  a.db + c0);
             GNN_LAUNCHED("update_ce_db");
         }
         if (a.dwt) {
-            const int64_t n = q + 1 < pl.pieces ? pl.dw_splits_of[0] : pl.dw_splits_of[1];
+            const int64_t n = pl.dw_splits[which];
             char *to = static_cast<char *>(a.dwt) + c0 * a.k * static_cast<int64_t>(dtype_size(a.dwdt));
-            if (n == 1) {
-                GNN_TRY(product(kTT, Product{dz, A, ld, lda, cols, a.k, a.b, a.b, to, a.dwdt, a.k, 1, 0, false}));
-            } else {
-                GNN_TRY(product(kTT, Product{dz, A, ld, lda, cols, a.k, a.b, a.b, base + pl.dw_part, GNN_F32, pl.ldk, n, cols * pl.ldk, false}));
-                GNN_TRY(reduce(f(pl.dw_part), n, cols, a.k, pl.ldk, to, a.dwdt, s));
+            Product p{z, A, ld, lda, cols, a.k, a.b, a.b, to, a.dwdt, a.k, 1, 0, false, scale};
+            if (n > 1) {
+                p.out = base + pl.dw_part;
+                p.odt = GNN_F32;
+                p.ld = pl.ldk;
+                p.nsplit = n;
+                p.split_stride = cols * pl.ldk;
             }
+            GNN_TRY(product(kTT, p));
+            if (n > 1) GNN_TRY(reduce(f(pl.dw_part), n, cols, a.k, pl.ldk, to, a.dwdt, s));
         }
-        if (a.d_a && a.b > 0) {
+        if (a.d_a && any) {
             const bool whole = pl.pieces == 1 && pl.da_splits == 1;
-            GNN_TRY(product(kNT, Product{dz, w, ld, ldw, a.b, a.k, ld, cols, whole ? a.d_a : base + pl.da_part, whole ? a.gdt : static_cast<int>(GNN_F32),
-                                         whole ? a.k : pl.ldk, pl.da_splits, a.b * pl.ldk, q > 0}));
+            Product p{z, w, ld, ldw, a.b, a.k, ld, cols, a.d_a, a.gdt, a.k, 1, 0, false, scale};
+            if (!whole) {
+                p.out = base + pl.da_part;
+                p.odt = GNN_F32;
+                p.ld = pl.ldk;
+                p.nsplit = pl.da_splits;
+                p.split_stride = a.b * pl.ldk;
+                p.add = q > 0;
+            }
+            GNN_TRY(product(kNT, p));
         }
     }
-    if (a.d_a && a.b > 0 && (pl.pieces > 1 || pl.da_splits > 1))
+    if (a.d_a && any && (pl.pieces > 1 || pl.da_splits > 1))
         GNN_TRY(reduce(f(pl.da_part), pl.da_splits, a.b, a.k, pl.ldk, a.d_a, a.gdt, s));
     return GNN_OK;
 }

@@ -39,9 +39,11 @@ template <int TILE, bool TX, bool TY> __global__ void __launch_bounds__(gemm::kT
     const int64_t gc = col0 + TileOut<TILE, TILE>::col(), M = p.M, N = p.N, ld = p.ld;
     float *out = static_cast<float *>(p.out) + blockIdx.z * p.split_stride;
     const bool add = p.add;
+    const float factor = p.factor ? *p.factor : 1.f;
     emit_tile(acc, lds, [&](int, int r, int, float4 v) {
         const int64_t gr = row0 + r;
         if (gr >= M || gc >= N) return;
+        v = make_float4(v.x * factor, v.y * factor, v.z * factor, v.w * factor);
         if (add) {
             const float4 o = load4_clamped<false>(out, gr * ld, gc, N);
             v = make_float4(v.x + o.x, v.y + o.y, v.z + o.z, v.w + o.w);

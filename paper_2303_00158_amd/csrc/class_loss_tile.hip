@@ -7,6 +7,49 @@ namespace closs {
 
 namespace {
 
+constexpr float kLog2e = 1.4426950408889634f;
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Of two neighbouring MFMA tiles' columns (j, j + 1) of tile row i a lane holds four each;
+// after an exchange with the lane 16 away it holds eight consecutive ones of
+// one of the two: x[e] is column 16 (2 j + (g & 1)) + 8 (g >> 1) + e, g = lane / 16.
+__device__ __forceinline__ void eight_of(const tile::f32x4 &lo, const tile::f32x4 &hi, float (&x)[8]) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const auto two = __builtin_amdgcn_permlane16_swap(__float_as_uint(lo[q]), __float_as_uint(hi[q]), false, false);
+        x[q] = __uint_as_float(two[0]);
+        x[q + 4] = __uint_as_float(two[1]);
+    }
+}
+
+// A wavefront's part of an output tile times `factor`, from (row0, col0).
+template <class C, class T>
+__device__ __forceinline__ void put_tile(const tile::Acc<C> &acc, const Product &p, T *out, float factor, int64_t row0, int64_t col0) {
+    const int lane = threadIdx.x & 63, g = lane >> 4;
+    const int64_t r0 = row0 + (lane & 15), c0 = col0 + (g & 1) * 16 + (g >> 1) * 8;
+#pragma unroll
+    for (int i = 0; i < C::MI; ++i) {
+        const int64_t r = r0 + 16 * i;
+#pragma unroll
+        for (int j = 0; j < C::NI / 2; ++j) {
+            float x[8];
+            eight_of(acc.v[i][2 * j], acc.v[i][2 * j + 1], x);
+            const int64_t c = c0 + 32 * j, at = r * p.ld + c, room = p.ld - c;
+            if (r >= p.M || room <= 0) continue;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] *= factor;
+            if constexpr (sizeof(T) == 4)
+                if (p.add) {
+                    row::Vec<float, 8> o;
+                    o.load_upto(out + at, room);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] += o.get(e);
+                }
+            tile::put8(out + at, room, x);
+        }
+    }
+}
+
 template <class C, bool TX, bool TY, class T>
 __global__ void __launch_bounds__(C::kThreads, C::PER_CU) class_product_kernel(Product p) {
     __shared__ __attribute__((aligned(16))) uint16_t st0[C::kStageElems], st1[C::kStageElems];
@@ -28,10 +71,154 @@ __global__ void __launch_bounds__(C::kThreads, C::PER_CU) class_product_kernel(P
     const tile::Ring ring{{st0, st1}};
     if (red > 0) tile::Product<C, TX, TY>(ox, oy).run(acc, ring, static_cast<int>(ceil_div(red, int64_t(tile::kBK))));
     const int wave = threadIdx.x >> 6;
-    T *out = static_cast<T *>(p.out) + split * p.split_stride;
-    // (rows are `ld` long in memory and the output's N columns are all stored up to there)
-    const tile::Epilogue ep{nullptr, p.add ? out : nullptr, nullptr, out, p.ld};
-    tile::finish<C, GNN_ACT_NONE, T>(acc, ep, row0 + (wave >> 1) * 16 * C::MI, col0 + (wave & 1) * 16 * C::NI, p.M);
+    put_tile<C, T>(acc, p, static_cast<T *>(p.out) + split * p.split_stride, p.factor ? *p.factor : 1.f,
+                   row0 + (wave >> 1) * 16 * C::MI, col0 + (wave & 1) * 16 * C::NI);
+}
+
+// ---------------------------------------------------------------------------
+// logits that stay in the accumulators
+// ---------------------------------------------------------------------------
+// A tile of logits, and this wavefront's part of it.
+template <class C> struct LogitTile {
+    int64_t row0, col0, row_strip, col_strip;
+    __device__ __forceinline__ bool run(const LogitArgs &a, const tile::Ring &ring, tile::Acc<C> &acc) {
+        const int64_t tm = ceil_div(a.M, int64_t(C::BM)), tn = ceil_div(a.N, int64_t(C::BN));
+        const int64_t t = wide::xcd_item(blockIdx.x, tm * tn);
+        if (t < 0) return false;
+        int64_t m, n;
+        tile::tile_of(t, tm, tn, &m, &n);
+        row0 = m * C::BM;
+        col0 = n * C::BN;
+        const tile::Operand ox{a.x + row0 * a.ldx, nullptr, a.ldx, 0, a.M - row0, a.R};
+        const tile::Operand oy{a.y + col0 * a.ldy, nullptr, a.ldy, 0, a.N - col0, a.R};
+        acc.clear();
+        tile::Product<C, false, false>(ox, oy).template run<true>(acc, ring, static_cast<int>(ceil_div(a.R, int64_t(tile::kBK))));
+        const int wave = threadIdx.x >> 6;
+        row_strip = 2 * m + (wave >> 1);
+        col_strip = 2 * n + (wave & 1);
+        row0 += (wave >> 1) * 16 * C::MI;
+        col0 += (wave & 1) * 16 * C::NI;
+        return true;
+    }
+    // the biases of this lane's columns: 16 j + 4 (lane / 16) + q
+    __device__ __forceinline__ void biases(const LogitArgs &a, float (&b)[C::NI][4]) const {
+        const int64_t c0 = col0 + 4 * ((threadIdx.x & 63) >> 4);
+#pragma unroll
+        for (int j = 0; j < C::NI; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) b[j][q] = a.bias && c0 + 16 * j + q < a.N ? a.bias[c0 + 16 * j + q] : 0.f;
+    }
+    // column of the row's label in this wavefront's part, or -1
+    __device__ __forceinline__ int label_at(const LogitArgs &a, int64_t r) const {
+        const int64_t y = r < a.M ? static_cast<int64_t>(a.rows.label[r]) - a.c0 - col0 : -1;
+        return y >= 0 && y < 16 * C::NI ? static_cast<int>(y) : -1;
+    }
+};
+
+// Largest logit of each row among a wavefront's columns, and the sum of exp(z - largest):
+// each lane's own first (of 4 NI columns), then those of the four lanes that share the row.
+template <class C> __global__ void __launch_bounds__(C::kThreads, C::PER_CU) class_sums_tile_kernel(LogitArgs a) {
+    __shared__ __attribute__((aligned(16))) uint16_t st0[C::kStageElems], st1[C::kStageElems];
+    tile::Acc<C> acc;
+    LogitTile<C> at;
+    if (!at.run(a, tile::Ring{{st0, st1}}, acc)) return;
+    const int lane = threadIdx.x & 63, g = lane >> 4;
+    float bias[C::NI][4];
+    at.biases(a, bias);
+    const int left = static_cast<int>(min(a.N - at.col0, int64_t(16 * C::NI)));  // columns there
+#pragma unroll
+    for (int i = 0; i < C::MI; ++i) {
+        const int64_t r = at.row0 + 16 * i + (lane & 15);
+        float x[C::NI][4], top = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < C::NI; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                x[j][q] = 16 * j + 4 * g + q < left ? acc.v[i][j][q] + bias[j][q] : -INFINITY;
+                top = fmaxf(top, x[j][q]);
+            }
+        const int y = at.label_at(a, r);
+        if (__any(y >= 0)) {
+#pragma unroll
+            for (int j = 0; j < C::NI; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    if (y == 16 * j + 4 * g + q) a.rows.z_label[r] = x[j][q];
+        }
+        const float from = top == -INFINITY ? 0.f : top;
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < C::NI; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) sum += exp2_of((x[j][q] - from) * kLog2e);
+        float all = fmaxf(top, __shfl_xor(top, 16, 64));
+        all = fmaxf(all, __shfl_xor(all, 32, 64));
+        sum *= top == all ? 1.f : exp2_of((top - all) * kLog2e);
+        sum += __shfl_xor(sum, 16, 64);
+        sum += __shfl_xor(sum, 32, 64);
+        if (g == 0 && r < a.M) a.part[at.col_strip * a.M + r] = make_float2(all, sum);
+    }
+}
+
+// dZ over the largest weight, in bf16, and its column sums over a wavefront's rows.
+template <class C> __global__ void __launch_bounds__(C::kThreads, C::PER_CU) class_dz_tile_kernel(LogitArgs a) {
+    __shared__ __attribute__((aligned(16))) uint16_t st0[C::kStageElems], st1[C::kStageElems];
+    tile::Acc<C> acc;
+    LogitTile<C> at;
+    if (!at.run(a, tile::Ring{{st0, st1}}, acc)) return;
+    const int lane = threadIdx.x & 63, g = lane >> 4;
+    float bias[C::NI][4], sum[C::NI][4];
+    at.biases(a, bias);
+#pragma unroll
+    for (int j = 0; j < C::NI; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) sum[j][q] = 0.f;
+    const float inverse = 1.f / *a.scale;
+    const int left = static_cast<int>(min(a.N - at.col0, int64_t(16 * C::NI)));
+#pragma unroll
+    for (int i = 0; i < C::MI; ++i) {
+        const int64_t r = at.row0 + 16 * i + (lane & 15);
+        const bool in = r < a.M;
+        const float w = in ? a.rows.weight[r] * inverse : 0.f, lse = in ? a.rows.lse[r] : 0.f;
+        tile::f32x4 d[C::NI];
+#pragma unroll
+        for (int j = 0; j < C::NI; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const float p = exp2_of((acc.v[i][j][q] + bias[j][q] - lse) * kLog2e);
+                d[j][q] = w != 0.f && 16 * j + 4 * g + q < left ? w * p : 0.f;
+            }
+        const int y = at.label_at(a, r);
+        if (__any(y >= 0)) {
+#pragma unroll
+            for (int j = 0; j < C::NI; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    if (y == 16 * j + 4 * g + q) d[j][q] -= w;
+        }
+#pragma unroll
+        for (int j = 0; j < C::NI; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) sum[j][q] += d[j][q];
+#pragma unroll
+        for (int j = 0; j < C::NI / 2; ++j) {
+            float x[8];
+            eight_of(d[2 * j], d[2 * j + 1], x);
+            const int64_t c = at.col0 + (g & 1) * 16 + (g >> 1) * 8 + 32 * j;
+            if (in && c < a.ld) tile::put8(a.dz + r * a.ld + c, 8, x);  // ld is a multiple of 8
+        }
+    }
+    if (!a.db_part) return;
+#pragma unroll
+    for (int j = 0; j < C::NI; ++j) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int o = 8; o > 0; o >>= 1) sum[j][q] += __shfl_xor(sum[j][q], o, 64);
+        const int64_t c = at.col0 + 16 * j + 4 * g;
+        if ((lane & 15) == 0 && c < a.ld)
+            *reinterpret_cast<float4 *>(a.db_part + at.row_strip * a.ld + c) = make_float4(sum[j][0], sum[j][1], sum[j][2], sum[j][3]);
+    }
 }
 
 tile::Choice choice(Kind kind, int64_t M, int64_t N, int64_t R, bool may_split) {
@@ -83,6 +270,49 @@ gnn_status product_bf16(Kind kind, const Product &p, hipStream_t s) {
         }
     };
     return kind == kNT ? go(std::true_type{}) : go(std::false_type{});
+}
+
+namespace {
+
+// go(tag of the tile of a piece's logits)
+template <class F> auto with_logit_tile(int64_t M, int64_t N, int64_t R, F &&go) {
+    switch (tile::choose(M, N, R, 1).pick) {
+        case tile::kBig: return go(tile::Big{});
+        case tile::kBig7: return go(tile::Big7{});
+        case tile::kMid: return go(tile::Mid{});
+        default: return go(tile::Small{});
+    }
+}
+
+}  // namespace
+
+int64_t logit_strips(int64_t M, int64_t N, int64_t R) {
+    return with_logit_tile(M, N, R, [&](auto c) { return 2 * ceil_div(N, int64_t(decltype(c)::BN)); });
+}
+int64_t logit_row_strips(int64_t M, int64_t N, int64_t R) {
+    return with_logit_tile(M, N, R, [&](auto c) { return 2 * ceil_div(M, int64_t(decltype(c)::BM)); });
+}
+
+gnn_status logit_sums(const LogitArgs &a, hipStream_t s) {
+    return with_logit_tile(a.M, a.N, a.R, [&](auto c) -> gnn_status {
+        using C = decltype(c);
+        const int64_t grid = static_cast<int64_t>(round_up(ceil_div(a.M, int64_t(C::BM)) * ceil_div(a.N, int64_t(C::BN)), wide::kXcds));
+        GNN_CHECK(grid <= kMaxGrid / C::kThreads, GNN_ESIZE, "update_ce: sizes exceed the grid limit");
+        class_sums_tile_kernel<C><<<static_cast<unsigned>(grid), C::kThreads, 0, s>>>(a);
+        GNN_LAUNCHED("update_ce_sums");
+        return GNN_OK;
+    });
+}
+
+gnn_status logit_dz(const LogitArgs &a, hipStream_t s) {
+    return with_logit_tile(a.M, a.N, a.R, [&](auto c) -> gnn_status {
+        using C = decltype(c);
+        const int64_t grid = static_cast<int64_t>(round_up(ceil_div(a.M, int64_t(C::BM)) * ceil_div(a.N, int64_t(C::BN)), wide::kXcds));
+        GNN_CHECK(grid <= kMaxGrid / C::kThreads, GNN_ESIZE, "update_ce: sizes exceed the grid limit");
+        class_dz_tile_kernel<C><<<static_cast<unsigned>(grid), C::kThreads, 0, s>>>(a);
+        GNN_LAUNCHED("update_ce_dz");
+        return GNN_OK;
+    });
 }
 
 }  // namespace closs

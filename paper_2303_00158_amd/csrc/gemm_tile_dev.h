@@ -305,8 +305,11 @@ template <class C, bool TA, bool TB> struct Product {
 
     // acc += the product over `chunks` chunks.  Copies past the last chunk are
     // of zeros; an odd count multiplies one chunk of them (with the last chunk
-    // in code of its own, the compiler moved accumulators about).
-    __device__ __forceinline__ void run(Acc<C> &acc, const Ring &ring, int chunks) const {
+    // in code of its own, the compiler moved accumulators about).  MOVES: what follows
+    // may make the compiler move accumulators on the loop's way out, in front
+    // of settle()'s wait (an epilogue with branches did), so the loop's end waits
+    // itself: 18 states of some 5,400 cycles.
+    template <bool MOVES = false> __device__ __forceinline__ void run(Acc<C> &acc, const Ring &ring, int chunks) const {
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
@@ -318,6 +321,7 @@ template <class C, bool TA, bool TB> struct Product {
         for (int c = 0; c < chunks; c += 2) {
             step<0>(acc, f, ring, c);
             step<1>(acc, f, ring, c + 1);
+            if constexpr (MOVES) asm volatile("s_nop 15\n\ts_nop 1" ::: "memory");
         }
         wide::chunk_barrier<wide::waitcnt(0, 0)>();  // the stages are drained
         settle(acc);
