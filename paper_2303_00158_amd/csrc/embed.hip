@@ -100,20 +100,91 @@ template <class F> void with_types(int idt, int odt, F &&go) {
 // the gradient: positions sorted by id
 // ---------------------------------------------------------------------------
 // Keys are ids; what names no row, and positions at or past the count, get the
-// key `rows` and come last.  Eight bits a pass, least first: a launch counts each
-// tile's digits, the next moves the tile's pairs behind the places of all
-// smaller digits, and of the same digit in earlier tiles.
+// key `rows` and come last.  A stable radix sort, least digit first.  Up to kSortTile
+// positions one workgroup does all of it in LDS (8,192 positions of 32,000 rows: 36 us in
+// four launches, SORT1 in this one).  More take two launches a digit: one counts each
+// tile's digits, the next moves the tile's pairs behind all smaller digits and behind
+// the same digit in earlier tiles, adding up the tiles' counts by itself.
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kSortKeys = 8;
 constexpr int kSortTile = kSortThreads * kSortKeys;
-constexpr int kBits = 8, kBins = 1 << kBits;
 
 struct SortArgs {
     const int64_t *ids, *n_dev;
     int64_t cap, rows;
     uint32_t *key[2], *pos[2];
-    uint32_t *counts;  // kBins x tiles
+    uint32_t *counts;  // tiles x bins
     int64_t tiles;
     int passes;
+};
+
+// Digits of BITS bits, and the counts of a tile's wavefronts.
+template <int BITS> struct Digits {
+    static constexpr int kBins = 1 << BITS;
+    typedef uint32_t WaveBins[kSortWaves][kBins];
+    __device__ __forceinline__ static uint32_t of(uint32_t key, int pass) { return (key >> (BITS * pass)) & (kBins - 1); }
+
+    // own[k] = how many of the wavefront's earlier elements (of smaller k, or in a lower lane)
+    // have the digit of its element k; bins[wave] = the wavefront's counts.
+    __device__ __forceinline__ static void rank(const uint32_t (&digit)[kSortKeys], const bool (&in)[kSortKeys], int rounds, WaveBins &bins,
+                                                uint32_t (&own)[kSortKeys]) {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        for (int i = threadIdx.x; i < kSortWaves * kBins; i += kSortThreads) (&bins[0][0])[i] = 0;
+        __syncthreads();
+        volatile uint32_t *mine = bins[wave];
+#pragma unroll
+        for (int k = 0; k < kSortKeys; ++k) {
+            if (k >= rounds) break;
+            uint64_t same = __ballot(in[k]);
+#pragma unroll
+            for (int b = 0; b < BITS; ++b) {
+                const uint64_t set = __ballot((digit[k] >> b) & 1);
+                same &= (digit[k] >> b) & 1 ? set : ~set;
+            }
+            const uint64_t below = same & ((1ull << lane) - 1);
+            const uint32_t before = in[k] ? mine[digit[k]] : 0;
+            own[k] = before + __popcll(below);
+            __builtin_amdgcn_wave_barrier();
+            if (in[k] && below == 0) mine[digit[k]] = before + __popcll(same);
+            __builtin_amdgcn_wave_barrier();
+        }
+        __syncthreads();
+    }
+
+    // bins[w][d] becomes the place of wavefront w's first element of digit d, where all
+    // smaller digits take `total` places of theirs and digit d starts `earlier` places on.
+    // total and earlier: of the digits that threads 0 .. kSortThreads hold, kEach each.
+    static constexpr int kEach = kBins > kSortThreads ? kBins / kSortThreads : 1;
+    __device__ __forceinline__ static void place(WaveBins &bins, const uint32_t (&total)[kEach], const uint32_t (&earlier)[kEach],
+                                                 uint32_t *sh) {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        uint32_t mine = 0;
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) mine += total[e];
+        uint32_t sum = mine;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const uint32_t y = __shfl_up(sum, o, 64);
+            if (lane >= o) sum += y;
+        }
+        if (lane == 63) sh[wave] = sum;
+        __syncthreads();
+        uint32_t at = sum - mine;
+        for (int w = 0; w < wave; ++w) at += sh[w];
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            const int d = threadIdx.x * kEach + e;
+            if (d < kBins) {
+                uint32_t to = at + earlier[e];
+                for (int w = 0; w < kSortWaves; ++w) {
+                    const uint32_t c = bins[w][d];
+                    bins[w][d] = to;
+                    to += c;
+                }
+            }
+            at += total[e];
+        }
+        __syncthreads();
+    }
 };
 
 __device__ __forceinline__ uint32_t key_of(const SortArgs &a, int64_t i, int64_t n) {
@@ -121,123 +192,170 @@ __device__ __forceinline__ uint32_t key_of(const SortArgs &a, int64_t i, int64_t
     const int64_t id = a.ids[i];
     return static_cast<uint32_t>(id >= 0 && id < a.rows ? id : a.rows);
 }
-// Element k of this thread's: a wavefront's elements are consecutive, 64 to a round.
-__device__ __forceinline__ int64_t sort_at(int64_t tile, int k) {
-    return tile * kSortTile + (threadIdx.x >> 6) * (64 * kSortKeys) + k * 64 + (threadIdx.x & 63);
+// Element k of this thread: a wavefront's elements are consecutive, 64 to a round.
+__device__ __forceinline__ int64_t sort_at(int64_t tile, int rounds, int k) {
+    return tile * kSortTile + (threadIdx.x >> 6) * (64 * rounds) + k * 64 + (threadIdx.x & 63);
 }
 
-__global__ void __launch_bounds__(kSortThreads) embed_count_kernel(SortArgs a, int pass) {
-    __shared__ uint32_t bins[kBins];
-    const int64_t n = row::live_rows(a.n_dev, a.cap), tile = blockIdx.x;
-    if (threadIdx.x < kBins) bins[threadIdx.x] = 0;
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < kSortKeys; ++k) {
-        const int64_t i = sort_at(tile, k);
-        if (i >= a.cap) continue;
-        uint32_t x;
-        if (pass == 0) {
-            x = key_of(a, i, n);
-            a.key[0][i] = x;
-            a.pos[0][i] = static_cast<uint32_t>(i);
-        } else {
-            x = a.key[pass & 1][i];
-        }
-        atomicAdd(&bins[(x >> (kBits * pass)) & (kBins - 1)], 1u);
-    }
-    __syncthreads();
-    if (threadIdx.x < kBins) a.counts[threadIdx.x * a.tiles + tile] = bins[threadIdx.x];
-}
-
-// Exclusive sums of one value of each of the first kBins threads.
-__device__ __forceinline__ uint32_t scan_bins(uint32_t x, uint32_t *sh) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    uint32_t sum = x;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t y = __shfl_up(sum, o, 64);
-        if (lane >= o) sum += y;
-    }
-    if (threadIdx.x < kBins && lane == 63) sh[wave] = sum;
-    __syncthreads();
-    uint32_t before = 0;
-    for (int w = 0; w < kBins / 64; ++w)
-        if (w < wave) before += sh[w];
-    return before + sum - x;
-}
-
-// Places of this thread's keys among their tile's equal digits, in the order of their
-// elements: a wavefront counts its own rounds in `mine`, and start[wave][digit]
-// becomes the place of the wavefront's first one.
-struct Ranks {
-    uint32_t own[kSortKeys];
-};
-typedef uint32_t WaveBins[kSortWaves][kBins];
-__device__ __forceinline__ void rank_digits(const uint32_t (&digit)[kSortKeys], const bool (&in)[kSortKeys], WaveBins &bins, Ranks &r) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (int i = threadIdx.x; i < kSortWaves * kBins; i += kSortThreads) bins[i / kBins][i % kBins] = 0;
-    __syncthreads();
-    volatile uint32_t *mine = bins[wave];
-#pragma unroll
-    for (int k = 0; k < kSortKeys; ++k) {
-        uint64_t same = __ballot(in[k]);
-#pragma unroll
-        for (int b = 0; b < kBits; ++b) {
-            const uint64_t set = __ballot((digit[k] >> b) & 1);
-            same &= (digit[k] >> b) & 1 ? set : ~set;
-        }
-        const uint64_t below = same & ((1ull << lane) - 1);
-        const uint32_t before = in[k] ? mine[digit[k]] : 0;
-        r.own[k] = before + __popcll(below);
-        __builtin_amdgcn_wave_barrier();
-        if (in[k] && below == 0) mine[digit[k]] = before + __popcll(same);
-        __builtin_amdgcn_wave_barrier();
-    }
-    __syncthreads();
-}
-
-__global__ void __launch_bounds__(kSortThreads) embed_move_kernel(SortArgs a, int pass) {
-    __shared__ WaveBins bins;
-    __shared__ uint32_t sh[kBins / 64];
-    const int64_t tile = blockIdx.x;
-    const uint32_t *key = a.key[pass & 1], *pos = a.pos[pass & 1];
-    uint32_t x[kSortKeys], p[kSortKeys], digit[kSortKeys];
+constexpr int kOneBits = 9;
+__global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(SortArgs a) {
+    using D = Digits<kOneBits>;
+    __shared__ D::WaveBins bins;
+    __shared__ uint32_t keys[kSortTile], places[kSortTile], sh[kSortWaves];
+    const int64_t n = row::live_rows(a.n_dev, a.cap);
+    const int rounds = static_cast<int>(ceil_div(a.cap, int64_t(kSortThreads)));
+    uint32_t x[kSortKeys], p[kSortKeys], digit[kSortKeys], own[kSortKeys];
     bool in[kSortKeys];
 #pragma unroll
     for (int k = 0; k < kSortKeys; ++k) {
-        const int64_t i = sort_at(tile, k);
+        const int64_t i = sort_at(0, rounds, k);
+        in[k] = k < rounds && i < a.cap;
+        x[k] = in[k] ? key_of(a, i, n) : 0;
+        p[k] = static_cast<uint32_t>(i);
+    }
+    for (int pass = 0; pass < a.passes; ++pass) {
+#pragma unroll
+        for (int k = 0; k < kSortKeys; ++k) digit[k] = D::of(x[k], pass);
+        D::rank(digit, in, rounds, bins, own);
+        uint32_t total[1] = {0}, none[1] = {0};
+        if (threadIdx.x < D::kBins)
+            for (int w = 0; w < kSortWaves; ++w) total[0] += bins[w][threadIdx.x];
+        D::place(bins, total, none, sh);
+        const bool last = pass + 1 == a.passes;
+        uint32_t *key_to = last ? a.key[0] : keys, *pos_to = last ? a.pos[0] : places;
+#pragma unroll
+        for (int k = 0; k < kSortKeys; ++k)
+            if (in[k]) {
+                const uint32_t to = bins[threadIdx.x >> 6][digit[k]] + own[k];
+                key_to[to] = x[k];
+                pos_to[to] = p[k];
+            }
+        if (last) return;
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kSortKeys; ++k)
+            if (in[k]) {
+                x[k] = keys[sort_at(0, rounds, k)];
+                p[k] = places[sort_at(0, rounds, k)];
+            }
+    }
+}
+
+template <int BITS> __global__ void __launch_bounds__(kSortThreads) embed_count_kernel(SortArgs a, int pass) {
+    using D = Digits<BITS>;
+    __shared__ uint32_t bins[D::kBins];
+    const int64_t n = row::live_rows(a.n_dev, a.cap), tile = blockIdx.x;
+    uint32_t x[kSortKeys];
+#pragma unroll
+    for (int k = 0; k < kSortKeys; ++k) {
+        const int64_t i = sort_at(tile, kSortKeys, k);
+        x[k] = i >= a.cap ? 0 : pass == 0 ? key_of(a, i, n) : a.key[pass & 1][i];
+    }
+    for (int d = threadIdx.x; d < D::kBins; d += kSortThreads) bins[d] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kSortKeys; ++k) {
+        const int64_t i = sort_at(tile, kSortKeys, k);
+        if (i >= a.cap) continue;
+        if (pass == 0) {
+            a.key[0][i] = x[k];
+            a.pos[0][i] = static_cast<uint32_t>(i);
+        }
+        atomicAdd(&bins[D::of(x[k], pass)], 1u);
+    }
+    __syncthreads();
+    for (int d = threadIdx.x; d < D::kBins; d += kSortThreads) a.counts[tile * D::kBins + d] = bins[d];
+}
+
+template <int BITS> __global__ void __launch_bounds__(kSortThreads) embed_move_kernel(SortArgs a, int pass) {
+    using D = Digits<BITS>;
+    __shared__ typename D::WaveBins bins;
+    __shared__ uint32_t sh[kSortWaves], sums[2][kSortThreads];
+    const int64_t tile = blockIdx.x;
+    const uint32_t *key = a.key[pass & 1], *pos = a.pos[pass & 1];
+    uint32_t x[kSortKeys], p[kSortKeys], digit[kSortKeys], own[kSortKeys];
+    bool in[kSortKeys];
+#pragma unroll
+    for (int k = 0; k < kSortKeys; ++k) {
+        const int64_t i = sort_at(tile, kSortKeys, k);
         in[k] = i < a.cap;
         x[k] = in[k] ? key[i] : 0;
         p[k] = in[k] ? pos[i] : 0;
-        digit[k] = (x[k] >> (kBits * pass)) & (kBins - 1);
+        digit[k] = D::of(x[k], pass);
     }
-    Ranks r;
-    rank_digits(digit, in, bins, r);
-    // a digit's first place: all smaller digits, and this one in earlier tiles
-    uint32_t total = 0, earlier = 0;
-    if (threadIdx.x < kBins)
-        for (int64_t t = 0; t < a.tiles; ++t) {
-            const uint32_t c = a.counts[threadIdx.x * a.tiles + t];
-            total += c;
-            if (t < tile) earlier += c;
+    // a digit's places: in all tiles, and in earlier ones
+    uint32_t total[D::kEach], earlier[D::kEach];
+    auto add_up = [&](int d, int64_t first, int64_t step, uint32_t &all, uint32_t &before) {
+        all = before = 0;
+#pragma unroll 8
+        for (int64_t t = first; t < a.tiles; t += step) {
+            const uint32_t c = a.counts[t * D::kBins + d];
+            all += c;
+            before += t < tile ? c : 0;
         }
-    const uint32_t smaller = scan_bins(total, sh);
-    if (threadIdx.x < kBins) {
-        uint32_t at = smaller + earlier;
-        for (int w = 0; w < kSortWaves; ++w) {
-            const uint32_t c = bins[w][threadIdx.x];
-            bins[w][threadIdx.x] = at;
-            at += c;
-        }
+    };
+    if constexpr (D::kBins >= kSortThreads) {
+#pragma unroll
+        for (int e = 0; e < D::kEach; ++e) add_up(threadIdx.x * D::kEach + e, 0, 1, total[e], earlier[e]);
+    } else {
+        constexpr int kParts = kSortThreads / D::kBins;
+        const int d = threadIdx.x % D::kBins;
+        add_up(d, threadIdx.x / D::kBins, kParts, sums[0][threadIdx.x], sums[1][threadIdx.x]);
+        __syncthreads();
+        total[0] = earlier[0] = 0;
+        if (threadIdx.x < D::kBins)
+#pragma unroll
+            for (int q = 0; q < kParts; ++q) {
+                total[0] += sums[0][q * D::kBins + d];
+                earlier[0] += sums[1][q * D::kBins + d];
+            }
     }
-    __syncthreads();
+    D::rank(digit, in, kSortKeys, bins, own);
+    D::place(bins, total, earlier, sh);
     uint32_t *key_to = a.key[(pass & 1) ^ 1], *pos_to = a.pos[(pass & 1) ^ 1];
 #pragma unroll
     for (int k = 0; k < kSortKeys; ++k) {
         if (!in[k]) continue;
-        const uint32_t to = bins[threadIdx.x >> 6][digit[k]] + r.own[k];
+        const uint32_t to = bins[threadIdx.x >> 6][digit[k]] + own[k];
         key_to[to] = x[k];
         pos_to[to] = p[k];
+    }
+}
+
+int key_bits(int64_t rows) {
+    int bits = 1;
+    while (rows >> bits) ++bits;
+    return bits;
+}
+
+// Sorts; which of key and pos hold the result goes to *where.
+gnn_status sort_ids(SortArgs a, int *where, hipStream_t s) {
+    const int bits = key_bits(a.rows);
+    *where = 0;
+    if (a.cap <= kSortTile) {
+        a.passes = static_cast<int>(ceil_div(bits, kOneBits));
+        embed_sort_kernel<<<1, kSortThreads, 0, s>>>(a);
+        GNN_LAUNCHED("embed_sort");
+        return GNN_OK;
+    }
+    // digits of up to 11 bits, whose counts fill 128 KB of LDS: few launches first
+    a.passes = static_cast<int>(ceil_div(bits, 11));
+    auto go = [&](auto width) -> gnn_status {
+        constexpr int BITS = decltype(width)::value;
+        for (int pass = 0; pass < a.passes; ++pass) {
+            embed_count_kernel<BITS><<<static_cast<unsigned>(a.tiles), kSortThreads, 0, s>>>(a, pass);
+            GNN_LAUNCHED("embed_count");
+            embed_move_kernel<BITS><<<static_cast<unsigned>(a.tiles), kSortThreads, 0, s>>>(a, pass);
+            GNN_LAUNCHED("embed_move");
+        }
+        return GNN_OK;
+    };
+    *where = a.passes & 1;
+    switch (ceil_div(bits, a.passes)) {
+        case 11: return go(std::integral_constant<int, 11>{});
+        case 10: return go(std::integral_constant<int, 10>{});
+        case 9: return go(std::integral_constant<int, 9>{});
+        default: return go(std::integral_constant<int, 8>{});
     }
 }
 
@@ -300,20 +418,30 @@ template <class T> __device__ __forceinline__ void zero_rows(const SumArgs &a, i
     row::Vec<T, VE> zero;
 #pragma unroll
     for (int i = 0; i < row::Vec<T, VE>::kWords; ++i) zero.w[i] = 0;
-    for (int64_t v = v0; v < v1; ++v) {
+    // a row to as many threads as it has vectors, several rows side by side
+    const int64_t vectors = ceil_div(a.dim, int64_t(VE));
+    const int64_t span = vectors >= kThreads ? kThreads : vectors, side = kThreads / span;
+    const int64_t slot = threadIdx.x / span, lane = threadIdx.x - slot * span;
+    if (slot >= side) return;
+    for (int64_t v = v0 + slot; v < v1; v += side) {
         if (named[v - v0]) continue;
         T *to = static_cast<T *>(a.d_table) + v * a.dim;
-        for (int64_t c = threadIdx.x * VE; c < a.dim; c += kThreads * VE) zero.store_upto(to + c, a.dim - c);
+        for (int64_t c = lane * VE; c < a.dim; c += span * VE) zero.store_upto(to + c, a.dim - c);
     }
 }
 
-constexpr int kAhead = 4;  // rows of g in flight
+// A tile's keys and positions are read at once, one to a lane, and handed around, so that
+// what the rows of g wait for is one load and not two behind each other, and kAhead rows are
+// in flight (tiles of 32 with four rows in flight and every key read where it is used: 8,192
+// x 1,024 in 36 us).
+constexpr int kAhead = 8;
 template <class TG, class T, int VE, int LANES> __global__ void __launch_bounds__(kThreads) embed_sum_kernel(SumArgs a) {
     if (blockIdx.x >= a.sum_blocks) {
         zero_rows<T>(a, blockIdx.x - a.sum_blocks);
         return;
     }
-    constexpr int kSlots = 64 / LANES;
+    constexpr int kSlots = 64 / LANES, kStep = LANES < kAhead ? kAhead : LANES;  // positions read at once
+    constexpr int kOwn = kStep / LANES;                                          // of these a lane's
     const int lane = threadIdx.x & (LANES - 1), slot = (threadIdx.x & 63) / LANES;
     const int64_t unit = static_cast<int64_t>(blockIdx.x) * kWaves + (threadIdx.x >> 6);
     const int64_t t = unit / a.passes * kSlots + slot;
@@ -322,24 +450,44 @@ template <class TG, class T, int VE, int LANES> __global__ void __launch_bounds_
     const int64_t beg = t * a.tile, end = min(a.cap, beg + a.tile);
     const TG *g = static_cast<const TG *>(a.g);
     const uint32_t none = static_cast<uint32_t>(a.rows);
+    const uint32_t before = beg > 0 ? a.key[beg - 1] : none, after = end < a.cap ? a.key[end] : none;
     uint32_t run = a.key[beg];
     if (run >= none) return;
-    bool began = beg == 0 || a.key[beg - 1] != run;  // the run begins in this tile
+    bool began = before != run;  // the run begins in this tile
     float sum[VE];
 #pragma unroll
     for (int e = 0; e < VE; ++e) sum[e] = 0.f;
-    for (int64_t p0 = beg; p0 < end; p0 += kAhead) {
-        uint32_t k[kAhead];
-        row::Vec<TG, VE> x[kAhead];
+    for (int64_t p0 = beg; p0 < end; p0 += kStep) {
+        uint32_t keys[kOwn], places[kOwn];
 #pragma unroll
-        for (int q = 0; q < kAhead; ++q) {
-            k[q] = p0 + q < end ? a.key[p0 + q] : none;
-            if (k[q] < none) x[q].load_upto(g + static_cast<int64_t>(a.pos[p0 + q]) * a.dim + c, room);
+        for (int o = 0; o < kOwn; ++o) {
+            const int64_t p = p0 + o * LANES + lane;
+            keys[o] = p < end ? a.key[p] : none;
+            places[o] = p < end ? a.pos[p] : 0;
         }
+        const int here = static_cast<int>(min(end - p0, int64_t(kStep)));
+#pragma unroll 1
+        for (int q0 = 0; q0 < here; q0 += kAhead) {
+            uint32_t k[kAhead];
+            row::Vec<TG, VE> x[kAhead];
 #pragma unroll
-        for (int q = 0; q < kAhead; ++q) {
-            if (k[q] != run) {
-                if (run < none && p0 + q < end) {
+            for (int q = 0; q < kAhead; ++q) {
+                uint32_t i;
+                if constexpr (LANES == 64) {
+                    k[q] = __builtin_amdgcn_readlane(keys[0], q0 + q);
+                    i = __builtin_amdgcn_readlane(places[0], q0 + q);
+                } else if constexpr (kOwn == 1) {
+                    k[q] = __shfl(keys[0], q0 + q, LANES);
+                    i = __shfl(places[0], q0 + q, LANES);
+                } else {
+                    k[q] = __shfl(keys[q / LANES], q % LANES, LANES);
+                    i = __shfl(places[q / LANES], q % LANES, LANES);
+                }
+                if (k[q] < none) x[q].load_upto(g + static_cast<int64_t>(i) * a.dim + c, room);
+            }
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q) {
+                if (k[q] != run && run < none && q0 + q < here) {
                     if (began) put_row<T, VE>(a, run, c, sum);
                     else put_part(a.first + t * a.dim + c, room, sum);
                     began = true;
@@ -347,22 +495,55 @@ template <class TG, class T, int VE, int LANES> __global__ void __launch_bounds_
 #pragma unroll
                     for (int e = 0; e < VE; ++e) sum[e] = 0.f;
                 }
-            }
-            if (k[q] < none) {
+                if (k[q] < none) {
 #pragma unroll
-                for (int e = 0; e < VE; ++e) sum[e] += x[q].get(e);
+                    for (int e = 0; e < VE; ++e) sum[e] += x[q].get(e);
+                }
             }
         }
     }
     if (run >= none) return;
     // the tile's last run: over, or one that goes on
     if (!began) put_part(a.first + t * a.dim + c, room, sum);
-    else if (end < a.cap && a.key[end] == run) put_part(a.last + t * a.dim + c, room, sum);
+    else if (after == run) put_part(a.last + t * a.dim + c, room, sum);
     else put_row<T, VE>(a, run, c, sum);
 }
 
-// The runs that cross tiles: of a run that begins in tile t, the sum that t left and those
-// of the tiles behind it, in order.
+// Runs that cross tiles.  Groups of kGroup tiles that one run spans, from before them to
+// their end, are summed first, in the place of their first tile's sum: a run of
+// n tiles takes its first tile's wavefront n / kGroup + 2 kGroup loads and not n (262,144
+// positions, the most frequent id 15,000 times, 2,048 wide: 254 us so, JOIN this way).
+constexpr int64_t kGroup = 32;
+__device__ __forceinline__ bool group_spanned(const SumArgs &a, int64_t u, uint32_t *run) {
+    const int64_t beg = u * a.tile, end = beg + kGroup * a.tile;
+    if (u == 0 || end > a.cap) return false;
+    *run = a.key[beg];
+    return *run < static_cast<uint32_t>(a.rows) && a.key[beg - 1] == *run && a.key[end - 1] == *run;
+}
+template <int VE> __device__ __forceinline__ void add_parts(const SumArgs &a, int64_t c, int64_t from, int64_t to, int64_t step, float (&sum)[VE]) {
+#pragma unroll 8
+    for (int64_t u = from; u < to; u += step) {
+        row::Vec<float, VE> x;
+        x.load_upto(a.first + u * a.dim + c, a.dim - c);
+#pragma unroll
+        for (int e = 0; e < VE; ++e) sum[e] += x.get(e);
+    }
+}
+template <int VE, int LANES> __global__ void __launch_bounds__(kThreads) embed_group_kernel(SumArgs a) {
+    constexpr int kSlots = 64 / LANES;
+    const int lane = threadIdx.x & (LANES - 1), slot = (threadIdx.x & 63) / LANES;
+    const int64_t unit = static_cast<int64_t>(blockIdx.x) * kWaves + (threadIdx.x >> 6);
+    const int64_t u = (unit / a.passes * kSlots + slot) * kGroup, c = ((unit % a.passes) * LANES + lane) * VE;
+    uint32_t run;
+    if (u + kGroup > a.tiles || !group_spanned(a, u, &run)) return;
+    float sum[VE];
+#pragma unroll
+    for (int e = 0; e < VE; ++e) sum[e] = 0.f;
+    add_parts<VE>(a, c, u, u + kGroup, 1, sum);
+    put_part(a.first + u * a.dim + c, a.dim - c, sum);
+}
+
+// Of a run that begins in tile t, the sum that t left and those of the tiles (groups) behind it.
 template <class T, int VE, int LANES> __global__ void __launch_bounds__(kThreads) embed_join_kernel(SumArgs a) {
     constexpr int kSlots = 64 / LANES;
     const int lane = threadIdx.x & (LANES - 1), slot = (threadIdx.x & 63) / LANES;
@@ -371,43 +552,41 @@ template <class T, int VE, int LANES> __global__ void __launch_bounds__(kThreads
     if (t + 1 >= a.tiles) return;
     const int64_t c = ((unit % a.passes) * LANES + lane) * VE, room = a.dim - c;
     const int64_t beg = t * a.tile, next = beg + a.tile;
-    const uint32_t run = a.key[next];
-    if (run >= static_cast<uint32_t>(a.rows) || a.key[next - 1] != run) return;
-    if (t > 0 && a.key[beg] == run && a.key[beg - 1] == run) return;  // it began earlier
+    const uint32_t run = a.key[next], end_key = a.key[next - 1], beg_key = a.key[beg], before = t > 0 ? a.key[beg - 1] : ~0u;
+    if (run >= static_cast<uint32_t>(a.rows) || end_key != run) return;
+    if (beg_key == run && before == run) return;  // it began earlier
     const int64_t over = lower(a.key, next, a.cap, run + 1);
+    const int64_t tiles = ceil_div(over, a.tile), head = min(tiles, ceil_div(t + 1, kGroup) * kGroup);
+    const int64_t whole = max(head, over / (a.tile * kGroup) * kGroup);  // groups up to there are spanned
     row::Vec<float, VE> x;
     x.load_upto(a.last + t * a.dim + c, room);
     float sum[VE];
 #pragma unroll
     for (int e = 0; e < VE; ++e) sum[e] = x.get(e);
-#pragma unroll 4
-    for (int64_t u = t + 1; u * a.tile < over; ++u) {
-        x.load_upto(a.first + u * a.dim + c, room);
-#pragma unroll
-        for (int e = 0; e < VE; ++e) sum[e] += x.get(e);
-    }
+    add_parts<VE>(a, c, t + 1, head, 1, sum);
+    add_parts<VE>(a, c, head, whole, kGroup, sum);
+    add_parts<VE>(a, c, whole, tiles, 1, sum);
     put_row<T, VE>(a, run, c, sum);
-}
-
-int sort_passes(int64_t rows) {
-    int bits = 1;
-    while (rows >> bits) ++bits;
-    return static_cast<int>(ceil_div(bits, kBits));
 }
 
 struct Plan {
     int64_t sort_tiles, tile, tiles;
     size_t key[2], pos[2], counts, first, last, total;
-    Plan(int64_t cap, int64_t dim) {
+    Plan(int64_t cap, int64_t rows, int64_t dim) {
         sort_tiles = std::max<int64_t>(1, ceil_div(cap, int64_t(kSortTile)));
-        tile = 32;
+        // positions of a tile: enough wavefronts for the chip (of 512 columns), up to 64, where the
+        // partial rows are a sixteenth of what is read
+        tile = 8;
+        while (tile < 64 && cap * ceil_div(dim, int64_t(512)) / (2 * tile) >= 4096) tile *= 2;
         tiles = ceil_div(cap, tile);
+        const int bits = key_bits(rows);
+        const int64_t bins = int64_t(1) << std::max<int64_t>(8, ceil_div(bits, ceil_div(bits, 11)));
         Carver c(nullptr);
         for (int i = 0; i < 2; ++i) {
             key[i] = c.take(static_cast<size_t>(cap) * 4);
             pos[i] = c.take(static_cast<size_t>(cap) * 4);
         }
-        counts = c.take(static_cast<size_t>(kBins * sort_tiles) * 4);
+        counts = c.take(static_cast<size_t>(bins * sort_tiles) * 4);
         first = c.take(static_cast<size_t>(tiles * dim) * 4);
         last = c.take(static_cast<size_t>(tiles * dim) * 4);
         total = round_up(c.off, 256);
@@ -435,11 +614,11 @@ gnn_status launch_embed_fwd(const void *table, int tdt, int64_t rows, int64_t di
     return GNN_OK;
 }
 
-size_t embed_bwd_ws_bytes(int64_t cap, int64_t, int64_t dim) { return Plan(cap, dim).total; }
+size_t embed_bwd_ws_bytes(int64_t cap, int64_t rows, int64_t dim) { return Plan(cap, rows, dim).total; }
 
 gnn_status launch_embed_bwd(const void *g, int gdt, const int64_t *ids, const int64_t *n_dev, int64_t cap, int64_t dim,
                             float scale, int64_t rows, bool add, void *d_table, int ddt, void *ws, hipStream_t s) {
-    const Plan pl(cap, dim);
+    const Plan pl(cap, rows, dim);
     char *base = static_cast<char *>(ws);
     SortArgs o{};
     o.ids = ids;
@@ -452,18 +631,12 @@ gnn_status launch_embed_bwd(const void *g, int gdt, const int64_t *ids, const in
     }
     o.counts = reinterpret_cast<uint32_t *>(base + pl.counts);
     o.tiles = pl.sort_tiles;
-    o.passes = sort_passes(rows);
-    if (cap > 0)
-        for (int pass = 0; pass < o.passes; ++pass) {
-            embed_count_kernel<<<static_cast<unsigned>(o.tiles), kSortThreads, 0, s>>>(o, pass);
-            GNN_LAUNCHED("embed_count");
-            embed_move_kernel<<<static_cast<unsigned>(o.tiles), kSortThreads, 0, s>>>(o, pass);
-            GNN_LAUNCHED("embed_move");
-        }
+    int where = 0;
+    if (cap > 0) GNN_TRY(sort_ids(o, &where, s));
     SumArgs a{};
     a.g = g;
-    a.key = o.key[o.passes & 1];
-    a.pos = o.pos[o.passes & 1];
+    a.key = o.key[where];
+    a.pos = o.pos[where];
     a.cap = cap;
     a.rows = rows;
     a.dim = dim;
@@ -497,6 +670,12 @@ gnn_status launch_embed_bwd(const void *g, int gdt, const int64_t *ids, const in
             embed_sum_kernel<TG, T, VE, LANES><<<static_cast<unsigned>(grid), kThreads, 0, s>>>(a);
             st = launch_status("embed_sum");
             if (st != GNN_OK || a.tiles < 2) return;
+            if (a.tiles > kGroup) {
+                const int64_t groups = ceil_div(ceil_div(a.tiles / kGroup, int64_t(64 / LANES)) * a.passes, int64_t(kWaves));
+                embed_group_kernel<VE, LANES><<<static_cast<unsigned>(groups), kThreads, 0, s>>>(a);
+                st = launch_status("embed_group");
+                if (st != GNN_OK) return;
+            }
             embed_join_kernel<T, VE, LANES><<<static_cast<unsigned>(a.sum_blocks), kThreads, 0, s>>>(a);
             st = launch_status("embed_join");
         });
