@@ -58,6 +58,8 @@ gnn_status logit_dz(const LogitArgs &a, hipStream_t s);
 
 int64_t splits_f32(Kind kind, int64_t M, int64_t N, int64_t R, bool may_split);
 gnn_status product_f32(Kind kind, const Product &p, hipStream_t s);
+// A kTT and a kNT product that do not depend on each other.
+gnn_status products_f32(const Product &tt, const Product &nt, hipStream_t s);
 int64_t splits_bf16(Kind kind, int64_t M, int64_t N, int64_t R, bool may_split);
 gnn_status product_bf16(Kind kind, const Product &p, hipStream_t s);
 

@@ -15,6 +15,8 @@
 // off by one and the same rounding, and their gradients with them (3,840 rows of 100,003
 // classes: 0.0037 of the gradients' norm that way, 0.0024 this way; a bf16
 // output's own rounding is 0.0017).
+#include <initializer_list>
+
 #include "class_loss.h"
 #include "gemm_engine.h"
 #include "loss_dev.h"
@@ -35,12 +37,16 @@ unsigned grid_of(int64_t n) {
 // ---------------------------------------------------------------------------
 // rows: labels and weights, operands in the products' type
 // ---------------------------------------------------------------------------
-__global__ void __launch_bounds__(kThreads) class_rows_kernel(CeArgs a, RowState r) {
-    const int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-    if (i >= a.b) return;
-    const int64_t y = a.labels[a.targets ? a.targets[i] : i];
-    const float w = a.row_scale ? a.row_scale[i] : 1.f / static_cast<float>(a.b);
-    const bool live = y >= 0 && y < a.c && w != 0.f;
+// Row i's label and weight; whether it takes part.
+__device__ __forceinline__ bool row_of_batch(const CeArgs &a, int64_t i, int64_t *label, float *weight) {
+    *label = a.labels[a.targets ? a.targets[i] : i];
+    *weight = a.row_scale ? a.row_scale[i] : 1.f / static_cast<float>(a.b);
+    return *label >= 0 && *label < a.c && *weight != 0.f;
+}
+__device__ __forceinline__ void start_row(const CeArgs &a, const RowState &r, int64_t i) {
+    int64_t y;
+    float w;
+    const bool live = row_of_batch(a, i, &y, &w);
     r.label[i] = live ? static_cast<int32_t>(y) : -1;
     r.weight[i] = live ? w : 0.f;
     r.top[i] = -INFINITY;
@@ -48,39 +54,56 @@ __global__ void __launch_bounds__(kThreads) class_rows_kernel(CeArgs a, RowState
     r.z_label[i] = 0.f;
 }
 
-// rows of K values to rows of ld, zeros behind them; rows that take no part (label < 0) are
-// zeros: dWt multiplies them by 0, which a NaN there would survive.
+__global__ void __launch_bounds__(kThreads) class_rows_kernel(CeArgs a, RowState r) {
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
+    if (i < a.b) start_row(a, r, i);
+}
+
+// Four values from K of a row to a row of ld, zeros behind them.
+template <class TI, class TO> __device__ __forceinline__ void pack4(const TI *in, int64_t r, int64_t c, int64_t K, bool live, int64_t ld, TO *out) {
+    row::Vec<TI, 4> v;
+    v.load_upto(in + r * K + c, live ? K - c : 0);
+    float x[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = v.get(e);
+    row::Vec<TO, 4> o;
+    o.set(x);
+    o.store(out + r * ld + c);
+}
 template <class TI, class TO>
-__global__ void __launch_bounds__(kThreads) class_pack_kernel(const TI *in, int64_t rows, int64_t K, int64_t ld, const int32_t *label,
-                                                              TO *out) {
+__global__ void __launch_bounds__(kThreads) class_pack_kernel(const TI *in, int64_t rows, int64_t K, int64_t ld, TO *out) {
     const int64_t groups = ld / 4;
     for (int64_t t = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; t < rows * groups;
          t += static_cast<int64_t>(gridDim.x) * kThreads) {
         const int64_t r = t / groups, c = (t - r * groups) * 4;
-        row::Vec<TI, 4> v;
-        v.load_upto(in + r * K + c, label && label[r] < 0 ? 0 : K - c);
-        float x[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = v.get(e);
-        row::Vec<TO, 4> o;
-        o.set(x);
-        o.store(out + r * ld + c);
+        pack4(in, r, c, K, true, ld, out);
+    }
+}
+// A with the rows' labels and weights on the way.  Rows that take no part are zeros:
+// dWt multiplies them by 0, which a NaN there would survive.
+template <class TI, class TO>
+__global__ void __launch_bounds__(kThreads) class_pack_rows_kernel(CeArgs a, RowState rs, int64_t ld, TO *out) {
+    const int64_t groups = ld / 4;
+    for (int64_t t = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; t < a.b * groups;
+         t += static_cast<int64_t>(gridDim.x) * kThreads) {
+        const int64_t r = t / groups, c = (t - r * groups) * 4;
+        int64_t y;
+        float w;
+        const bool live = row_of_batch(a, r, &y, &w);
+        pack4(static_cast<const TI *>(a.a), r, c, a.k, live, ld, out);
+        if (c == 0) start_row(a, rs, r);
     }
 }
 
-gnn_status pack(const void *in, int idt, int64_t rows, int64_t K, int64_t ld, const int32_t *label, void *out, int odt, hipStream_t s) {
-    const unsigned grid = grid_of(rows * (ld / 4));
+// go(a pointer's type for the input, one for the output)
+template <class F> void with_pack_types(int idt, int odt, F &&go) {
     if (idt == GNN_BF16) {
-        const uint16_t *x = static_cast<const uint16_t *>(in);
-        if (odt == GNN_BF16) class_pack_kernel<<<grid, kThreads, 0, s>>>(x, rows, K, ld, label, static_cast<uint16_t *>(out));
-        else class_pack_kernel<<<grid, kThreads, 0, s>>>(x, rows, K, ld, label, static_cast<float *>(out));
+        if (odt == GNN_BF16) go(uint16_t{}, uint16_t{});
+        else go(uint16_t{}, float{});
     } else {
-        const float *x = static_cast<const float *>(in);
-        if (odt == GNN_BF16) class_pack_kernel<<<grid, kThreads, 0, s>>>(x, rows, K, ld, label, static_cast<uint16_t *>(out));
-        else class_pack_kernel<<<grid, kThreads, 0, s>>>(x, rows, K, ld, label, static_cast<float *>(out));
+        if (odt == GNN_BF16) go(float{}, uint16_t{});
+        else go(float{}, float{});
     }
-    GNN_LAUNCHED("update_ce_pack");
-    return GNN_OK;
 }
 
 // ---------------------------------------------------------------------------
@@ -158,52 +181,63 @@ __global__ void __launch_bounds__(kThreads) class_join_kernel(const float2 *part
     join_row(r, i, top, sum, last, row_loss);
 }
 
-// The weighted sum of the rows' losses, in a fixed order, and the largest weight.
-__global__ void __launch_bounds__(1024) class_total_kernel(const float *row_loss, const float *weight, int64_t b, float *loss, float *scale) {
-    __shared__ float sh[2][16];
-    float s = 0.f, most = 0.f;
-    for (int64_t i = threadIdx.x; i < b; i += 1024) {
-        const float w = weight[i];
-        if (w != 0.f) s += row_loss[i] * w;
-        most = fmaxf(most, fabsf(w));
-    }
-    s = loss::wave_sum(s);
-    most = loss::wave_max(most);
-    if ((threadIdx.x & 63) == 0) {
-        sh[0][threadIdx.x >> 6] = s;
-        sh[1][threadIdx.x >> 6] = most;
-    }
-    __syncthreads();
-    if (threadIdx.x != 0) return;
-    s = most = 0.f;
+// The weighted sum of the rows' losses, in a fixed order, and the largest weight (bf16; fp32
+// products need no common factor).  All of a workgroup's threads.
+struct Total {
+    const float *row_loss, *weight;
+    int64_t b;
+    float *loss, *scale;
+    template <int THREADS> __device__ __forceinline__ void run() const {
+        __shared__ float sh[2][THREADS / 64];
+        float s = 0.f, most = 0.f;
+        for (int64_t i = threadIdx.x; i < b; i += THREADS) {
+            const float w = weight[i];
+            if (w != 0.f) s += row_loss[i] * w;
+            most = fmaxf(most, fabsf(w));
+        }
+        s = loss::wave_sum(s);
+        most = loss::wave_max(most);
+        if ((threadIdx.x & 63) == 0) {
+            sh[0][threadIdx.x >> 6] = s;
+            sh[1][threadIdx.x >> 6] = most;
+        }
+        __syncthreads();
+        if (threadIdx.x != 0) return;
+        s = most = 0.f;
 #pragma unroll
-    for (int w = 0; w < 16; ++w) {
-        s += sh[0][w];
-        most = fmaxf(most, sh[1][w]);
+        for (int w = 0; w < THREADS / 64; ++w) {
+            s += sh[0][w];
+            most = fmaxf(most, sh[1][w]);
+        }
+        *loss = s;
+        // (no weights, or so small that their reciprocal leaves fp32: dZ as it is)
+        if (scale) *scale = most >= 0x1p-100f ? most : 1.f;
     }
-    *loss = s;
-    // (no weights, or so small that their reciprocal leaves fp32: dZ as it is)
-    *scale = most >= 0x1p-100f ? most : 1.f;
-}
+};
+constexpr int64_t kFewRows = 4096;  // whose total a workgroup of dZ's launch takes along
+__global__ void __launch_bounds__(1024) class_total_kernel(Total t) { t.run<1024>(); }
 
 // dZ of a piece in place of its logits, zeros in the columns up to ld, and the column sums
 // of a part of the rows.
 constexpr int kStripe = 256;  // columns of a workgroup: 64 threads of 4, times 4 rows
 __global__ void __launch_bounds__(kThreads) class_dz_kernel(float *z, int64_t ld, int64_t b, int64_t cols, int64_t c0, const float *bias, RowState r,
-                                                            const float *scale, float *part, int64_t parts) {
+                                                            float *part, int64_t parts, Total total) {
     __shared__ float sh[4][kStripe];
+    if (blockIdx.x >= ceil_div(ld, int64_t(kStripe)) * parts) {
+        total.run<kThreads>();
+        return;
+    }
     const int64_t stripes = ceil_div(ld, int64_t(kStripe)), stripe = blockIdx.x % stripes, p = blockIdx.x / stripes;
     const int64_t per = ceil_div(b, parts), beg = min(b, p * per), end = min(b, beg + per);
     const int x = (threadIdx.x & 63) * 4, y = threadIdx.x >> 6;
     const int64_t c = stripe * kStripe + x;
-    const float inverse = 1.f / *scale;
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
     if (c < ld) {
         float bs[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) bs[e] = bias && c + e < cols ? bias[c0 + c + e] : 0.f;
         for (int64_t i = beg + y; i < end; i += 4) {
-            const float w = r.weight[i] * inverse, lse = r.lse[i];
+            const float w = r.weight[i], lse = r.lse[i];
             const int64_t label = r.label[i] - c0;
             float v[4] = {0.f, 0.f, 0.f, 0.f};
             if (w != 0.f) {
@@ -233,42 +267,73 @@ __global__ void __launch_bounds__(kThreads) class_dz_kernel(float *z, int64_t ld
     part[p * ld + col] = t;
 }
 
-// db of a piece: 32 columns of a workgroup, every eighth part to a thread.
-__global__ void __launch_bounds__(kThreads) class_db_kernel(const float *part, int64_t parts, int64_t ld, int64_t cols, const float *scale, float *db) {
-    __shared__ float sh[8][32];
-    const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
-    const int64_t c = static_cast<int64_t>(blockIdx.x) * 32 + x;
-    float t = 0.f;
-    if (c < cols)
-#pragma unroll 4
-        for (int64_t p = y; p < parts; p += 8) t += part[p * ld + c];
-    sh[y][x] = t;
-    __syncthreads();
-    if (y != 0 || c >= cols) return;
-    t = 0.f;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) t += sh[k][x];
-    db[c] = t * *scale;
-}
-
-// out = the partials in their order; rows of `ld` to rows of `cols`
-template <class T>
-__global__ void __launch_bounds__(kThreads) class_reduce_kernel(const float *part, int64_t nsplit, int64_t rows, int64_t cols, int64_t ld, T *out) {
-    const int64_t groups = ld / 4;
-    for (int64_t t = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; t < rows * groups;
-         t += static_cast<int64_t>(gridDim.x) * kThreads) {
-        const int64_t r = t / groups, c = (t - r * groups) * 4;
-        const float4 v = gemm::sum_splits(part + r * ld + c, rows * ld, static_cast<int>(nsplit));
-        const float x[4] = {v.x, v.y, v.z, v.w};
-        row::Vec<T, 4> o;
-        o.set(x);
-        o.store_upto(out + r * cols + c, cols - c);
+// What is left of a piece behind its products, in one launch: the partials of dWt and, behind
+// the last piece, of dA, in their order, rows of `ld` to rows of `cols`; and db, 32 columns of a
+// workgroup, every eighth part to a thread.
+struct Reduce {
+    const float *part;
+    int64_t nsplit, rows, cols, ld;
+    void *out;
+    int bf16;
+    int64_t blocks;  // 0: nothing
+    __device__ __forceinline__ void run(int64_t blk) const {
+        const int64_t groups = ld / 4;
+        for (int64_t t = blk * kThreads + threadIdx.x; t < rows * groups; t += blocks * kThreads) {
+            const int64_t r = t / groups, c = (t - r * groups) * 4;
+            const float4 v = gemm::sum_splits(part + r * ld + c, rows * ld, static_cast<int>(nsplit));
+            const float x[4] = {v.x, v.y, v.z, v.w};
+            if (bf16) {
+                row::Vec<uint16_t, 4> o;
+                o.set(x);
+                o.store_upto(static_cast<uint16_t *>(out) + r * cols + c, cols - c);
+            } else {
+                row::Vec<float, 4> o;
+                o.set(x);
+                o.store_upto(static_cast<float *>(out) + r * cols + c, cols - c);
+            }
+        }
     }
+};
+Reduce reduce_of(const float *part, int64_t nsplit, int64_t rows, int64_t cols, int64_t ld, void *out, int odt) {
+    return Reduce{part, nsplit, rows, cols, ld, out, odt == GNN_BF16, std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows * (ld / 4), int64_t(kThreads)), 16384))};
 }
-gnn_status reduce(const float *part, int64_t nsplit, int64_t rows, int64_t cols, int64_t ld, void *out, int odt, hipStream_t s) {
-    const unsigned grid = grid_of(rows * (ld / 4));
-    if (odt == GNN_BF16) class_reduce_kernel<<<grid, kThreads, 0, s>>>(part, nsplit, rows, cols, ld, static_cast<uint16_t *>(out));
-    else class_reduce_kernel<<<grid, kThreads, 0, s>>>(part, nsplit, rows, cols, ld, static_cast<float *>(out));
+struct ReduceDb {
+    const float *part;
+    int64_t parts, ld, cols;
+    const float *scale;
+    float *db;
+    int64_t blocks;  // 0: nothing
+    __device__ __forceinline__ void run(int64_t blk) const {
+        __shared__ float sh[8][32];
+        const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+        const int64_t c = blk * 32 + x;
+        float t = 0.f;
+        if (c < cols)
+#pragma unroll 4
+            for (int64_t p = y; p < parts; p += 8) t += part[p * ld + c];
+        sh[y][x] = t;
+        __syncthreads();
+        if (y != 0 || c >= cols) return;
+        t = 0.f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) t += sh[k][x];
+        db[c] = scale ? t * *scale : t;
+    }
+};
+__global__ void __launch_bounds__(kThreads) class_reduce_kernel(ReduceDb db, Reduce w, Reduce a) {
+    int64_t blk = blockIdx.x;
+    if (blk < db.blocks) {
+        db.run(blk);
+        return;
+    }
+    blk -= db.blocks;
+    if (blk < w.blocks) w.run(blk);
+    else a.run(blk - w.blocks);
+}
+gnn_status reduce(const ReduceDb &db, const Reduce &w, const Reduce &a, hipStream_t s) {
+    const int64_t blocks = db.blocks + w.blocks + a.blocks;
+    if (blocks == 0) return GNN_OK;
+    class_reduce_kernel<<<static_cast<unsigned>(blocks), kThreads, 0, s>>>(db, w, a);
     GNN_LAUNCHED("update_ce_reduce");
     return GNN_OK;
 }
@@ -352,17 +417,20 @@ gnn_status launch_update_ce(const CeArgs &a, void *ws, hipStream_t s) {
     const RowState r{reinterpret_cast<int32_t *>(base + pl.label), f(pl.weight), f(pl.top), f(pl.sum), f(pl.z_label), f(pl.lse)};
     float *row_loss = a.row_loss ? a.row_loss : f(pl.row_loss), *scale = f(pl.scale), *z = f(pl.z);
     const bool any = a.b > 0;
-    if (any) {
-        class_rows_kernel<<<static_cast<unsigned>(ceil_div(a.b, int64_t(kThreads))), kThreads, 0, s>>>(a, r);
-        GNN_LAUNCHED("update_ce_rows");
-    }
+    // A as the products read it
     const void *A = a.a;
     int64_t lda = a.k;
     const bool rows16 = a.k * static_cast<int64_t>(es) % 16 == 0;
     if (any && (a.dwt || a.adt != gdt || !rows16 || !aligned(a.a, 16))) {
-        GNN_TRY(pack(a.a, a.adt, a.b, a.k, pl.ldk, r.label, base + pl.a, gdt, s));
+        with_pack_types(a.adt, gdt, [&](auto ti, auto to) {
+            class_pack_rows_kernel<decltype(ti)><<<grid_of(a.b * (pl.ldk / 4)), kThreads, 0, s>>>(a, r, pl.ldk, reinterpret_cast<decltype(to) *>(base + pl.a));
+        });
+        GNN_LAUNCHED("update_ce_pack");
         A = base + pl.a;
         lda = pl.ldk;
+    } else if (any) {
+        class_rows_kernel<<<static_cast<unsigned>(ceil_div(a.b, int64_t(kThreads))), kThreads, 0, s>>>(a, r);
+        GNN_LAUNCHED("update_ce_rows");
     }
     // the weights' rows [c0, c0 + cols) as the products read them
     const bool copy_w = a.wdt != gdt || !rows16 || !aligned(a.wt, 16);
@@ -372,22 +440,25 @@ gnn_status launch_update_ce(const CeArgs &a, void *ws, hipStream_t s) {
         w = static_cast<const char *>(a.wt) + c0 * a.k * static_cast<int64_t>(dtype_size(a.wdt));
         ldw = a.k;
         if (!copy_w) return GNN_OK;
-        GNN_TRY(pack(w, a.wdt, cols, a.k, pl.ldk, nullptr, base + pl.w, gdt, s));
+        with_pack_types(a.wdt, gdt, [&](auto ti, auto to) {
+            class_pack_kernel<<<grid_of(cols * (pl.ldk / 4)), kThreads, 0, s>>>(static_cast<const decltype(ti) *>(w), cols, a.k, pl.ldk,
+                                                                                reinterpret_cast<decltype(to) *>(base + pl.w));
+        });
+        GNN_LAUNCHED("update_ce_pack");
         w = base + pl.w;
         ldw = pl.ldk;
         return GNN_OK;
     };
-    auto product = [&](Kind kind, const Product &p) { return pl.bf ? product_bf16(kind, p, s) : product_f32(kind, p, s); };
     auto logits = [&](int64_t cols) {
         const int64_t K = std::min(lda, ldw);
-        return product(kNN, Product{A, w, lda, ldw, a.b, cols, K, K, z, GNN_F32, row_of(cols), 1, 0, false, nullptr});
+        return product_f32(kNN, Product{A, w, lda, ldw, a.b, cols, K, K, z, GNN_F32, row_of(cols), 1, 0, false, nullptr}, s);
     };
     auto tile_args = [&](int64_t c0, int64_t cols) {
         return LogitArgs{static_cast<const uint16_t *>(A), static_cast<const uint16_t *>(w), lda, ldw, a.b, cols, std::min(lda, ldw), c0,
                          a.bias ? a.bias + c0 : nullptr, r, reinterpret_cast<float2 *>(z), reinterpret_cast<uint16_t *>(z), row_of(cols), scale,
                          a.db ? f(pl.db) : nullptr};
     };
-    // (copies of the weights are a piece's)
+    // the rows' sums and losses (copies of the weights are a piece's)
     const int64_t step = copy_w ? pl.piece : pl.sums_piece;
     for (int64_t c0 = 0; any && c0 < a.c; c0 += step) {
         const int64_t cols = std::min(step, a.c - c0);
@@ -408,58 +479,68 @@ gnn_status launch_update_ce(const CeArgs &a, void *ws, hipStream_t s) {
         else class_sums_kernel<256><<<static_cast<unsigned>(a.b), kThreads, 0, s>>>(z, a.b, cols, ld, c0, a.bias, r, last, row_loss);
         GNN_LAUNCHED("update_ce_sums");
     }
-    class_total_kernel<<<1, 1024, 0, s>>>(row_loss, r.weight, a.b, a.loss_out, scale);
-    GNN_LAUNCHED("update_ce_total");
+    // their total: beside dZ where there is one in fp32 and the rows are few
+    const Total total{row_loss, r.weight, a.b, a.loss_out, pl.bf ? scale : nullptr};
+    bool owed = grads && any && !pl.bf && a.b <= kFewRows;
+    if (!owed) {
+        class_total_kernel<<<1, 1024, 0, s>>>(total);
+        GNN_LAUNCHED("update_ce_total");
+    }
     if (!grads) return GNN_OK;
+    const float *factor = pl.bf ? scale : nullptr;
     for (int64_t q = 0; q < pl.pieces; ++q) {
         const int64_t c0 = q * pl.piece, cols = std::min(pl.piece, a.c - c0), ld = row_of(cols);
-        const int which = q + 1 < pl.pieces ? 0 : 1;
+        const bool again = pl.pieces > 1, last = q + 1 == pl.pieces;
+        const int which = last ? 1 : 0;
         // (a single piece's weights are still there, and in fp32 its logits)
-        const bool again = pl.pieces > 1;
         if (any && again) GNN_TRY(weights(c0, cols));
         if (any && pl.bf) {
             GNN_TRY(logit_dz(tile_args(c0, cols), s));
         } else if (any) {
             if (again) GNN_TRY(logits(cols));
-            class_dz_kernel<<<static_cast<unsigned>(ceil_div(ld, int64_t(kStripe)) * pl.parts[which]), kThreads, 0, s>>>(
-                z, ld, a.b, cols, c0, a.bias, r, scale, a.db ? f(pl.db) : nullptr, pl.parts[which]);
+            const int64_t blocks = ceil_div(ld, int64_t(kStripe)) * pl.parts[which] + (owed ? 1 : 0);
+            class_dz_kernel<<<static_cast<unsigned>(blocks), kThreads, 0, s>>>(z, ld, a.b, cols, c0, a.bias, r, a.db ? f(pl.db) : nullptr,
+                                                                               pl.parts[which], total);
             GNN_LAUNCHED("update_ce_dz");
+            owed = false;
         }
-        if (a.db) {
-            class_db_kernel<<<static_cast<unsigned>(ceil_div(cols, int64_t(32))), kThreads, 0, s>>>(f(pl.db), any ? pl.parts[which] : 0, ld, cols, scale,
-                                                                                                  a.db + c0);
-            GNN_LAUNCHED("update_ce_db");
-        }
+        ReduceDb rb{};
+        if (a.db) rb = ReduceDb{f(pl.db), any ? pl.parts[which] : 0, ld, cols, factor, a.db + c0, ceil_div(cols, int64_t(32))};
+        Reduce rw{}, ra{};
+        Product pw{z, A, ld, lda, cols, a.k, a.b, a.b, nullptr, a.dwdt, a.k, 1, 0, false, factor};
         if (a.dwt) {
-            const int64_t n = pl.dw_splits[which];
-            char *to = static_cast<char *>(a.dwt) + c0 * a.k * static_cast<int64_t>(dtype_size(a.dwdt));
-            Product p{z, A, ld, lda, cols, a.k, a.b, a.b, to, a.dwdt, a.k, 1, 0, false, scale};
-            if (n > 1) {
-                p.out = base + pl.dw_part;
-                p.odt = GNN_F32;
-                p.ld = pl.ldk;
-                p.nsplit = n;
-                p.split_stride = cols * pl.ldk;
+            pw.out = static_cast<char *>(a.dwt) + c0 * a.k * static_cast<int64_t>(dtype_size(a.dwdt));
+            if (const int64_t n = pl.dw_splits[which]; n > 1) {
+                rw = reduce_of(f(pl.dw_part), n, cols, a.k, pl.ldk, pw.out, a.dwdt);
+                pw.out = base + pl.dw_part;
+                pw.odt = GNN_F32;
+                pw.ld = pl.ldk;
+                pw.nsplit = n;
+                pw.split_stride = cols * pl.ldk;
             }
-            GNN_TRY(product(kTT, p));
-            if (n > 1) GNN_TRY(reduce(f(pl.dw_part), n, cols, a.k, pl.ldk, to, a.dwdt, s));
         }
-        if (a.d_a && any) {
-            const bool whole = pl.pieces == 1 && pl.da_splits == 1;
-            Product p{z, w, ld, ldw, a.b, a.k, ld, cols, a.d_a, a.gdt, a.k, 1, 0, false, scale};
-            if (!whole) {
-                p.out = base + pl.da_part;
-                p.odt = GNN_F32;
-                p.ld = pl.ldk;
-                p.nsplit = pl.da_splits;
-                p.split_stride = a.b * pl.ldk;
-                p.add = q > 0;
-            }
-            GNN_TRY(product(kNT, p));
+        const bool da = a.d_a && any;
+        Product pa{z, w, ld, ldw, a.b, a.k, ld, cols, a.d_a, a.gdt, a.k, 1, 0, false, factor};
+        if (da && (again || pl.da_splits > 1)) {
+            if (last) ra = reduce_of(f(pl.da_part), pl.da_splits, a.b, a.k, pl.ldk, a.d_a, a.gdt);
+            pa.out = base + pl.da_part;
+            pa.odt = GNN_F32;
+            pa.ld = pl.ldk;
+            pa.nsplit = pl.da_splits;
+            pa.split_stride = a.b * pl.ldk;
+            pa.add = q > 0;
         }
+        if (pl.bf) {
+            if (a.dwt) GNN_TRY(product_bf16(kTT, pw, s));
+            if (da) GNN_TRY(product_bf16(kNT, pa, s));
+        } else if (a.dwt && da) {
+            GNN_TRY(products_f32(pw, pa, s));
+        } else {
+            if (a.dwt) GNN_TRY(product_f32(kTT, pw, s));
+            if (da) GNN_TRY(product_f32(kNT, pa, s));
+        }
+        GNN_TRY(reduce(rb, rw, ra, s));
     }
-    if (a.d_a && any && (pl.pieces > 1 || pl.da_splits > 1))
-        GNN_TRY(reduce(f(pl.da_part), pl.da_splits, a.b, a.k, pl.ldk, a.d_a, a.gdt, s));
     return GNN_OK;
 }
 

@@ -1,4 +1,6 @@
 // fp32 products of the loss over many classes, on the general engine.
+#include <type_traits>
+
 #include "class_loss.h"
 #include "gemm_engine.h"
 
@@ -22,22 +24,23 @@ template <int TILE> struct Source<TILE, true> {
     }
 };
 
-template <int TILE, bool TX, bool TY> __global__ void __launch_bounds__(gemm::kThreads) class_engine_kernel(Product p, TileMap map) {
+// Workgroup blk of a product's.
+template <int TILE, bool TX, bool TY> __device__ __forceinline__ void run_product(const Product &p, const TileMap &map, int64_t blk, char *lds) {
     constexpr int D = depth<TILE>();
-    __shared__ __attribute__((aligned(16))) char lds[lds_bytes<TILE, TILE>()];
+    const int64_t split = blk / map.blocks();
     int64_t tx, ty;
-    map.tile_of(blockIdx.x, &tx, &ty);
+    map.tile_of(blk - split * map.blocks(), &tx, &ty);
     const int64_t row0 = tx * TILE, col0 = ty * TILE;
     if (tx >= map.mt) return;
     int64_t beg, end;
-    split_range<Cfg<false>::BK>(p.R, gridDim.z, blockIdx.z, &beg, &end);
+    split_range<Cfg<false>::BK>(p.R, static_cast<int>(p.nsplit), static_cast<int>(split), &beg, &end);
     end = min(end, p.Ry);
     auto sx = Source<TILE, TX>::make(p.x, p.ldx, p.M, end, p.ldx, row0);
     auto sy = Source<TILE, TY>::make(p.y, p.ldy, p.N, end, p.ldy, col0);
     Acc<TILE, TILE> acc;
     run_tile<false, D>(acc, sx, sy, beg, end, lds, [](const auto &, int, int64_t, bool) {});
     const int64_t gc = col0 + TileOut<TILE, TILE>::col(), M = p.M, N = p.N, ld = p.ld;
-    float *out = static_cast<float *>(p.out) + blockIdx.z * p.split_stride;
+    float *out = static_cast<float *>(p.out) + split * p.split_stride;
     const bool add = p.add;
     const float factor = p.factor ? *p.factor : 1.f;
     emit_tile(acc, lds, [&](int, int r, int, float4 v) {
@@ -52,6 +55,18 @@ template <int TILE, bool TX, bool TY> __global__ void __launch_bounds__(gemm::kT
     });
 }
 
+template <int TILE, bool TX, bool TY> __global__ void __launch_bounds__(gemm::kThreads) class_engine_kernel(Product p, TileMap map) {
+    __shared__ __attribute__((aligned(16))) char lds[lds_bytes<TILE, TILE>()];
+    run_product<TILE, TX, TY>(p, map, blockIdx.x, lds);
+}
+
+// dWt and dA of a piece side by side: of small models both are a launch's latency.
+__global__ void __launch_bounds__(gemm::kThreads) class_engine_pair_kernel(Product tt, TileMap mt, int64_t tts, Product nt, TileMap mn) {
+    __shared__ __attribute__((aligned(16))) char lds[lds_bytes<64, 64>()];
+    if (blockIdx.x < tts) run_product<64, true, true>(tt, mt, blockIdx.x, lds);
+    else run_product<64, false, true>(nt, mn, blockIdx.x - tts, lds);
+}
+
 }  // namespace
 
 int64_t splits_f32(Kind, int64_t M, int64_t N, int64_t R, bool may_split) {
@@ -64,8 +79,9 @@ int64_t splits_f32(Kind, int64_t M, int64_t N, int64_t R, bool may_split) {
 gnn_status product_f32(Kind kind, const Product &p, hipStream_t s) {
     const int tile = pick_tile(p.M, p.N);
     const TileMap map{ceil_div(p.M, tile), ceil_div(p.N, tile)};
-    GNN_CHECK(map.blocks() <= kMaxGrid / gemm::kThreads, GNN_ESIZE, "update_ce: sizes exceed the grid limit");
-    const dim3 grid(static_cast<unsigned>(map.blocks()), 1, static_cast<unsigned>(p.nsplit));
+    const int64_t blocks = map.blocks() * p.nsplit;
+    GNN_CHECK(blocks <= kMaxGrid / gemm::kThreads, GNN_ESIZE, "update_ce: sizes exceed the grid limit");
+    const unsigned grid = static_cast<unsigned>(blocks);
     auto go = [&](auto tx, auto ty) {
         constexpr bool TX = decltype(tx)::value, TY = decltype(ty)::value;
         if (tile == 128) class_engine_kernel<128, TX, TY><<<grid, gemm::kThreads, 0, s>>>(p, map);
@@ -75,6 +91,19 @@ gnn_status product_f32(Kind kind, const Product &p, hipStream_t s) {
     else if (kind == kTT) go(std::true_type{}, std::true_type{});
     else go(std::false_type{}, std::true_type{});
     GNN_LAUNCHED("update_ce_product");
+    return GNN_OK;
+}
+
+gnn_status products_f32(const Product &tt, const Product &nt, hipStream_t s) {
+    const TileMap mt{ceil_div(tt.M, int64_t(64)), ceil_div(tt.N, int64_t(64))}, mn{ceil_div(nt.M, int64_t(64)), ceil_div(nt.N, int64_t(64))};
+    const int64_t a = mt.blocks() * tt.nsplit, b = mn.blocks() * nt.nsplit;
+    // products of many tiles fill the chip one after the other
+    if (pick_tile(tt.M, tt.N) != 64 || pick_tile(nt.M, nt.N) != 64 || a + b > 2048) {
+        GNN_TRY(product_f32(kTT, tt, s));
+        return product_f32(kNT, nt, s);
+    }
+    class_engine_pair_kernel<<<static_cast<unsigned>(a + b), gemm::kThreads, 0, s>>>(tt, mt, a, nt, mn);
+    GNN_LAUNCHED("update_ce_products");
     return GNN_OK;
 }
 

@@ -102,11 +102,12 @@ template <class F> void with_types(int idt, int odt, F &&go) {
 // Keys are ids; what names no row, and positions at or past the count, get the
 // key `rows` and come last.  A stable radix sort, least digit first.  Up to kSortTile
 // positions one workgroup does all of it in LDS (8,192 positions of 32,000 rows: 36 us in
-// four launches, SORT1 in this one).  More take two launches a digit: one counts each
+// four launches, 23 in this one).  More take two launches a digit: one counts each
 // tile's digits, the next moves the tile's pairs behind all smaller digits and behind
 // the same digit in earlier tiles, adding up the tiles' counts by itself.
-constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kSortKeys = 8;
-constexpr int kSortTile = kSortThreads * kSortKeys;
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
+constexpr int kSortKeys = 8, kSortTile = kSortThreads * kSortKeys;  // of the one workgroup
+constexpr int kMoveKeys = 2, kMoveTile = kSortThreads * kMoveKeys;  // of a tile among others
 
 struct SortArgs {
     const int64_t *ids, *n_dev;
@@ -125,14 +126,15 @@ template <int BITS> struct Digits {
 
     // own[k] = how many of the wavefront's earlier elements (of smaller k, or in a lower lane)
     // have the digit of its element k; bins[wave] = the wavefront's counts.
-    __device__ __forceinline__ static void rank(const uint32_t (&digit)[kSortKeys], const bool (&in)[kSortKeys], int rounds, WaveBins &bins,
-                                                uint32_t (&own)[kSortKeys]) {
+    template <int KEYS>
+    __device__ __forceinline__ static void rank(const uint32_t (&digit)[KEYS], const bool (&in)[KEYS], int rounds, WaveBins &bins,
+                                                uint32_t (&own)[KEYS]) {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
         for (int i = threadIdx.x; i < kSortWaves * kBins; i += kSortThreads) (&bins[0][0])[i] = 0;
         __syncthreads();
         volatile uint32_t *mine = bins[wave];
 #pragma unroll
-        for (int k = 0; k < kSortKeys; ++k) {
+        for (int k = 0; k < KEYS; ++k) {
             if (k >= rounds) break;
             uint64_t same = __ballot(in[k]);
 #pragma unroll
@@ -194,7 +196,7 @@ __device__ __forceinline__ uint32_t key_of(const SortArgs &a, int64_t i, int64_t
 }
 // Element k of this thread: a wavefront's elements are consecutive, 64 to a round.
 __device__ __forceinline__ int64_t sort_at(int64_t tile, int rounds, int k) {
-    return tile * kSortTile + (threadIdx.x >> 6) * (64 * rounds) + k * 64 + (threadIdx.x & 63);
+    return tile * (kSortThreads * rounds) + (threadIdx.x >> 6) * (64 * rounds) + k * 64 + (threadIdx.x & 63);
 }
 
 constexpr int kOneBits = 9;
@@ -245,17 +247,17 @@ template <int BITS> __global__ void __launch_bounds__(kSortThreads) embed_count_
     using D = Digits<BITS>;
     __shared__ uint32_t bins[D::kBins];
     const int64_t n = row::live_rows(a.n_dev, a.cap), tile = blockIdx.x;
-    uint32_t x[kSortKeys];
+    uint32_t x[kMoveKeys];
 #pragma unroll
-    for (int k = 0; k < kSortKeys; ++k) {
-        const int64_t i = sort_at(tile, kSortKeys, k);
+    for (int k = 0; k < kMoveKeys; ++k) {
+        const int64_t i = sort_at(tile, kMoveKeys, k);
         x[k] = i >= a.cap ? 0 : pass == 0 ? key_of(a, i, n) : a.key[pass & 1][i];
     }
     for (int d = threadIdx.x; d < D::kBins; d += kSortThreads) bins[d] = 0;
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < kSortKeys; ++k) {
-        const int64_t i = sort_at(tile, kSortKeys, k);
+    for (int k = 0; k < kMoveKeys; ++k) {
+        const int64_t i = sort_at(tile, kMoveKeys, k);
         if (i >= a.cap) continue;
         if (pass == 0) {
             a.key[0][i] = x[k];
@@ -273,11 +275,11 @@ template <int BITS> __global__ void __launch_bounds__(kSortThreads) embed_move_k
     __shared__ uint32_t sh[kSortWaves], sums[2][kSortThreads];
     const int64_t tile = blockIdx.x;
     const uint32_t *key = a.key[pass & 1], *pos = a.pos[pass & 1];
-    uint32_t x[kSortKeys], p[kSortKeys], digit[kSortKeys], own[kSortKeys];
-    bool in[kSortKeys];
+    uint32_t x[kMoveKeys], p[kMoveKeys], digit[kMoveKeys], own[kMoveKeys];
+    bool in[kMoveKeys];
 #pragma unroll
-    for (int k = 0; k < kSortKeys; ++k) {
-        const int64_t i = sort_at(tile, kSortKeys, k);
+    for (int k = 0; k < kMoveKeys; ++k) {
+        const int64_t i = sort_at(tile, kMoveKeys, k);
         in[k] = i < a.cap;
         x[k] = in[k] ? key[i] : 0;
         p[k] = in[k] ? pos[i] : 0;
@@ -310,11 +312,11 @@ template <int BITS> __global__ void __launch_bounds__(kSortThreads) embed_move_k
                 earlier[0] += sums[1][q * D::kBins + d];
             }
     }
-    D::rank(digit, in, kSortKeys, bins, own);
+    D::rank(digit, in, kMoveKeys, bins, own);
     D::place(bins, total, earlier, sh);
     uint32_t *key_to = a.key[(pass & 1) ^ 1], *pos_to = a.pos[(pass & 1) ^ 1];
 #pragma unroll
-    for (int k = 0; k < kSortKeys; ++k) {
+    for (int k = 0; k < kMoveKeys; ++k) {
         if (!in[k]) continue;
         const uint32_t to = bins[threadIdx.x >> 6][digit[k]] + own[k];
         key_to[to] = x[k];
@@ -393,26 +395,36 @@ template <int VE> __device__ __forceinline__ void put_part(float *to, int64_t ro
     v.store_upto(to, room);
 }
 
-// The first position whose key is at least k, among [lo, hi).
-__device__ __forceinline__ int64_t lower(const uint32_t *key, int64_t lo, int64_t hi, uint32_t k) {
+// The first position whose key is at least k, among [lo, hi), by LANES neighbouring
+// lanes that ask for the same: each looks at one place, so 262,144 positions take a
+// wavefront three loads behind each other and not eighteen.
+template <int LANES> __device__ __forceinline__ int64_t lower(const uint32_t *key, int64_t lo, int64_t hi, uint32_t k) {
+    const int lane = threadIdx.x & (LANES - 1), shift = (threadIdx.x & 63) & ~(LANES - 1);
     while (lo < hi) {
-        const int64_t mid = (lo + hi) / 2;
-        if (key[mid] < k) lo = mid + 1;
-        else hi = mid;
+        const int64_t step = ceil_div(hi - lo, int64_t(LANES)), p = lo + lane * step;
+        uint64_t below = __ballot(p < hi && key[p] < k) >> shift;
+        if constexpr (LANES < 64) below &= (1ull << LANES) - 1;
+        const int n = __popcll(below);  // the first n places are below k
+        if (n == 0) return lo;
+        hi = min(hi, lo + n * step);
+        lo += (n - 1) * step + 1;
     }
     return lo;
 }
 
-// Rows [v0, v1) that no id names: zeros.  A lane looks for one row, the
-// workgroup writes them.
+// Rows [v0, v1) that no id names: zeros.  The positions that name these rows are marked off.
 template <class T> __device__ __forceinline__ void zero_rows(const SumArgs &a, int64_t blk) {
     __shared__ uint8_t named[kThreads];
+    __shared__ int64_t ends[2];
     const int64_t v0 = blk * a.zero_rows, v1 = min(a.rows, v0 + a.zero_rows);
-    if (v0 + threadIdx.x < v1) {
-        const uint32_t v = static_cast<uint32_t>(v0 + threadIdx.x);
-        const int64_t p = lower(a.key, 0, a.cap, v);
-        named[threadIdx.x] = p < a.cap && a.key[p] == v;
+    named[threadIdx.x] = 0;
+    const int wave = threadIdx.x >> 6;
+    if (wave < 2) {
+        const int64_t p = lower<64>(a.key, 0, a.cap, static_cast<uint32_t>(wave == 0 ? v0 : v1));
+        if ((threadIdx.x & 63) == 0) ends[wave] = p;
     }
+    __syncthreads();
+    for (int64_t p = ends[0] + threadIdx.x; p < ends[1]; p += kThreads) named[a.key[p] - v0] = 1;
     __syncthreads();
     constexpr int VE = 16 / sizeof(T);
     row::Vec<T, VE> zero;
@@ -512,8 +524,9 @@ template <class TG, class T, int VE, int LANES> __global__ void __launch_bounds_
 // Runs that cross tiles.  Groups of kGroup tiles that one run spans, from before them to
 // their end, are summed first, in the place of their first tile's sum: a run of
 // n tiles takes its first tile's wavefront n / kGroup + 2 kGroup loads and not n (262,144
-// positions, the most frequent id 15,000 times, 2,048 wide: 254 us so, JOIN this way).
-constexpr int64_t kGroup = 32;
+// positions, the most frequent id 15,000 times, 2,048 wide: 254 us so, 32 this way).  Few
+// tiles are joined without (kFewTiles): the launch would cost what it saves.
+constexpr int64_t kGroup = 16, kFewTiles = 2048;
 __device__ __forceinline__ bool group_spanned(const SumArgs &a, int64_t u, uint32_t *run) {
     const int64_t beg = u * a.tile, end = beg + kGroup * a.tile;
     if (u == 0 || end > a.cap) return false;
@@ -555,8 +568,8 @@ template <class T, int VE, int LANES> __global__ void __launch_bounds__(kThreads
     const uint32_t run = a.key[next], end_key = a.key[next - 1], beg_key = a.key[beg], before = t > 0 ? a.key[beg - 1] : ~0u;
     if (run >= static_cast<uint32_t>(a.rows) || end_key != run) return;
     if (beg_key == run && before == run) return;  // it began earlier
-    const int64_t over = lower(a.key, next, a.cap, run + 1);
-    const int64_t tiles = ceil_div(over, a.tile), head = min(tiles, ceil_div(t + 1, kGroup) * kGroup);
+    const int64_t over = lower<LANES>(a.key, next, a.cap, run + 1);
+    const int64_t tiles = ceil_div(over, a.tile), head = a.tiles > kFewTiles ? min(tiles, ceil_div(t + 1, kGroup) * kGroup) : tiles;
     const int64_t whole = max(head, over / (a.tile * kGroup) * kGroup);  // groups up to there are spanned
     row::Vec<float, VE> x;
     x.load_upto(a.last + t * a.dim + c, room);
@@ -573,7 +586,7 @@ struct Plan {
     int64_t sort_tiles, tile, tiles;
     size_t key[2], pos[2], counts, first, last, total;
     Plan(int64_t cap, int64_t rows, int64_t dim) {
-        sort_tiles = std::max<int64_t>(1, ceil_div(cap, int64_t(kSortTile)));
+        sort_tiles = std::max<int64_t>(1, ceil_div(cap, int64_t(kMoveTile)));
         // positions of a tile: enough wavefronts for the chip (of 512 columns), up to 64, where the
         // partial rows are a sixteenth of what is read
         tile = 8;
@@ -670,7 +683,7 @@ gnn_status launch_embed_bwd(const void *g, int gdt, const int64_t *ids, const in
             embed_sum_kernel<TG, T, VE, LANES><<<static_cast<unsigned>(grid), kThreads, 0, s>>>(a);
             st = launch_status("embed_sum");
             if (st != GNN_OK || a.tiles < 2) return;
-            if (a.tiles > kGroup) {
+            if (a.tiles > kFewTiles) {
                 const int64_t groups = ceil_div(ceil_div(a.tiles / kGroup, int64_t(64 / LANES)) * a.passes, int64_t(kWaves));
                 embed_group_kernel<VE, LANES><<<static_cast<unsigned>(groups), kThreads, 0, s>>>(a);
                 st = launch_status("embed_group");
