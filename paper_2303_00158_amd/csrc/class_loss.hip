@@ -158,11 +158,14 @@ __global__ void __launch_bounds__(kThreads) class_sums_kernel(const float *z, in
     join_row(r, i, top, sum, last, row_loss);
 }
 
-// From the tiles' strips: 16 rows of a workgroup, each strip of a row to one of 16 threads.
+// From the tiles' strips: ROWS rows of a workgroup, each strip of a row to one of the threads that
+// share it; these meet in a fixed order.  (One row of 1,000 strips takes 16 threads 20 us, 256 of them 6.)
+template <int ROWS>
 __global__ void __launch_bounds__(kThreads) class_join_kernel(const float2 *part, int64_t strips, int64_t b, RowState r, bool last, float *row_loss) {
-    __shared__ float2 sh[16][17];
-    const int x = threadIdx.x & 15, y = threadIdx.x >> 4;
-    const int64_t i = static_cast<int64_t>(blockIdx.x) * 16 + x;
+    constexpr int kLanes = kThreads / ROWS;
+    __shared__ float2 sh[kLanes][ROWS + 1];
+    const int x = threadIdx.x % ROWS, y = threadIdx.x / ROWS;
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * ROWS + x;
     float top = -INFINITY, sum = 0.f;
     auto take = [&](float2 v) {
         const float now = fmaxf(top, v.x), from = now == -INFINITY ? 0.f : now;
@@ -171,14 +174,16 @@ __global__ void __launch_bounds__(kThreads) class_join_kernel(const float2 *part
     };
     if (i < b) {
 #pragma unroll 4
-        for (int64_t p = y; p < strips; p += 16) take(part[p * b + i]);
+        for (int64_t p = y; p < strips; p += kLanes) take(part[p * b + i]);
     }
-    sh[y][x] = make_float2(top, sum);
-    __syncthreads();
-    if (y != 0 || i >= b) return;
-#pragma unroll
-    for (int k = 1; k < 16; ++k) take(sh[k][x]);
-    join_row(r, i, top, sum, last, row_loss);
+    // halves until one is left
+    for (int n = kLanes; n > 1; n /= 2) {
+        sh[y][x] = make_float2(top, sum);
+        __syncthreads();
+        if (y < n / 2) take(sh[y + n / 2][x]);
+        __syncthreads();
+    }
+    if (y == 0 && i < b) join_row(r, i, top, sum, last, row_loss);
 }
 
 // The weighted sum of the rows' losses, in a fixed order, and the largest weight (bf16; fp32
@@ -467,8 +472,9 @@ gnn_status launch_update_ce(const CeArgs &a, void *ws, hipStream_t s) {
         if (pl.bf) {
             const LogitArgs t = tile_args(c0, cols);
             GNN_TRY(logit_sums(t, s));
-            class_join_kernel<<<static_cast<unsigned>(ceil_div(a.b, int64_t(16))), kThreads, 0, s>>>(t.part, logit_strips(a.b, cols, t.R), a.b, r, last,
-                                                                                                  row_loss);
+            const int64_t strips = logit_strips(a.b, cols, t.R);
+            if (a.b <= 256) class_join_kernel<1><<<static_cast<unsigned>(a.b), kThreads, 0, s>>>(t.part, strips, a.b, r, last, row_loss);
+            else class_join_kernel<16><<<static_cast<unsigned>(ceil_div(a.b, int64_t(16))), kThreads, 0, s>>>(t.part, strips, a.b, r, last, row_loss);
             GNN_LAUNCHED("update_ce_join");
             continue;
         }
