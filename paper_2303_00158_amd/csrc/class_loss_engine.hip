@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(gemm::kThreads) class_engine_pair_kernel(Produ
 
 int64_t splits_f32(Kind, int64_t M, int64_t N, int64_t R, bool may_split) {
     const int tile = pick_tile(M, N);
-    const int64_t tiles = ceil_div(M, tile) * ceil_div(N, tile), chunks = ceil_div(R, int64_t(Cfg<false>::BK));
+    const int64_t tiles = std::max<int64_t>(ceil_div(M, tile) * ceil_div(N, tile), 1), chunks = ceil_div(R, int64_t(Cfg<false>::BK));
     if (!may_split || tiles >= 128 || chunks < 16) return 1;
     return std::min<int64_t>({chunks / 4, ceil_div(256, tiles), 16});
 }

@@ -212,6 +212,9 @@ def test_no_rows_and_no_bias(gemm):
     check(call(a, wt, None, labels, gemm), want, offs)
     outs = call(a[:0], wt, bias, labels[:0], gemm)
     assert (outs[0] == 0).all() and (outs[2] == 0).all() and (outs[3] == 0).all()
+    a, wt, bias, labels = problem(gen, 0, 48, 5000)
+    outs = call(a, wt, bias, labels, gemm)
+    assert (outs[0] == 0).all() and (outs[2] == 0).all() and (outs[3] == 0).all()
 
 
 @pytest.mark.gpu
@@ -339,6 +342,8 @@ def test_workspace_sizes():
     # a piece, not the whole: 100,000 rows of 1,000,000 classes would have 400 GB of logits
     assert size(100_000, 256, 1_000_000, gnn.GNN_BF16, 1) < 4 << 30
     assert 0 < size(0, 8, 10, gnn.GNN_F32, 1) <= size(10, 8, 10, gnn.GNN_F32, 1)
+    for gemm in (gnn.GNN_F32, gnn.GNN_BF16):  # no rows and a long reduction over the classes
+        assert size(0, 8, 100_000, gemm, 1) > 0
     assert size(1000, 64, 500, gnn.GNN_F32, 0) <= size(1000, 64, 500, gnn.GNN_F32, 1)
     assert gnn.lib().gnn_update_ce_workspace_size(1, 8, 10, 0, 1, None) == gnn.GNN_EINVAL
     nb = ctypes.c_size_t()
