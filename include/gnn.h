@@ -760,7 +760,7 @@ typedef struct gnn_adamw_tensor {
     void *m, *v;              /* [device] state, n of the call's sdt each (GNN_F8E4M3: m and sqrt(v)), updated */
     float *m_scale, *v_scale; /* [device] fp32 ceil(n / GNN_ADAMW_GROUP) for GNN_F8E4M3; else NULL */
     uint16_t *shadow;         /* [device] bf16 n, or NULL: written with the new w */
-    int64_t n;
+    int64_t n;                /* below 2^33 */
     double weight_decay;      /* finite, not negative */
     gnn_dtype gdt;            /* GNN_F32 or GNN_BF16 */
 } gnn_adamw_tensor;

@@ -877,7 +877,7 @@ gnn_status gnn_adamw(const gnn_adamw_tensor *tensors, int64_t count, gnn_dtype s
         const gnn_adamw_tensor &t = tensors[i];
         const long long at = static_cast<long long>(i);
         GNN_CHECK(act_dtype(t.gdt), GNN_EUNSUPPORTED, "%s: tensor %lld: gdt must be GNN_F32 or GNN_BF16", who, at);
-        GNN_CHECK(t.n >= 0 && t.n < (1ll << 34), GNN_EINVAL, "%s: tensor %lld: n out of [0, 2^34)", who, at);
+        GNN_CHECK(t.n >= 0 && t.n < (1ll << 33), GNN_EINVAL, "%s: tensor %lld: n out of [0, 2^33)", who, at);
         GNN_CHECK(t.weight_decay >= 0 && std::isfinite(t.weight_decay), GNN_EINVAL,
                   "%s: tensor %lld: weight_decay must be finite and not negative", who, at);
         if (t.n == 0) continue;

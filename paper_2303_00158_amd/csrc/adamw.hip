@@ -64,6 +64,7 @@ struct Args {
     const int64_t *step_dev;
 };
 static_assert(sizeof(Args) <= 4096, "kernel arguments");
+static_assert((1ll << 33) / kChunk <= kMaxGrid / kThreads, "a tensor fits a launch");
 
 // What goes by the learning rate and the step.
 struct Rates {

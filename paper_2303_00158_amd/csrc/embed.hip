@@ -114,9 +114,14 @@ struct SortArgs {
     int64_t cap, rows;
     uint32_t *key[2], *pos[2];
     uint32_t *counts;  // tiles x bins
+    uint32_t *totals;  // bins
     int64_t tiles;
     int passes;
 };
+// Up to so many tiles each adds up the others' counts by itself (128 KB to 2 MB out of
+// the L2, a few us); above, what that reads grows with the square of the tiles, and a launch
+// of its own makes the counts of earlier tiles.
+constexpr int64_t kDirectTiles = 256;
 
 // Digits of BITS bits, and the counts of a tile's wavefronts.
 template <int BITS> struct Digits {
@@ -269,6 +274,29 @@ template <int BITS> __global__ void __launch_bounds__(kSortThreads) embed_count_
     for (int d = threadIdx.x; d < D::kBins; d += kSortThreads) a.counts[tile * D::kBins + d] = bins[d];
 }
 
+// counts[t][d] becomes the sum over the tiles before t, totals[d] the sum over all: 32 digits
+// of a workgroup, the tiles in 32 ranges.
+template <int BITS> __global__ void __launch_bounds__(kSortThreads) embed_scan_kernel(SortArgs a) {
+    constexpr int kBins = Digits<BITS>::kBins;
+    __shared__ uint32_t sh[32][33];
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5, d = blockIdx.x * 32 + x;
+    const int64_t per = ceil_div(a.tiles, int64_t(32)), beg = min(a.tiles, y * per), end = min(a.tiles, beg + per);
+    uint32_t sum = 0;
+#pragma unroll 8
+    for (int64_t t = beg; t < end; ++t) sum += a.counts[t * kBins + d];
+    sh[y][x] = sum;
+    __syncthreads();
+    uint32_t before = 0;
+    for (int q = 0; q < y; ++q) before += sh[q][x];
+    if (y == 31) a.totals[d] = before + sum;
+#pragma unroll 8
+    for (int64_t t = beg; t < end; ++t) {
+        const uint32_t c = a.counts[t * kBins + d];
+        a.counts[t * kBins + d] = before;
+        before += c;
+    }
+}
+
 template <int BITS> __global__ void __launch_bounds__(kSortThreads) embed_move_kernel(SortArgs a, int pass) {
     using D = Digits<BITS>;
     __shared__ typename D::WaveBins bins;
@@ -289,6 +317,13 @@ template <int BITS> __global__ void __launch_bounds__(kSortThreads) embed_move_k
     uint32_t total[D::kEach], earlier[D::kEach];
     auto add_up = [&](int d, int64_t first, int64_t step, uint32_t &all, uint32_t &before) {
         all = before = 0;
+        if (a.tiles > kDirectTiles) {
+            if (first == 0) {
+                all = a.totals[d];
+                before = a.counts[tile * D::kBins + d];
+            }
+            return;
+        }
 #pragma unroll 8
         for (int64_t t = first; t < a.tiles; t += step) {
             const uint32_t c = a.counts[t * D::kBins + d];
@@ -347,6 +382,10 @@ gnn_status sort_ids(SortArgs a, int *where, hipStream_t s) {
         for (int pass = 0; pass < a.passes; ++pass) {
             embed_count_kernel<BITS><<<static_cast<unsigned>(a.tiles), kSortThreads, 0, s>>>(a, pass);
             GNN_LAUNCHED("embed_count");
+            if (a.tiles > kDirectTiles) {
+                embed_scan_kernel<BITS><<<Digits<BITS>::kBins / 32, kSortThreads, 0, s>>>(a);
+                GNN_LAUNCHED("embed_scan");
+            }
             embed_move_kernel<BITS><<<static_cast<unsigned>(a.tiles), kSortThreads, 0, s>>>(a, pass);
             GNN_LAUNCHED("embed_move");
         }
@@ -584,7 +623,7 @@ template <class T, int VE, int LANES> __global__ void __launch_bounds__(kThreads
 
 struct Plan {
     int64_t sort_tiles, tile, tiles;
-    size_t key[2], pos[2], counts, first, last, total;
+    size_t key[2], pos[2], counts, totals, first, last, total;
     Plan(int64_t cap, int64_t rows, int64_t dim) {
         sort_tiles = std::max<int64_t>(1, ceil_div(cap, int64_t(kMoveTile)));
         // positions of a tile: enough wavefronts for the chip (of 512 columns), up to 64, where the
@@ -600,6 +639,7 @@ struct Plan {
             pos[i] = c.take(static_cast<size_t>(cap) * 4);
         }
         counts = c.take(static_cast<size_t>(bins * sort_tiles) * 4);
+        totals = c.take(static_cast<size_t>(bins) * 4);
         first = c.take(static_cast<size_t>(tiles * dim) * 4);
         last = c.take(static_cast<size_t>(tiles * dim) * 4);
         total = round_up(c.off, 256);
@@ -632,32 +672,30 @@ size_t embed_bwd_ws_bytes(int64_t cap, int64_t rows, int64_t dim) { return Plan(
 gnn_status launch_embed_bwd(const void *g, int gdt, const int64_t *ids, const int64_t *n_dev, int64_t cap, int64_t dim,
                             float scale, int64_t rows, bool add, void *d_table, int ddt, void *ws, hipStream_t s) {
     const Plan pl(cap, rows, dim);
-    char *base = static_cast<char *>(ws);
+    // (without ids there may be no workspace)
+    auto at = [&](size_t off) -> void * { return cap > 0 ? static_cast<char *>(ws) + off : nullptr; };
     SortArgs o{};
     o.ids = ids;
     o.n_dev = n_dev;
     o.cap = cap;
     o.rows = rows;
     for (int i = 0; i < 2; ++i) {
-        o.key[i] = reinterpret_cast<uint32_t *>(base + pl.key[i]);
-        o.pos[i] = reinterpret_cast<uint32_t *>(base + pl.pos[i]);
+        o.key[i] = static_cast<uint32_t *>(at(pl.key[i]));
+        o.pos[i] = static_cast<uint32_t *>(at(pl.pos[i]));
     }
-    o.counts = reinterpret_cast<uint32_t *>(base + pl.counts);
+    o.counts = static_cast<uint32_t *>(at(pl.counts));
+    o.totals = static_cast<uint32_t *>(at(pl.totals));
     o.tiles = pl.sort_tiles;
-    int where = 0;
-    if (cap > 0) GNN_TRY(sort_ids(o, &where, s));
     SumArgs a{};
     a.g = g;
-    a.key = o.key[where];
-    a.pos = o.pos[where];
     a.cap = cap;
     a.rows = rows;
     a.dim = dim;
     a.scale = scale;
     a.add = add;
     a.d_table = d_table;
-    a.first = reinterpret_cast<float *>(base + pl.first);
-    a.last = reinterpret_cast<float *>(base + pl.last);
+    a.first = static_cast<float *>(at(pl.first));
+    a.last = static_cast<float *>(at(pl.last));
     a.tile = pl.tile;
     a.tiles = pl.tiles;
     // a workgroup of zeros: about 64 KB
@@ -680,6 +718,13 @@ gnn_status launch_embed_bwd(const void *g, int gdt, const int64_t *ids, const in
                 return;
             }
             if (grid == 0) return;
+            if (cap > 0) {
+                int where = 0;
+                st = sort_ids(o, &where, s);
+                if (st != GNN_OK) return;
+                a.key = o.key[where];
+                a.pos = o.pos[where];
+            }
             embed_sum_kernel<TG, T, VE, LANES><<<static_cast<unsigned>(grid), kThreads, 0, s>>>(a);
             st = launch_status("embed_sum");
             if (st != GNN_OK || a.tiles < 2) return;

@@ -373,7 +373,7 @@ P = (ctypes.addressof(BUF) + 255) // 256 * 256  # any address: a refused call re
     (dict(step=0), gnn.GNN_EINVAL, "step"), (dict(lr_dev=P + 2), gnn.GNN_EINVAL, "misaligned"),
     (dict(step_dev=P + 4), gnn.GNN_EINVAL, "misaligned"),
     (dict(t=dict(gdt=2)), gnn.GNN_EUNSUPPORTED, "gdt"), (dict(t=dict(n=-1)), gnn.GNN_EINVAL, "n out"),
-    (dict(t=dict(n=1 << 34)), gnn.GNN_EINVAL, "n out"), (dict(t=dict(weight_decay=-0.1)), gnn.GNN_EINVAL, "decay"),
+    (dict(t=dict(n=1 << 33)), gnn.GNN_EINVAL, "n out"), (dict(t=dict(weight_decay=-0.1)), gnn.GNN_EINVAL, "decay"),
     (dict(t=dict(weight_decay=math.nan)), gnn.GNN_EINVAL, "decay"), (dict(t=dict(w=None)), gnn.GNN_EINVAL, "NULL"),
     (dict(t=dict(g=None)), gnn.GNN_EINVAL, "NULL"), (dict(t=dict(m=None)), gnn.GNN_EINVAL, "NULL"),
     (dict(t=dict(v=None)), gnn.GNN_EINVAL, "NULL"), (dict(sdt=3, t=dict(m_scale=None)), gnn.GNN_EINVAL, "NULL"),

@@ -180,6 +180,22 @@ def test_gradient_of_tables_at_the_digits_edges(rows, n):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows, law", [(300, "zipf"), (40_000, "zipf"), (5_000_000, "zipf"), (7, "same")])
+@pytest.mark.parametrize("n", [524_288, 524_289, 3_000_001])
+def test_gradient_of_many_positions(n, rows, law):
+    """Both ways to the counts of earlier tiles, runs of thousands of tiles."""
+    gen = torch.Generator().manual_seed(n + rows)
+    ids = make_ids(gen, law, n, rows)
+    # sums of whole numbers are exact in any order
+    g = torch.randint(-3, 4, (n, 4), generator=gen).float().to(DEV)
+    d = torch.full((rows, 4), 7.0, device=DEV)
+    gnn.embed_bwd(g, ids, d)
+    there = (ids >= 0) & (ids < rows)
+    want = torch.zeros((rows, 4), dtype=torch.float64, device=DEV).index_put_((ids[there],), g[there].double(), accumulate=True)
+    assert torch.equal(d.double(), want)
+
+
+@pytest.mark.gpu
 def test_gradient_by_a_device_count():
     gen = torch.Generator().manual_seed(8)
     ids, g = make_ids(gen, "zipf", 9000, 400), rand(gen, 9000, 20)
