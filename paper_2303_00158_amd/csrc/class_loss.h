@@ -45,6 +45,8 @@ struct LogitArgs {
     RowState rows;
     // sums: a wavefront's columns' largest logit and sum for each row
     float2 *part;          // strips x M
+    float *keep;           // the logits themselves, rows of ld_keep, or null
+    int64_t ld_keep;
     // dZ over *scale
     uint16_t *dz;          // rows of ld
     int64_t ld;

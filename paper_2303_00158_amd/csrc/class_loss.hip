@@ -4,10 +4,11 @@
 //   dZ = s (exp(z - lse) - onehot(y)),  dWt = dZ^T A,  db = sum_i dZ,  dA = dZ Wt.
 //
 // Bound by the matrix products: 2 b K C operations for the loss, 6 b K C with the
-// gradients, and 2 b K C more because the logits are computed twice, once for the rows'
-// sums and once for dZ (in fp32 only where there is more than one piece).  Only one
-// piece of dZ (fp32: of Z and dZ, in one place) exists at a time, so memory goes by b, not by b C.
-// bf16 logits stay in the tiles' accumulators (class_loss_tile.hip).
+// gradients, and 2 b K C more where the logits are computed twice, once for the rows'
+// sums and once for dZ.  bf16 logits stay in the tiles' accumulators (class_loss_tile.hip); only
+// one piece of dZ exists at a time, so memory goes by b, not by b C.  Of long reductions up to
+// 2^28 logits (1 GB) are kept in fp32 from the first time, which spares them the
+// second (4,096 x 2,048 x 100,003, two thirds kept: 5,644 us without, 5,231 with).  fp32 keeps the logits of its one piece, or computes them twice.
 //
 // dZ is an operand of the products behind it, so bf16 rounds it, and it is rounded over the
 // largest row weight, which the products' ends multiply back: with a common weight
@@ -272,6 +273,48 @@ __global__ void __launch_bounds__(kThreads) class_dz_kernel(float *z, int64_t ld
     part[p * ld + col] = t;
 }
 
+// The same over the largest weight from logits that were kept, in bf16 and with their biases in them: 32
+// threads of eight columns, times 8 rows.
+__global__ void __launch_bounds__(kThreads) class_dz_kept_kernel(const float *z, int64_t ldz, uint16_t *dz, int64_t ld, int64_t b, int64_t cols,
+                                                                 int64_t c0, RowState r, const float *scale, float *part, int64_t parts) {
+    __shared__ float sh[8][kStripe];
+    const int64_t stripes = ceil_div(ld, int64_t(kStripe)), stripe = blockIdx.x % stripes, p = blockIdx.x / stripes;
+    const int64_t per = ceil_div(b, parts), beg = min(b, p * per), end = min(b, beg + per);
+    const int x = (threadIdx.x & 31) * 8, y = threadIdx.x >> 5;
+    const int64_t c = stripe * kStripe + x, room = cols - c;
+    const float inverse = 1.f / *scale;
+    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (c < ld) {
+#pragma unroll 2
+        for (int64_t i = beg + y; i < end; i += 8) {
+            const float w = r.weight[i] * inverse, lse = r.lse[i];
+            const int64_t label = r.label[i] - c0 - c;
+            row::Vec<float, 8> zz;
+            zz.load_upto(z + i * ldz + c, room);
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float d = w * __builtin_amdgcn_exp2f((zz.get(e) - lse) * 1.4426950408889634f);
+                v[e] = w != 0.f && e < room ? d - (e == label ? w : 0.f) : 0.f;
+                sum[e] += v[e];
+            }
+            row::Vec<uint16_t, 8> o;
+            o.set(v);
+            o.store(dz + i * ld + c);
+        }
+    }
+    if (!part) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sh[y][x + e] = sum[e];
+    __syncthreads();
+    const int64_t col = stripe * kStripe + threadIdx.x;
+    if (col >= ld) return;
+    float t = 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) t += sh[k][threadIdx.x];
+    part[p * ld + col] = t;
+}
+
 // What is left of a piece behind its products, in one launch: the partials of dWt and, behind
 // the last piece, of dA, in their order, rows of `ld` to rows of `cols`; and db, 32 columns of a
 // workgroup, every eighth part to a thread.
@@ -351,19 +394,35 @@ constexpr int64_t kPieceCols = 256;  // its columns: a multiple of these
 constexpr int64_t kSumsPieces = 8;   // such pieces that the bf16 sums take at once: a strip has 32 columns or more, its
                                      // part 8 bytes a row, so that theirs fit in a piece of dZ
 
+// Logits that bf16 keeps for dZ, about, and the reduction from which on: 134 million kept
+// ones cost 150 us on their way out of the tiles and 155 in dZ's pass; made again, 580 with dZ at a
+// reduction of 2,048, so that both cost the same at some 1,050.
+constexpr int64_t kKept = 1 << 28, kKeepK = 1536;
+
 int64_t row_of(int64_t n) { return (n + 7) / 8 * 8; }
 
 struct Plan {
     bool bf;
-    int64_t ldk, piece, pieces, sums_piece, parts[2];
+    int64_t ldk, c, piece, pieces, sums_piece, parts[2];
+    int64_t kept, kept_parts;         // classes [0, kept): whole pieces, or all
     int64_t da_splits, dw_splits[2];  // of a full piece and of the last one
-    size_t label, weight, top, sum, z_label, lse, row_loss, scale, a, w, z, db, dw_part, da_part, total;
-    Plan(int64_t b, int64_t k, int64_t c, int gemm_dt, bool grads) {
+    size_t label, weight, top, sum, z_label, lse, row_loss, scale, a, w, z, zk, db, dw_part, da_part, total;
+    // classes that the rows' sums take at once from c0 (copies of the weights are a piece's)
+    int64_t segment(int64_t c0, bool copy) const {
+        const int64_t most = copy ? piece : c0 < kept ? kept : sums_piece;
+        return std::min(most, (c0 < kept ? std::min(kept, c) : c) - c0);
+    }
+    Plan(int64_t b, int64_t k, int64_t classes, int gemm_dt, bool grads) : c(classes) {
         bf = gemm_dt == GNN_BF16;
         ldk = row_of(k);
         piece = std::min(row_of(c), std::max<int64_t>(kPiece / std::max<int64_t>(b, 1) / kPieceCols * kPieceCols, kPieceCols));
         pieces = ceil_div(c, piece);
         sums_piece = std::min(row_of(c), bf ? kSumsPieces * piece : piece);
+        kept = 0;
+        if (bf && grads && k >= kKeepK && b > 0) {
+            kept = kKept / b / piece * piece;
+            if (kept >= c) kept = row_of(c);
+        }
         const size_t es = bf ? 2 : 4;
         const int64_t last = row_of(c - (pieces - 1) * piece);
         auto splits = [&](Kind kind, int64_t m, int64_t n, int64_t r) {
@@ -384,17 +443,21 @@ struct Plan {
         // one after the other: the sums' strips, dZ (bf16); logits and dZ (fp32)
         int64_t strips = 0;
         if (bf && b > 0)
-            for (const int64_t step : {piece, sums_piece})
-                for (int64_t c0 = 0; c0 < c; c0 += step) strips = std::max(strips, logit_strips(b, std::min(step, c - c0), ldk));
+            for (const bool copy : {false, true})
+                for (int64_t c0 = 0; c0 < c; c0 += segment(c0, copy)) strips = std::max(strips, logit_strips(b, segment(c0, copy), ldk));
+        zk = cv.take(static_cast<size_t>(b * kept) * 4);
         z = cv.take(std::max(static_cast<size_t>(b * strips) * 8, bf && !grads ? size_t(0) : static_cast<size_t>(b * piece) * es));
         db = dw_part = da_part = 0;
-        da_splits = dw_splits[0] = dw_splits[1] = parts[0] = parts[1] = 1;
+        da_splits = dw_splits[0] = dw_splits[1] = parts[0] = parts[1] = kept_parts = 1;
         if (grads) {
             const int64_t width[2] = {piece, last};
-            int64_t most = 0, dw = 0;
+            auto row_parts = [&](int64_t n, int64_t rows_each) {
+                return std::max<int64_t>(1, std::min<int64_t>(ceil_div(2048, ceil_div(n, int64_t(kStripe))), ceil_div(b, rows_each)));
+            };
+            kept_parts = row_parts(piece, 32);
+            int64_t most = kept > 0 ? kept_parts * piece : 0, dw = 0;
             for (int i = 0; i < 2; ++i) {
-                parts[i] = bf ? logit_row_strips(b, width[i], ldk)
-                              : std::max<int64_t>(1, std::min<int64_t>(ceil_div(2048, ceil_div(width[i], int64_t(kStripe))), ceil_div(b, int64_t(16))));
+                parts[i] = bf ? logit_row_strips(b, width[i], ldk) : row_parts(width[i], 16);
                 most = std::max(most, parts[i] * width[i]);
                 dw_splits[i] = splits(kTT, width[i], k, b);
                 if (dw_splits[i] > 1) dw = std::max(dw, dw_splits[i] * width[i]);
@@ -460,13 +523,13 @@ gnn_status launch_update_ce(const CeArgs &a, void *ws, hipStream_t s) {
     };
     auto tile_args = [&](int64_t c0, int64_t cols) {
         return LogitArgs{static_cast<const uint16_t *>(A), static_cast<const uint16_t *>(w), lda, ldw, a.b, cols, std::min(lda, ldw), c0,
-                         a.bias ? a.bias + c0 : nullptr, r, reinterpret_cast<float2 *>(z), reinterpret_cast<uint16_t *>(z), row_of(cols), scale,
+                         a.bias ? a.bias + c0 : nullptr, r, reinterpret_cast<float2 *>(z), c0 < pl.kept ? f(pl.zk) + c0 : nullptr, pl.kept,
+                         reinterpret_cast<uint16_t *>(z), row_of(cols), scale,
                          a.db ? f(pl.db) : nullptr};
     };
-    // the rows' sums and losses (copies of the weights are a piece's)
-    const int64_t step = copy_w ? pl.piece : pl.sums_piece;
-    for (int64_t c0 = 0; any && c0 < a.c; c0 += step) {
-        const int64_t cols = std::min(step, a.c - c0);
+    // the rows' sums and losses
+    for (int64_t c0 = 0, cols; any && c0 < a.c; c0 += cols) {
+        cols = pl.segment(c0, copy_w);
         const bool last = c0 + cols == a.c;
         GNN_TRY(weights(c0, cols));
         if (pl.bf) {
@@ -498,20 +561,25 @@ gnn_status launch_update_ce(const CeArgs &a, void *ws, hipStream_t s) {
         const int64_t c0 = q * pl.piece, cols = std::min(pl.piece, a.c - c0), ld = row_of(cols);
         const bool again = pl.pieces > 1, last = q + 1 == pl.pieces;
         const int which = last ? 1 : 0;
+        int64_t parts = pl.parts[which];
         // (a single piece's weights are still there, and in fp32 its logits)
-        if (any && again) GNN_TRY(weights(c0, cols));
-        if (any && pl.bf) {
+        if (any && again && (c0 >= pl.kept || a.d_a)) GNN_TRY(weights(c0, cols));
+        if (any && c0 < pl.kept) {
+            parts = pl.kept_parts;
+            class_dz_kept_kernel<<<static_cast<unsigned>(ceil_div(ld, int64_t(kStripe)) * parts), kThreads, 0, s>>>(
+                f(pl.zk) + c0, pl.kept, reinterpret_cast<uint16_t *>(z), ld, a.b, cols, c0, r, scale, a.db ? f(pl.db) : nullptr, parts);
+            GNN_LAUNCHED("update_ce_dz");
+        } else if (any && pl.bf) {
             GNN_TRY(logit_dz(tile_args(c0, cols), s));
         } else if (any) {
             if (again) GNN_TRY(logits(cols));
-            const int64_t blocks = ceil_div(ld, int64_t(kStripe)) * pl.parts[which] + (owed ? 1 : 0);
-            class_dz_kernel<<<static_cast<unsigned>(blocks), kThreads, 0, s>>>(z, ld, a.b, cols, c0, a.bias, r, a.db ? f(pl.db) : nullptr,
-                                                                               pl.parts[which], total);
+            const int64_t blocks = ceil_div(ld, int64_t(kStripe)) * parts + (owed ? 1 : 0);
+            class_dz_kernel<<<static_cast<unsigned>(blocks), kThreads, 0, s>>>(z, ld, a.b, cols, c0, a.bias, r, a.db ? f(pl.db) : nullptr, parts, total);
             GNN_LAUNCHED("update_ce_dz");
             owed = false;
         }
         ReduceDb rb{};
-        if (a.db) rb = ReduceDb{f(pl.db), any ? pl.parts[which] : 0, ld, cols, factor, a.db + c0, ceil_div(cols, int64_t(32))};
+        if (a.db) rb = ReduceDb{f(pl.db), any ? parts : 0, ld, cols, factor, a.db + c0, ceil_div(cols, int64_t(32))};
         Reduce rw{}, ra{};
         Product pw{z, A, ld, lda, cols, a.k, a.b, a.b, nullptr, a.dwdt, a.k, 1, 0, false, factor};
         if (a.dwt) {

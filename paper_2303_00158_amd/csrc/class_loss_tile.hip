@@ -117,7 +117,7 @@ template <class C> struct LogitTile {
 
 // Largest logit of each row among a wavefront's columns, and the sum of exp(z - largest):
 // each lane's own first (of 4 NI columns), then those of the four lanes that share the row.
-template <class C> __global__ void __launch_bounds__(C::kThreads, C::PER_CU) class_sums_tile_kernel(LogitArgs a) {
+template <class C, bool KEEP> __global__ void __launch_bounds__(C::kThreads, C::PER_CU) class_sums_tile_kernel(LogitArgs a) {
     __shared__ __attribute__((aligned(16))) uint16_t st0[C::kStageElems], st1[C::kStageElems];
     tile::Acc<C> acc;
     LogitTile<C> at;
@@ -157,6 +157,16 @@ template <class C> __global__ void __launch_bounds__(C::kThreads, C::PER_CU) cla
         sum += __shfl_xor(sum, 16, 64);
         sum += __shfl_xor(sum, 32, 64);
         if (g == 0 && r < a.M) a.part[at.col_strip * a.M + r] = make_float2(all, sum);
+        if constexpr (KEEP) {
+#pragma unroll
+            for (int j = 0; j < C::NI / 2; ++j) {
+                float o[8];
+                eight_of(tile::f32x4{x[2 * j][0], x[2 * j][1], x[2 * j][2], x[2 * j][3]},
+                         tile::f32x4{x[2 * j + 1][0], x[2 * j + 1][1], x[2 * j + 1][2], x[2 * j + 1][3]}, o);
+                const int64_t c = at.col0 + (g & 1) * 16 + (g >> 1) * 8 + 32 * j;
+                if (r < a.M && c < a.N) tile::put8(a.keep + r * a.ld_keep + c, a.N - c, o);
+            }
+        }
     }
 }
 
@@ -298,7 +308,8 @@ gnn_status logit_sums(const LogitArgs &a, hipStream_t s) {
         using C = decltype(c);
         const int64_t grid = static_cast<int64_t>(round_up(ceil_div(a.M, int64_t(C::BM)) * ceil_div(a.N, int64_t(C::BN)), wide::kXcds));
         GNN_CHECK(grid <= kMaxGrid / C::kThreads, GNN_ESIZE, "update_ce: sizes exceed the grid limit");
-        class_sums_tile_kernel<C><<<static_cast<unsigned>(grid), C::kThreads, 0, s>>>(a);
+        if (a.keep) class_sums_tile_kernel<C, true><<<static_cast<unsigned>(grid), C::kThreads, 0, s>>>(a);
+        else class_sums_tile_kernel<C, false><<<static_cast<unsigned>(grid), C::kThreads, 0, s>>>(a);
         GNN_LAUNCHED("update_ce_sums");
         return GNN_OK;
     });

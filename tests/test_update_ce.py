@@ -136,7 +136,8 @@ def test_loss_and_gradients(b, k, c, gemm):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("gemm", [gnn.GNN_F32, gnn.GNN_BF16])
-@pytest.mark.parametrize("b, k, c", [(8200, 40, 17_000), (100_000, 24, 1500), (600_001, 8, 520), (3000, 72, 50_000)])
+@pytest.mark.parametrize("b, k, c", [(8200, 40, 17_000), (100_000, 24, 1500), (600_001, 8, 520), (3000, 72, 50_000),
+                                     (1500, 1536, 9000), (20_000, 1541, 14_000), (70_000, 1536, 2000)])
 def test_several_pieces(b, k, c, gemm):
     gen = torch.Generator().manual_seed(b)
     dt = BF16 if gemm == gnn.GNN_BF16 else F32
