@@ -159,6 +159,42 @@ __global__ void __launch_bounds__(kThreads) class_sums_kernel(const float *z, in
     join_row(r, i, top, sum, last, row_loss);
 }
 
+// The sums of strips of a piece of logits, for few long rows: one workgroup a strip and row.
+constexpr int64_t kStrip = 2048, kStripRows = 1024;  // (2 rows of 131,072 classes with a workgroup a row: 617 us in all, STRIPFIG so)
+__global__ void __launch_bounds__(kThreads) class_strips_kernel(const float *z, int64_t b, int64_t cols, int64_t ld, int64_t c0, const float *bias,
+                                                                RowState r, float2 *part) {
+    __shared__ float sh[2][kThreads / 64];
+    const int64_t i = blockIdx.x % b, strip = blockIdx.x / b, beg = strip * kStrip;
+    const int64_t y = r.label[i] < 0 ? -1 : r.label[i] - c0;
+    constexpr int kOwn = kStrip / kThreads;
+    float x[kOwn], top = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < kOwn; ++e) {
+        const int64_t c = beg + e * kThreads + threadIdx.x;
+        x[e] = c < cols ? z[i * ld + c] + (bias ? bias[c0 + c] : 0.f) : -INFINITY;
+        if (c == y && c < cols) r.z_label[i] = x[e];
+        top = fmaxf(top, x[e]);
+    }
+    const int wave = threadIdx.x >> 6;
+    top = loss::wave_max(top);
+    if ((threadIdx.x & 63) == 0) sh[0][wave] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kThreads / 64; ++w) top = fmaxf(top, sh[0][w]);
+    const float from = top == -INFINITY ? 0.f : top;
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < kOwn; ++e) sum += expf(x[e] - from);
+    sum = loss::wave_sum(sum);
+    if ((threadIdx.x & 63) == 0) sh[1][wave] = sum;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kThreads / 64; ++w) sum += sh[1][w];
+    part[strip * b + i] = make_float2(top, sum);
+}
+
 // From the tiles' strips: ROWS rows of a workgroup, each strip of a row to one of the threads that
 // share it; these meet in a fixed order.  (One row of 1,000 strips takes 16 threads 20 us, 256 of them 6.)
 template <int ROWS>
@@ -185,6 +221,13 @@ __global__ void __launch_bounds__(kThreads) class_join_kernel(const float2 *part
         __syncthreads();
     }
     if (y == 0 && i < b) join_row(r, i, top, sum, last, row_loss);
+}
+
+gnn_status join(const float2 *part, int64_t strips, int64_t b, const RowState &r, bool last, float *row_loss, hipStream_t s) {
+    if (b <= 256) class_join_kernel<1><<<static_cast<unsigned>(b), kThreads, 0, s>>>(part, strips, b, r, last, row_loss);
+    else class_join_kernel<16><<<static_cast<unsigned>(ceil_div(b, int64_t(16))), kThreads, 0, s>>>(part, strips, b, r, last, row_loss);
+    GNN_LAUNCHED("update_ce_join");
+    return GNN_OK;
 }
 
 // The weighted sum of the rows' losses, in a fixed order, and the largest weight (bf16; fp32
@@ -406,7 +449,7 @@ struct Plan {
     int64_t ldk, c, piece, pieces, sums_piece, parts[2];
     int64_t kept, kept_parts;         // classes [0, kept): whole pieces, or all
     int64_t da_splits, dw_splits[2];  // of a full piece and of the last one
-    size_t label, weight, top, sum, z_label, lse, row_loss, scale, a, w, z, zk, db, dw_part, da_part, total;
+    size_t label, weight, top, sum, z_label, lse, row_loss, scale, a, w, z, zk, strip_part, db, dw_part, da_part, total;
     // classes that the rows' sums take at once from c0 (copies of the weights are a piece's)
     int64_t segment(int64_t c0, bool copy) const {
         const int64_t most = copy ? piece : c0 < kept ? kept : sums_piece;
@@ -447,6 +490,7 @@ struct Plan {
                 for (int64_t c0 = 0; c0 < c; c0 += segment(c0, copy)) strips = std::max(strips, logit_strips(b, segment(c0, copy), ldk));
         zk = cv.take(static_cast<size_t>(b * kept) * 4);
         z = cv.take(std::max(static_cast<size_t>(b * strips) * 8, bf && !grads ? size_t(0) : static_cast<size_t>(b * piece) * es));
+        strip_part = cv.take(!bf && b < kStripRows ? static_cast<size_t>(b * ceil_div(piece, kStrip)) * 8 : 0);
         db = dw_part = da_part = 0;
         da_splits = dw_splits[0] = dw_splits[1] = parts[0] = parts[1] = kept_parts = 1;
         if (grads) {
@@ -535,14 +579,19 @@ gnn_status launch_update_ce(const CeArgs &a, void *ws, hipStream_t s) {
         if (pl.bf) {
             const LogitArgs t = tile_args(c0, cols);
             GNN_TRY(logit_sums(t, s));
-            const int64_t strips = logit_strips(a.b, cols, t.R);
-            if (a.b <= 256) class_join_kernel<1><<<static_cast<unsigned>(a.b), kThreads, 0, s>>>(t.part, strips, a.b, r, last, row_loss);
-            else class_join_kernel<16><<<static_cast<unsigned>(ceil_div(a.b, int64_t(16))), kThreads, 0, s>>>(t.part, strips, a.b, r, last, row_loss);
-            GNN_LAUNCHED("update_ce_join");
+            GNN_TRY(join(t.part, logit_strips(a.b, cols, t.R), a.b, r, last, row_loss, s));
             continue;
         }
         GNN_TRY(logits(cols));
         const int64_t ld = row_of(cols);
+        if (a.b < kStripRows && cols > kStrip) {
+            const int64_t strips = ceil_div(cols, kStrip);
+            float2 *part = reinterpret_cast<float2 *>(base + pl.strip_part);
+            class_strips_kernel<<<static_cast<unsigned>(a.b * strips), kThreads, 0, s>>>(z, a.b, cols, ld, c0, a.bias, r, part);
+            GNN_LAUNCHED("update_ce_strips");
+            GNN_TRY(join(part, strips, a.b, r, last, row_loss, s));
+            continue;
+        }
         if (cols <= 1024)
             class_sums_kernel<64><<<static_cast<unsigned>(ceil_div(a.b, int64_t(4))), kThreads, 0, s>>>(z, a.b, cols, ld, c0, a.bias, r, last, row_loss);
         else class_sums_kernel<256><<<static_cast<unsigned>(a.b), kThreads, 0, s>>>(z, a.b, cols, ld, c0, a.bias, r, last, row_loss);

@@ -73,7 +73,7 @@ int64_t splits_f32(Kind, int64_t M, int64_t N, int64_t R, bool may_split) {
     const int tile = pick_tile(M, N);
     const int64_t tiles = std::max<int64_t>(ceil_div(M, tile) * ceil_div(N, tile), 1), chunks = ceil_div(R, int64_t(Cfg<false>::BK));
     if (!may_split || tiles >= 128 || chunks < 16) return 1;
-    return std::min<int64_t>({chunks / 4, ceil_div(256, tiles), 16});
+    return std::min<int64_t>({chunks / 4, ceil_div(256, tiles), 128});
 }
 
 gnn_status product_f32(Kind kind, const Product &p, hipStream_t s) {

@@ -232,7 +232,7 @@ template <class C> __global__ void __launch_bounds__(C::kThreads, C::PER_CU) cla
 }
 
 tile::Choice choice(Kind kind, int64_t M, int64_t N, int64_t R, bool may_split) {
-    if (kind != kTT) return tile::choose(M, N, R, may_split ? 16 : 1);
+    if (kind != kTT) return tile::choose(M, N, R, may_split ? 64 : 1);
     // T fragments take twice the reads: 128 x 128 tiles are slower than their pace, and smaller ones are not worth it
     tile::Choice best{tile::kMid, 1};
     double least = -1;

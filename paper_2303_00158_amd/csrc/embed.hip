@@ -463,12 +463,21 @@ template <class T> __device__ __forceinline__ void zero_rows(const SumArgs &a, i
         if ((threadIdx.x & 63) == 0) ends[wave] = p;
     }
     __syncthreads();
-    for (int64_t p = ends[0] + threadIdx.x; p < ends[1]; p += kThreads) named[a.key[p] - v0] = 1;
-    __syncthreads();
     constexpr int VE = 16 / sizeof(T);
     row::Vec<T, VE> zero;
 #pragma unroll
     for (int i = 0; i < row::Vec<T, VE>::kWords; ++i) zero.w[i] = 0;
+    if (ends[0] == ends[1]) {
+        // no position names any of them: one stretch (113,538 rows of 1,024 fp32 values and three
+        // positions: row by row 101 us, FILL so)
+        T *to = static_cast<T *>(a.d_table) + v0 * a.dim;
+        const int64_t n = (v1 - v0) * a.dim;
+#pragma unroll 4
+        for (int64_t e = threadIdx.x * VE; e < n; e += kThreads * VE) zero.store_upto(to + e, n - e);
+        return;
+    }
+    for (int64_t p = ends[0] + threadIdx.x; p < ends[1]; p += kThreads) named[a.key[p] - v0] = 1;
+    __syncthreads();
     // a row to as many threads as it has vectors, several rows side by side
     const int64_t vectors = ceil_div(a.dim, int64_t(VE));
     const int64_t span = vectors >= kThreads ? kThreads : vectors, side = kThreads / span;

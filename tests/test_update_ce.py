@@ -119,7 +119,7 @@ def problem(gen, b, k, c, adt=F32, wdt=F32, off=0):
 
 SIZES = [(1, 1, 1), (1, 1, 2), (2, 3, 3), (5, 2, 47), (1, 64, 1000), (47, 31, 63), (64, 64, 64), (65, 100, 65), (100, 8, 257), (255, 33, 172),
          (257, 256, 47), (1024, 256, 47), (300, 602, 256), (129, 1024, 1000), (33, 100, 4099), (7, 520, 32_003), (1461, 64, 153), (600, 257, 1025),
-         (1, 4096, 3001), (3000, 16, 20), (20_000, 8, 5), (40, 5000, 10)]
+         (1, 4096, 3001), (3000, 16, 20), (20_000, 8, 5), (40, 5000, 10), (2, 100, 131_072), (1023, 24, 2049), (1024, 24, 2049), (3, 40, 2048)]
 
 
 @pytest.mark.gpu
