@@ -160,7 +160,8 @@ __global__ void __launch_bounds__(kThreads) class_sums_kernel(const float *z, in
 }
 
 // The sums of strips of a piece of logits, for few long rows: one workgroup a strip and row.
-constexpr int64_t kStrip = 2048, kStripRows = 1024;  // (2 rows of 131,072 classes with a workgroup a row: 617 us in all, STRIPFIG so)
+constexpr int64_t kStrip = 2048, kStripRows = 1024;  // (2 rows of 131,072 classes with a workgroup a row: 617 us in all, 156 so
+                                                     // and with dA's reduction split up to 128 ways)
 __global__ void __launch_bounds__(kThreads) class_strips_kernel(const float *z, int64_t b, int64_t cols, int64_t ld, int64_t c0, const float *bias,
                                                                 RowState r, float2 *part) {
     __shared__ float sh[2][kThreads / 64];
