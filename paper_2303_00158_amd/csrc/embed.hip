@@ -102,7 +102,7 @@ template <class F> void with_types(int idt, int odt, F &&go) {
 // Keys are ids; what names no row, and positions at or past the count, get the
 // key `rows` and come last.  A stable radix sort, least digit first.  Up to kSortTile
 // positions one workgroup does all of it in LDS (8,192 positions of 32,000 rows: 36 us in
-// four launches, 23 in this one).  More take two launches a digit: one counts each
+// four launches, 20 in this one).  More take two launches a digit: one counts each
 // tile's digits, the next moves the tile's pairs behind all smaller digits and behind
 // the same digit in earlier tiles, adding up the tiles' counts by itself.
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
@@ -134,24 +134,28 @@ template <int BITS> struct Digits {
     template <int KEYS>
     __device__ __forceinline__ static void rank(const uint32_t (&digit)[KEYS], const bool (&in)[KEYS], int rounds, WaveBins &bins,
                                                 uint32_t (&own)[KEYS]) {
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        const int wave = threadIdx.x >> 6;
         for (int i = threadIdx.x; i < kSortWaves * kBins; i += kSortThreads) (&bins[0][0])[i] = 0;
         __syncthreads();
         volatile uint32_t *mine = bins[wave];
 #pragma unroll
         for (int k = 0; k < KEYS; ++k) {
             if (k >= rounds) break;
-            uint64_t same = __ballot(in[k]);
+            // lanes whose digit has the same bits, in two halves: a bit costs the lane four instructions
+            const uint64_t there = __ballot(in[k]);
+            uint32_t lo = static_cast<uint32_t>(there), hi = static_cast<uint32_t>(there >> 32);
 #pragma unroll
             for (int b = 0; b < BITS; ++b) {
-                const uint64_t set = __ballot((digit[k] >> b) & 1);
-                same &= (digit[k] >> b) & 1 ? set : ~set;
+                const uint32_t bit = static_cast<uint32_t>(static_cast<int32_t>(digit[k] << (31 - b)) >> 31);  // all ones, or none
+                const uint64_t set = __ballot(bit != 0);
+                lo &= ~(static_cast<uint32_t>(set) ^ bit);
+                hi &= ~(static_cast<uint32_t>(set >> 32) ^ bit);
             }
-            const uint64_t below = same & ((1ull << lane) - 1);
+            const uint32_t below = __builtin_amdgcn_mbcnt_hi(hi, __builtin_amdgcn_mbcnt_lo(lo, 0));
             const uint32_t before = in[k] ? mine[digit[k]] : 0;
-            own[k] = before + __popcll(below);
+            own[k] = before + below;
             __builtin_amdgcn_wave_barrier();
-            if (in[k] && below == 0) mine[digit[k]] = before + __popcll(same);
+            if (in[k] && below == 0) mine[digit[k]] = before + __popc(lo) + __popc(hi);
             __builtin_amdgcn_wave_barrier();
         }
         __syncthreads();
@@ -181,11 +185,13 @@ template <int BITS> struct Digits {
         for (int e = 0; e < kEach; ++e) {
             const int d = threadIdx.x * kEach + e;
             if (d < kBins) {
-                uint32_t to = at + earlier[e];
+                uint32_t to = at + earlier[e], c[kSortWaves];
+#pragma unroll
+                for (int w = 0; w < kSortWaves; ++w) c[w] = bins[w][d];
+#pragma unroll
                 for (int w = 0; w < kSortWaves; ++w) {
-                    const uint32_t c = bins[w][d];
                     bins[w][d] = to;
-                    to += c;
+                    to += c[w];
                 }
             }
             at += total[e];
@@ -204,10 +210,9 @@ __device__ __forceinline__ int64_t sort_at(int64_t tile, int rounds, int k) {
     return tile * (kSortThreads * rounds) + (threadIdx.x >> 6) * (64 * rounds) + k * 64 + (threadIdx.x & 63);
 }
 
-constexpr int kOneBits = 9;
-__global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(SortArgs a) {
-    using D = Digits<kOneBits>;
-    __shared__ D::WaveBins bins;
+template <int BITS> __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(SortArgs a) {
+    using D = Digits<BITS>;
+    __shared__ typename D::WaveBins bins;
     __shared__ uint32_t keys[kSortTile], places[kSortTile], sh[kSortWaves];
     const int64_t n = row::live_rows(a.n_dev, a.cap);
     const int rounds = static_cast<int>(ceil_div(a.cap, int64_t(kSortThreads)));
@@ -226,6 +231,7 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(SortArgs a) {
         D::rank(digit, in, rounds, bins, own);
         uint32_t total[1] = {0}, none[1] = {0};
         if (threadIdx.x < D::kBins)
+#pragma unroll
             for (int w = 0; w < kSortWaves; ++w) total[0] += bins[w][threadIdx.x];
         D::place(bins, total, none, sh);
         const bool last = pass + 1 == a.passes;
@@ -365,39 +371,49 @@ int key_bits(int64_t rows) {
     return bits;
 }
 
+// go(tag of a digit's width, 5 to 11), at least `bits`
+template <class F> gnn_status with_bits(int64_t bits, F &&go) {
+    if (bits <= 5) return go(std::integral_constant<int, 5>{});
+    if (bits == 6) return go(std::integral_constant<int, 6>{});
+    if (bits == 7) return go(std::integral_constant<int, 7>{});
+    if (bits == 8) return go(std::integral_constant<int, 8>{});
+    if (bits == 9) return go(std::integral_constant<int, 9>{});
+    if (bits == 10) return go(std::integral_constant<int, 10>{});
+    return go(std::integral_constant<int, 11>{});
+}
+
 // Sorts; which of key and pos hold the result goes to *where.
 gnn_status sort_ids(SortArgs a, int *where, hipStream_t s) {
     const int bits = key_bits(a.rows);
     *where = 0;
     if (a.cap <= kSortTile) {
-        a.passes = static_cast<int>(ceil_div(bits, kOneBits));
-        embed_sort_kernel<<<1, kSortThreads, 0, s>>>(a);
-        GNN_LAUNCHED("embed_sort");
-        return GNN_OK;
+        // digits of up to 9 bits: the counts of wider ones would not fit beside the positions
+        a.passes = static_cast<int>(ceil_div(bits, 9));
+        return with_bits(ceil_div(bits, a.passes), [&](auto width) -> gnn_status {
+            constexpr int BITS = decltype(width)::value;
+            if constexpr (BITS <= 9) embed_sort_kernel<BITS><<<1, kSortThreads, 0, s>>>(a);
+            GNN_LAUNCHED("embed_sort");
+            return GNN_OK;
+        });
     }
     // digits of up to 11 bits, whose counts fill 128 KB of LDS: few launches first
     a.passes = static_cast<int>(ceil_div(bits, 11));
-    auto go = [&](auto width) -> gnn_status {
-        constexpr int BITS = decltype(width)::value;
-        for (int pass = 0; pass < a.passes; ++pass) {
-            embed_count_kernel<BITS><<<static_cast<unsigned>(a.tiles), kSortThreads, 0, s>>>(a, pass);
-            GNN_LAUNCHED("embed_count");
-            if (a.tiles > kDirectTiles) {
-                embed_scan_kernel<BITS><<<Digits<BITS>::kBins / 32, kSortThreads, 0, s>>>(a);
-                GNN_LAUNCHED("embed_scan");
-            }
-            embed_move_kernel<BITS><<<static_cast<unsigned>(a.tiles), kSortThreads, 0, s>>>(a, pass);
-            GNN_LAUNCHED("embed_move");
-        }
-        return GNN_OK;
-    };
     *where = a.passes & 1;
-    switch (ceil_div(bits, a.passes)) {
-        case 11: return go(std::integral_constant<int, 11>{});
-        case 10: return go(std::integral_constant<int, 10>{});
-        case 9: return go(std::integral_constant<int, 9>{});
-        default: return go(std::integral_constant<int, 8>{});
-    }
+    return with_bits(std::max<int64_t>(8, ceil_div(bits, a.passes)), [&](auto width) -> gnn_status {
+        constexpr int BITS = decltype(width)::value;
+        if constexpr (BITS >= 8)
+            for (int pass = 0; pass < a.passes; ++pass) {
+                embed_count_kernel<BITS><<<static_cast<unsigned>(a.tiles), kSortThreads, 0, s>>>(a, pass);
+                GNN_LAUNCHED("embed_count");
+                if (a.tiles > kDirectTiles) {
+                    embed_scan_kernel<BITS><<<Digits<BITS>::kBins / 32, kSortThreads, 0, s>>>(a);
+                    GNN_LAUNCHED("embed_scan");
+                }
+                embed_move_kernel<BITS><<<static_cast<unsigned>(a.tiles), kSortThreads, 0, s>>>(a, pass);
+                GNN_LAUNCHED("embed_move");
+            }
+        return GNN_OK;
+    });
 }
 
 // ---------------------------------------------------------------------------
