@@ -636,8 +636,9 @@ gnn_status gnn_distill_topk(const void *logits, gnn_dtype ldt, int64_t b, int64_
 
 /* The last layer and its loss in one call, for many classes: the softmax
  * cross-entropy of the logits Z = A Wt^T + b (equation 2 with the loss of Section
- * II-B) and its gradients, computed in pieces of the classes, so that neither the
- * logits nor their gradient exist as a whole:
+ * II-B) and its gradients, computed in pieces of the classes, so that memory does
+ * not go by b c: the workspace has room for some 2^27 values of dZ (or 256 classes)
+ * and, where that spares time, for up to 2^28 logits:
  *   lse_i = log sum_c exp(z_ic),  row_loss_i = lse_i - z_i[y_i],
  *   loss = sum_i s_i row_loss_i,  dZ = s (exp(z - lse) - onehot(y)),
  *   dwt = dZ^T A,  db = column sums of dZ,  d_a = dZ Wt.

@@ -787,7 +787,7 @@ def update_ce(a: torch.Tensor, wt: torch.Tensor, bias: Optional[torch.Tensor], l
               row_scale: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """gnn_update_ce: the softmax cross-entropy of the logits a wt^T + bias (a:
     b x k; wt: a row of k for each class) and those of its gradients that are
-    given, without the logits in memory.  row_scale: each row's factor in the
+    given, in pieces of the classes (memory does not go by b times them).  row_scale: each row's factor in the
     loss (1 / b when None; 0, or a label outside the classes, leaves a row
     out).  d_a may be a itself.  ws: workspace (allocated when None)."""
     b, k = _matrix("a", a)

@@ -100,6 +100,16 @@ def test_lookup(dim, tdt, odt):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("n, dim", [(131_071, 256), (131_073, 256), (70_001, 1024), (400_003, 12)])
+def test_lookup_on_both_sides_of_the_few_units_rule(n, dim):
+    gen = torch.Generator().manual_seed(dim)
+    table, ids = rand(gen, 999, dim), make_ids(gen, "zipf", n, 999)
+    out = torch.full((n, dim), 7.0, device=DEV)
+    gnn.embed_fwd(table, ids, out, 1.5)
+    assert torch.equal(out, lookup(table, ids, 1.5, F32))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dt", [F32, BF16])
 @pytest.mark.parametrize("dim, stride", [(7, 8), (16, 24), (100, 101), (256, 260), (1001, 1024)])
 def test_lookup_strided_and_misaligned(dim, stride, dt):

@@ -305,6 +305,40 @@ def test_the_same_bits_again_also_from_a_graph_on_another_stream(b, k, c, gemm):
         assert all(torch.equal(x, y) for x, y in zip(first, second)), n
 
 
+@pytest.mark.gpu
+def test_offsets_past_32_bits():
+    """2.2e9 weights: the first, the last and the rows around 2^31 values against 64 bits."""
+    b, k, c = 3, 2200, 1_000_003
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    wt = torch.empty((c, k), dtype=BF16, device=DEV)
+    for at in range(0, c, 100_000):
+        wt[at:at + 100_000] = torch.randn((min(100_000, c - at), k), generator=gen, device=DEV) / math.sqrt(k)
+    a = torch.randn((b, k), generator=gen, device=DEV).to(BF16)
+    labels = torch.tensor([0, c - 1, 976_128], device=DEV)  # row 976,128 has value 2^31
+    loss, row, dwt, db = torch.empty(1, device=DEV), torch.empty(b, device=DEV), torch.empty_like(wt), torch.empty(c, device=DEV)
+    d_a = torch.empty((b, k), device=DEV)
+    gnn.update_ce(a, wt, None, labels, loss, gnn.GNN_BF16, row_loss=row, d_a=d_a, dwt=dwt, db=db)
+    z = torch.cat([a.double() @ wt[at:at + 100_000].double().t() for at in range(0, c, 100_000)], 1)
+    lse = torch.logsumexp(z, 1)
+    want = lse - z.gather(1, labels[:, None])[:, 0]
+    # logits are off by (k + 4) U of their terms' sizes (about 28 for the normal ones here), the sum by its additions
+    off = (k + 4) * U * float((a.double().abs() @ wt[:1000].double().abs().t()).max()) * 1.5
+    assert ((row.double() - want).abs() <= 2 * off + (2 * math.ceil(c / 256) + 60) * U).all()
+    dz = torch.exp(z - lse[:, None])
+    dz[torch.arange(b, device=DEV), labels] -= 1
+    dz /= b
+    e = 2 * off + (2 * math.ceil(c / 256) + 100) * U
+    assert ((db.double() - dz.sum(0)).abs() <= e * dz.abs().sum(0) + 1e-30).all()
+    for at in (0, 1, 976_127, 976_128, 976_129, c - 2, c - 1):
+        w = dz[:, at] @ a.double()
+        assert ((dwt[at].double() - w).abs() <= (dz[:, at].abs() @ a.double().abs()) * (e + 2.0 ** -8 * 1.1) + w.abs() * 2.0 ** -8 * 1.1).all(), at
+    w, size = torch.zeros((b, k), dtype=torch.float64, device=DEV), torch.zeros((b, k), dtype=torch.float64, device=DEV)
+    for at in range(0, c, 100_000):
+        w += dz[:, at:at + 100_000] @ wt[at:at + 100_000].double()
+        size += dz[:, at:at + 100_000].abs() @ wt[at:at + 100_000].double().abs()
+    assert ((d_a.double() - w).abs() <= size * (e + 2.0 ** -8 * 1.1 + (c + 4) * U)).all()
+
+
 # --- refusals ---------------------------------------------------------------
 
 BUF = ctypes.create_string_buffer(1 << 16)
