@@ -256,7 +256,8 @@ template <bool EIGHT> __global__ void __launch_bounds__(kThreads) adamw_kernel(A
 
 }  // namespace
 
-gnn_status launch_adamw(const gnn_adamw_tensor *t, int64_t count, int sdt, double lr, double beta1, double beta2, double eps,
+gnn_status launch_adamw(const gnn_adamw_tensor *t, int64_t count, int sdt, double lr, double beta1, double beta2,
+                        double eps,
                         int64_t step, const float *lr_dev, const int64_t *step_dev, uint64_t seed, hipStream_t s) {
     Args a{};
     a.b1 = static_cast<float>(beta1);

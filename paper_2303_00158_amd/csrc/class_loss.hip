@@ -8,7 +8,8 @@
 // sums and once for dZ.  bf16 logits stay in the tiles' accumulators (class_loss_tile.hip); only
 // one piece of dZ exists at a time, so memory goes by b, not by b C.  Of long reductions up to
 // 2^28 logits (1 GB) are kept in fp32 from the first time, which spares them the
-// second (4,096 x 2,048 x 100,003, two thirds kept: 5,644 us without, 5,231 with).  fp32 keeps the logits of its one piece, or computes them twice.
+// second (4,096 x 2,048 x 100,003, two thirds kept: 5,644 us without, 5,231 with).  fp32 keeps the logits of its one
+// piece, or computes them twice.
 //
 // dZ is an operand of the products behind it, so bf16 rounds it, and it is rounded over the
 // largest row weight, which the products' ends multiply back: with a common weight
@@ -61,7 +62,8 @@ __global__ void __launch_bounds__(kThreads) class_rows_kernel(CeArgs a, RowState
 }
 
 // Four values from K of a row to a row of ld, zeros behind them.
-template <class TI, class TO> __device__ __forceinline__ void pack4(const TI *in, int64_t r, int64_t c, int64_t K, bool live, int64_t ld, TO *out) {
+template <class TI, class TO> __device__ __forceinline__ void pack4(const TI *in, int64_t r, int64_t c, int64_t K,
+                                                                    bool live, int64_t ld, TO *out) {
     row::Vec<TI, 4> v;
     v.load_upto(in + r * K + c, live ? K - c : 0);
     float x[4];
@@ -72,7 +74,8 @@ template <class TI, class TO> __device__ __forceinline__ void pack4(const TI *in
     o.store(out + r * ld + c);
 }
 template <class TI, class TO>
-__global__ void __launch_bounds__(kThreads) class_pack_kernel(const TI *in, int64_t rows, int64_t K, int64_t ld, TO *out) {
+__global__ void __launch_bounds__(kThreads) class_pack_kernel(const TI *in, int64_t rows, int64_t K, int64_t ld,
+                                                              TO *out) {
     const int64_t groups = ld / 4;
     for (int64_t t = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; t < rows * groups;
          t += static_cast<int64_t>(gridDim.x) * kThreads) {
@@ -125,7 +128,8 @@ __device__ __forceinline__ void join_row(const RowState &r, int64_t i, float top
 
 // From a piece of logits, T threads to a row.
 template <int T>
-__global__ void __launch_bounds__(kThreads) class_sums_kernel(const float *z, int64_t b, int64_t cols, int64_t ld, int64_t c0, const float *bias,
+__global__ void __launch_bounds__(kThreads) class_sums_kernel(const float *z, int64_t b, int64_t cols, int64_t ld,
+                                                              int64_t c0, const float *bias,
                                                               RowState r, bool last, float *row_loss) {
     constexpr int kRows = kThreads / T;
     __shared__ float sh[2][kThreads / 64];
@@ -159,10 +163,11 @@ __global__ void __launch_bounds__(kThreads) class_sums_kernel(const float *z, in
     join_row(r, i, top, sum, last, row_loss);
 }
 
-// The sums of strips of a piece of logits, for few long rows: one workgroup a strip and row.
-constexpr int64_t kStrip = 2048, kStripRows = 1024;  // (2 rows of 131,072 classes with a workgroup a row: 617 us in all, 156 so
-                                                     // and with dA's reduction split up to 128 ways)
-__global__ void __launch_bounds__(kThreads) class_strips_kernel(const float *z, int64_t b, int64_t cols, int64_t ld, int64_t c0, const float *bias,
+// The sums of strips of a piece of logits, for few long rows: one workgroup a strip and row (2 rows of
+// 131,072 classes with a workgroup a row: 617 us in all, 156 so and with dA's reduction split up to 128 ways).
+constexpr int64_t kStrip = 2048, kStripRows = 1024;
+__global__ void __launch_bounds__(kThreads) class_strips_kernel(const float *z, int64_t b, int64_t cols, int64_t ld,
+                                                                int64_t c0, const float *bias,
                                                                 RowState r, float2 *part) {
     __shared__ float sh[2][kThreads / 64];
     const int64_t i = blockIdx.x % b, strip = blockIdx.x / b, beg = strip * kStrip;
@@ -199,7 +204,8 @@ __global__ void __launch_bounds__(kThreads) class_strips_kernel(const float *z, 
 // From the tiles' strips: ROWS rows of a workgroup, each strip of a row to one of the threads that
 // share it; these meet in a fixed order.  (One row of 1,000 strips takes 16 threads 20 us, 256 of them 6.)
 template <int ROWS>
-__global__ void __launch_bounds__(kThreads) class_join_kernel(const float2 *part, int64_t strips, int64_t b, RowState r, bool last, float *row_loss) {
+__global__ void __launch_bounds__(kThreads) class_join_kernel(const float2 *part, int64_t strips, int64_t b,
+                                                              RowState r, bool last, float *row_loss) {
     constexpr int kLanes = kThreads / ROWS;
     __shared__ float2 sh[kLanes][ROWS + 1];
     const int x = threadIdx.x % ROWS, y = threadIdx.x / ROWS;
@@ -224,9 +230,11 @@ __global__ void __launch_bounds__(kThreads) class_join_kernel(const float2 *part
     if (y == 0 && i < b) join_row(r, i, top, sum, last, row_loss);
 }
 
-gnn_status join(const float2 *part, int64_t strips, int64_t b, const RowState &r, bool last, float *row_loss, hipStream_t s) {
+gnn_status join(const float2 *part, int64_t strips, int64_t b, const RowState &r, bool last, float *row_loss,
+                hipStream_t s) {
     if (b <= 256) class_join_kernel<1><<<static_cast<unsigned>(b), kThreads, 0, s>>>(part, strips, b, r, last, row_loss);
-    else class_join_kernel<16><<<static_cast<unsigned>(ceil_div(b, int64_t(16))), kThreads, 0, s>>>(part, strips, b, r, last, row_loss);
+    else class_join_kernel<16><<<static_cast<unsigned>(ceil_div(b, int64_t(16))), kThreads, 0, s>>>(part, strips, b,
+            r, last, row_loss);
     GNN_LAUNCHED("update_ce_join");
     return GNN_OK;
 }
@@ -270,7 +278,8 @@ __global__ void __launch_bounds__(1024) class_total_kernel(Total t) { t.run<1024
 // dZ of a piece in place of its logits, zeros in the columns up to ld, and the column sums
 // of a part of the rows.
 constexpr int kStripe = 256;  // columns of a workgroup: 64 threads of 4, times 4 rows
-__global__ void __launch_bounds__(kThreads) class_dz_kernel(float *z, int64_t ld, int64_t b, int64_t cols, int64_t c0, const float *bias, RowState r,
+__global__ void __launch_bounds__(kThreads) class_dz_kernel(float *z, int64_t ld, int64_t b, int64_t cols,
+                                                            int64_t c0, const float *bias, RowState r,
                                                             float *part, int64_t parts, Total total) {
     __shared__ float sh[4][kStripe];
     if (blockIdx.x >= ceil_div(ld, int64_t(kStripe)) * parts) {
@@ -319,8 +328,10 @@ __global__ void __launch_bounds__(kThreads) class_dz_kernel(float *z, int64_t ld
 
 // The same over the largest weight from logits that were kept, in bf16 and with their biases in them: 32
 // threads of eight columns, times 8 rows.
-__global__ void __launch_bounds__(kThreads) class_dz_kept_kernel(const float *z, int64_t ldz, uint16_t *dz, int64_t ld, int64_t b, int64_t cols,
-                                                                 int64_t c0, RowState r, const float *scale, float *part, int64_t parts) {
+__global__ void __launch_bounds__(kThreads) class_dz_kept_kernel(const float *z, int64_t ldz, uint16_t *dz,
+                                                                 int64_t ld, int64_t b, int64_t cols,
+                                                                 int64_t c0, RowState r, const float *scale,
+                                                                     float *part, int64_t parts) {
     __shared__ float sh[8][kStripe];
     const int64_t stripes = ceil_div(ld, int64_t(kStripe)), stripe = blockIdx.x % stripes, p = blockIdx.x / stripes;
     const int64_t per = ceil_div(b, parts), beg = min(b, p * per), end = min(b, beg + per);
@@ -387,7 +398,7 @@ struct Reduce {
     }
 };
 Reduce reduce_of(const float *part, int64_t nsplit, int64_t rows, int64_t cols, int64_t ld, void *out, int odt) {
-    return Reduce{part, nsplit, rows, cols, ld, out, odt == GNN_BF16, std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows * (ld / 4), int64_t(kThreads)), 16384))};
+    return Reduce{part, nsplit, rows, cols, ld, out, odt == GNN_BF16, grid_of(rows * (ld / 4))};
 }
 struct ReduceDb {
     const float *part;
@@ -459,7 +470,8 @@ struct Plan {
     Plan(int64_t b, int64_t k, int64_t classes, int gemm_dt, bool grads) : c(classes) {
         bf = gemm_dt == GNN_BF16;
         ldk = row_of(k);
-        piece = std::min(row_of(c), std::max<int64_t>(kPiece / std::max<int64_t>(b, 1) / kPieceCols * kPieceCols, kPieceCols));
+        piece = std::min(row_of(c), std::max<int64_t>(kPiece / std::max<int64_t>(b, 1) / kPieceCols * kPieceCols,
+                                                      kPieceCols));
         pieces = ceil_div(c, piece);
         sums_piece = std::min(row_of(c), bf ? kSumsPieces * piece : piece);
         kept = 0;
@@ -488,16 +500,19 @@ struct Plan {
         int64_t strips = 0;
         if (bf && b > 0)
             for (const bool copy : {false, true})
-                for (int64_t c0 = 0; c0 < c; c0 += segment(c0, copy)) strips = std::max(strips, logit_strips(b, segment(c0, copy), ldk));
+                for (int64_t c0 = 0; c0 < c; c0 += segment(c0, copy))
+                    strips = std::max(strips, logit_strips(b, segment(c0, copy), ldk));
         zk = cv.take(static_cast<size_t>(b * kept) * 4);
-        z = cv.take(std::max(static_cast<size_t>(b * strips) * 8, bf && !grads ? size_t(0) : static_cast<size_t>(b * piece) * es));
+        const size_t dz = bf && !grads ? 0 : static_cast<size_t>(b * piece) * es;
+        z = cv.take(std::max(static_cast<size_t>(b * strips) * 8, dz));
         strip_part = cv.take(!bf && b < kStripRows ? static_cast<size_t>(b * ceil_div(piece, kStrip)) * 8 : 0);
         db = dw_part = da_part = 0;
         da_splits = dw_splits[0] = dw_splits[1] = parts[0] = parts[1] = kept_parts = 1;
         if (grads) {
             const int64_t width[2] = {piece, last};
             auto row_parts = [&](int64_t n, int64_t rows_each) {
-                return std::max<int64_t>(1, std::min<int64_t>(ceil_div(2048, ceil_div(n, int64_t(kStripe))), ceil_div(b, rows_each)));
+                return std::max<int64_t>(1, std::min<int64_t>(ceil_div(2048, ceil_div(n, int64_t(kStripe))),
+                                                              ceil_div(b, rows_each)));
             };
             kept_parts = row_parts(piece, 32);
             int64_t most = kept > 0 ? kept_parts * piece : 0, dw = 0;
@@ -518,7 +533,9 @@ struct Plan {
 
 }  // namespace
 
-size_t update_ce_ws_bytes(int64_t b, int64_t k, int64_t c, int gemm_dt, bool grads) { return Plan(b, k, c, gemm_dt, grads).total; }
+size_t update_ce_ws_bytes(int64_t b, int64_t k, int64_t c, int gemm_dt, bool grads) {
+    return Plan(b, k, c, gemm_dt, grads).total;
+}
 
 gnn_status launch_update_ce(const CeArgs &a, void *ws, hipStream_t s) {
     const bool grads = a.d_a || a.dwt || a.db;
@@ -527,7 +544,8 @@ gnn_status launch_update_ce(const CeArgs &a, void *ws, hipStream_t s) {
     const int gdt = a.gemm_dt;
     const size_t es = dtype_size(gdt);
     auto f = [&](size_t at) { return reinterpret_cast<float *>(base + at); };
-    const RowState r{reinterpret_cast<int32_t *>(base + pl.label), f(pl.weight), f(pl.top), f(pl.sum), f(pl.z_label), f(pl.lse)};
+    const RowState r{reinterpret_cast<int32_t *>(base + pl.label), f(pl.weight), f(pl.top), f(pl.sum), f(pl.z_label),
+                     f(pl.lse)};
     float *row_loss = a.row_loss ? a.row_loss : f(pl.row_loss), *scale = f(pl.scale), *z = f(pl.z);
     const bool any = a.b > 0;
     // A as the products read it
@@ -536,7 +554,8 @@ gnn_status launch_update_ce(const CeArgs &a, void *ws, hipStream_t s) {
     const bool rows16 = a.k * static_cast<int64_t>(es) % 16 == 0;
     if (any && (a.dwt || a.adt != gdt || !rows16 || !aligned(a.a, 16))) {
         with_pack_types(a.adt, gdt, [&](auto ti, auto to) {
-            class_pack_rows_kernel<decltype(ti)><<<grid_of(a.b * (pl.ldk / 4)), kThreads, 0, s>>>(a, r, pl.ldk, reinterpret_cast<decltype(to) *>(base + pl.a));
+            class_pack_rows_kernel<decltype(ti)><<<grid_of(a.b * (pl.ldk / 4)), kThreads, 0, s>>>(a, r, pl.ldk,
+                    reinterpret_cast<decltype(to) *>(base + pl.a));
         });
         GNN_LAUNCHED("update_ce_pack");
         A = base + pl.a;
@@ -554,7 +573,8 @@ gnn_status launch_update_ce(const CeArgs &a, void *ws, hipStream_t s) {
         ldw = a.k;
         if (!copy_w) return GNN_OK;
         with_pack_types(a.wdt, gdt, [&](auto ti, auto to) {
-            class_pack_kernel<<<grid_of(cols * (pl.ldk / 4)), kThreads, 0, s>>>(static_cast<const decltype(ti) *>(w), cols, a.k, pl.ldk,
+            class_pack_kernel<<<grid_of(cols * (pl.ldk / 4)), kThreads, 0, s>>>(static_cast<const decltype(ti) *>(w),
+                                                                                cols, a.k, pl.ldk,
                                                                                 reinterpret_cast<decltype(to) *>(base + pl.w));
         });
         GNN_LAUNCHED("update_ce_pack");
@@ -564,11 +584,13 @@ gnn_status launch_update_ce(const CeArgs &a, void *ws, hipStream_t s) {
     };
     auto logits = [&](int64_t cols) {
         const int64_t K = std::min(lda, ldw);
-        return product_f32(kNN, Product{A, w, lda, ldw, a.b, cols, K, K, z, GNN_F32, row_of(cols), 1, 0, false, nullptr}, s);
+        return product_f32(kNN, Product{A, w, lda, ldw, a.b, cols, K, K, z, GNN_F32, row_of(cols), 1, 0, false,
+                                        nullptr}, s);
     };
     auto tile_args = [&](int64_t c0, int64_t cols) {
-        return LogitArgs{static_cast<const uint16_t *>(A), static_cast<const uint16_t *>(w), lda, ldw, a.b, cols, std::min(lda, ldw), c0,
-                         a.bias ? a.bias + c0 : nullptr, r, reinterpret_cast<float2 *>(z), c0 < pl.kept ? f(pl.zk) + c0 : nullptr, pl.kept,
+        return LogitArgs{static_cast<const uint16_t *>(A), static_cast<const uint16_t *>(w), lda, ldw, a.b, cols,
+                         std::min(lda, ldw), c0, a.bias ? a.bias + c0 : nullptr, r, reinterpret_cast<float2 *>(z),
+                         c0 < pl.kept ? f(pl.zk) + c0 : nullptr, pl.kept,
                          reinterpret_cast<uint16_t *>(z), row_of(cols), scale,
                          a.db ? f(pl.db) : nullptr};
     };
@@ -588,14 +610,17 @@ gnn_status launch_update_ce(const CeArgs &a, void *ws, hipStream_t s) {
         if (a.b < kStripRows && cols > kStrip) {
             const int64_t strips = ceil_div(cols, kStrip);
             float2 *part = reinterpret_cast<float2 *>(base + pl.strip_part);
-            class_strips_kernel<<<static_cast<unsigned>(a.b * strips), kThreads, 0, s>>>(z, a.b, cols, ld, c0, a.bias, r, part);
+            class_strips_kernel<<<static_cast<unsigned>(a.b * strips), kThreads, 0, s>>>(z, a.b, cols, ld, c0,
+                    a.bias, r, part);
             GNN_LAUNCHED("update_ce_strips");
             GNN_TRY(join(part, strips, a.b, r, last, row_loss, s));
             continue;
         }
         if (cols <= 1024)
-            class_sums_kernel<64><<<static_cast<unsigned>(ceil_div(a.b, int64_t(4))), kThreads, 0, s>>>(z, a.b, cols, ld, c0, a.bias, r, last, row_loss);
-        else class_sums_kernel<256><<<static_cast<unsigned>(a.b), kThreads, 0, s>>>(z, a.b, cols, ld, c0, a.bias, r, last, row_loss);
+            class_sums_kernel<64><<<static_cast<unsigned>(ceil_div(a.b, int64_t(4))), kThreads, 0, s>>>(z, a.b, cols,
+                    ld, c0, a.bias, r, last, row_loss);
+        else class_sums_kernel<256><<<static_cast<unsigned>(a.b), kThreads, 0, s>>>(z, a.b, cols, ld, c0, a.bias, r,
+                                                                                    last, row_loss);
         GNN_LAUNCHED("update_ce_sums");
     }
     // their total: beside dZ where there is one in fp32 and the rows are few
@@ -617,14 +642,16 @@ gnn_status launch_update_ce(const CeArgs &a, void *ws, hipStream_t s) {
         if (any && c0 < pl.kept) {
             parts = pl.kept_parts;
             class_dz_kept_kernel<<<static_cast<unsigned>(ceil_div(ld, int64_t(kStripe)) * parts), kThreads, 0, s>>>(
-                f(pl.zk) + c0, pl.kept, reinterpret_cast<uint16_t *>(z), ld, a.b, cols, c0, r, scale, a.db ? f(pl.db) : nullptr, parts);
+                f(pl.zk) + c0, pl.kept, reinterpret_cast<uint16_t *>(z), ld, a.b, cols, c0, r, scale,
+                a.db ? f(pl.db) : nullptr, parts);
             GNN_LAUNCHED("update_ce_dz");
         } else if (any && pl.bf) {
             GNN_TRY(logit_dz(tile_args(c0, cols), s));
         } else if (any) {
             if (again) GNN_TRY(logits(cols));
             const int64_t blocks = ceil_div(ld, int64_t(kStripe)) * parts + (owed ? 1 : 0);
-            class_dz_kernel<<<static_cast<unsigned>(blocks), kThreads, 0, s>>>(z, ld, a.b, cols, c0, a.bias, r, a.db ? f(pl.db) : nullptr, parts, total);
+            class_dz_kernel<<<static_cast<unsigned>(blocks), kThreads, 0, s>>>(z, ld, a.b, cols, c0, a.bias, r,
+                                                                               a.db ? f(pl.db) : nullptr, parts, total);
             GNN_LAUNCHED("update_ce_dz");
             owed = false;
         }

@@ -25,7 +25,9 @@ template <int TILE> struct Source<TILE, true> {
 };
 
 // Workgroup blk of a product's.
-template <int TILE, bool TX, bool TY> __device__ __forceinline__ void run_product(const Product &p, const TileMap &map, int64_t blk, char *lds) {
+template <int TILE, bool TX, bool TY> __device__ __forceinline__ void run_product(const Product &p,
+                                                                                  const TileMap &map, int64_t blk,
+                                                                                          char *lds) {
     constexpr int D = depth<TILE>();
     const int64_t split = blk / map.blocks();
     int64_t tx, ty;
@@ -55,13 +57,15 @@ template <int TILE, bool TX, bool TY> __device__ __forceinline__ void run_produc
     });
 }
 
-template <int TILE, bool TX, bool TY> __global__ void __launch_bounds__(gemm::kThreads) class_engine_kernel(Product p, TileMap map) {
+template <int TILE, bool TX,
+    bool TY> __global__ void __launch_bounds__(gemm::kThreads) class_engine_kernel(Product p, TileMap map) {
     __shared__ __attribute__((aligned(16))) char lds[lds_bytes<TILE, TILE>()];
     run_product<TILE, TX, TY>(p, map, blockIdx.x, lds);
 }
 
 // dWt and dA of a piece side by side: of small models both are a launch's latency.
-__global__ void __launch_bounds__(gemm::kThreads) class_engine_pair_kernel(Product tt, TileMap mt, int64_t tts, Product nt, TileMap mn) {
+__global__ void __launch_bounds__(gemm::kThreads) class_engine_pair_kernel(Product tt, TileMap mt, int64_t tts,
+                                                                           Product nt, TileMap mn) {
     __shared__ __attribute__((aligned(16))) char lds[lds_bytes<64, 64>()];
     if (blockIdx.x < tts) run_product<64, true, true>(tt, mt, blockIdx.x, lds);
     else run_product<64, false, true>(nt, mn, blockIdx.x - tts, lds);
@@ -71,7 +75,8 @@ __global__ void __launch_bounds__(gemm::kThreads) class_engine_pair_kernel(Produ
 
 int64_t splits_f32(Kind, int64_t M, int64_t N, int64_t R, bool may_split) {
     const int tile = pick_tile(M, N);
-    const int64_t tiles = std::max<int64_t>(ceil_div(M, tile) * ceil_div(N, tile), 1), chunks = ceil_div(R, int64_t(Cfg<false>::BK));
+    const int64_t tiles = std::max<int64_t>(ceil_div(M, tile) * ceil_div(N, tile), 1), chunks = ceil_div(R,
+            int64_t(Cfg<false>::BK));
     if (!may_split || tiles >= 128 || chunks < 16) return 1;
     return std::min<int64_t>({chunks / 4, ceil_div(256, tiles), 128});
 }
@@ -95,7 +100,8 @@ gnn_status product_f32(Kind kind, const Product &p, hipStream_t s) {
 }
 
 gnn_status products_f32(const Product &tt, const Product &nt, hipStream_t s) {
-    const TileMap mt{ceil_div(tt.M, int64_t(64)), ceil_div(tt.N, int64_t(64))}, mn{ceil_div(nt.M, int64_t(64)), ceil_div(nt.N, int64_t(64))};
+    const TileMap mt{ceil_div(tt.M, int64_t(64)), ceil_div(tt.N, int64_t(64))}, mn{ceil_div(nt.M, int64_t(64)),
+                                                                                   ceil_div(nt.N, int64_t(64))};
     const int64_t a = mt.blocks() * tt.nsplit, b = mn.blocks() * nt.nsplit;
     // products of many tiles fill the chip one after the other
     if (pick_tile(tt.M, tt.N) != 64 || pick_tile(nt.M, nt.N) != 64 || a + b > 2048) {

@@ -24,7 +24,8 @@ __device__ __forceinline__ void eight_of(const tile::f32x4 &lo, const tile::f32x
 
 // A wavefront's part of an output tile times `factor`, from (row0, col0).
 template <class C, class T>
-__device__ __forceinline__ void put_tile(const tile::Acc<C> &acc, const Product &p, T *out, float factor, int64_t row0, int64_t col0) {
+__device__ __forceinline__ void put_tile(const tile::Acc<C> &acc, const Product &p, T *out, float factor,
+                                         int64_t row0, int64_t col0) {
     const int lane = threadIdx.x & 63, g = lane >> 4;
     const int64_t r0 = row0 + (lane & 15), c0 = col0 + (g & 1) * 16 + (g >> 1) * 8;
 #pragma unroll
@@ -64,7 +65,8 @@ __global__ void __launch_bounds__(C::kThreads, C::PER_CU) class_product_kernel(P
     const uint16_t *x = static_cast<const uint16_t *>(p.x), *y = static_cast<const uint16_t *>(p.y);
     const tile::Operand ox = TX ? tile::Operand{x + beg * p.ldx + row0, nullptr, p.ldx, 0, p.ldx - row0, red}
                                 : tile::Operand{x + row0 * p.ldx + beg, nullptr, p.ldx, 0, p.M - row0, red};
-    const tile::Operand oy = TY ? tile::Operand{y + beg * p.ldy + col0, nullptr, p.ldy, 0, p.ldy - col0, min(end, p.Ry) - beg}
+    const tile::Operand oy = TY ? tile::Operand{y + beg * p.ldy + col0, nullptr, p.ldy, 0, p.ldy - col0, min(end,
+            p.Ry) - beg}
                                 : tile::Operand{y + col0 * p.ldy + beg, nullptr, p.ldy, 0, p.N - col0, red};
     tile::Acc<C> acc;
     acc.clear();
@@ -92,7 +94,8 @@ template <class C> struct LogitTile {
         const tile::Operand ox{a.x + row0 * a.ldx, nullptr, a.ldx, 0, a.M - row0, a.R};
         const tile::Operand oy{a.y + col0 * a.ldy, nullptr, a.ldy, 0, a.N - col0, a.R};
         acc.clear();
-        tile::Product<C, false, false>(ox, oy).template run<true>(acc, ring, static_cast<int>(ceil_div(a.R, int64_t(tile::kBK))));
+        tile::Product<C, false, false>(ox, oy).template run<true>(acc, ring, static_cast<int>(ceil_div(a.R,
+                int64_t(tile::kBK))));
         const int wave = threadIdx.x >> 6;
         row_strip = 2 * m + (wave >> 1);
         col_strip = 2 * n + (wave & 1);
@@ -117,7 +120,8 @@ template <class C> struct LogitTile {
 
 // Largest logit of each row among a wavefront's columns, and the sum of exp(z - largest):
 // each lane's own first (of 4 NI columns), then those of the four lanes that share the row.
-template <class C, bool KEEP> __global__ void __launch_bounds__(C::kThreads, C::PER_CU) class_sums_tile_kernel(LogitArgs a) {
+template <class C, bool KEEP> __global__ void __launch_bounds__(C::kThreads,
+                                                                C::PER_CU) class_sums_tile_kernel(LogitArgs a) {
     __shared__ __attribute__((aligned(16))) uint16_t st0[C::kStageElems], st1[C::kStageElems];
     tile::Acc<C> acc;
     LogitTile<C> at;
@@ -227,7 +231,8 @@ template <class C> __global__ void __launch_bounds__(C::kThreads, C::PER_CU) cla
             for (int o = 8; o > 0; o >>= 1) sum[j][q] += __shfl_xor(sum[j][q], o, 64);
         const int64_t c = at.col0 + 16 * j + 4 * g;
         if ((lane & 15) == 0 && c < a.ld)
-            *reinterpret_cast<float4 *>(a.db_part + at.row_strip * a.ld + c) = make_float4(sum[j][0], sum[j][1], sum[j][2], sum[j][3]);
+            *reinterpret_cast<float4 *>(a.db_part + at.row_strip * a.ld + c) = make_float4(sum[j][0], sum[j][1],
+                    sum[j][2], sum[j][3]);
     }
 }
 
@@ -241,7 +246,8 @@ tile::Choice choice(Kind kind, int64_t M, int64_t N, int64_t R, bool may_split) 
         using C = decltype(cfg);
         const int64_t t = ceil_div(M, int64_t(C::BM)) * ceil_div(N, int64_t(C::BN));
         for (int64_t n = 1; n == 1 || (may_split && n <= 64 && n * t <= 256 * C::PER_CU && n * 4 <= chunks); n *= 2) {
-            const double us = tile::cost<C>(t, chunks, n, pace) + (n > 1 ? 4 + static_cast<double>(n) * M * N * 8 / 8e6 : 0);
+            const double us = tile::cost<C>(t, chunks, n, pace) + (n > 1
+                                                                   ? 4 + static_cast<double>(n) * M * N * 8 / 8e6 : 0);
             if (least < 0 || us < least) {
                 least = us;
                 best = tile::Choice{pick, n};
@@ -257,7 +263,8 @@ template <class C, bool TX, bool TY> gnn_status launch(const Product &p, hipStre
     const int64_t tiles = ceil_div(p.M, int64_t(C::BM)) * ceil_div(p.N, int64_t(C::BN));
     const int64_t grid = static_cast<int64_t>(round_up(tiles * p.nsplit, wide::kXcds));
     GNN_CHECK(grid <= kMaxGrid / C::kThreads, GNN_ESIZE, "update_ce: sizes exceed the grid limit");
-    if (p.odt == GNN_BF16) class_product_kernel<C, TX, TY, uint16_t><<<static_cast<unsigned>(grid), C::kThreads, 0, s>>>(p);
+    if (p.odt == GNN_BF16) class_product_kernel<C, TX, TY, uint16_t><<<static_cast<unsigned>(grid), C::kThreads, 0,
+        s>>>(p);
     else class_product_kernel<C, TX, TY, float><<<static_cast<unsigned>(grid), C::kThreads, 0, s>>>(p);
     GNN_LAUNCHED("update_ce_product");
     return GNN_OK;
@@ -265,11 +272,13 @@ template <class C, bool TX, bool TY> gnn_status launch(const Product &p, hipStre
 
 }  // namespace
 
-int64_t splits_bf16(Kind kind, int64_t M, int64_t N, int64_t R, bool may_split) { return choice(kind, M, N, R, may_split).nsplit; }
+int64_t splits_bf16(Kind kind, int64_t M, int64_t N, int64_t R, bool may_split) { return choice(kind, M, N, R,
+        may_split).nsplit; }
 
 gnn_status product_bf16(Kind kind, const Product &p, hipStream_t s) {
     const tile::Pick pick = choice(kind, p.M, p.N, p.R, p.nsplit > 1).pick;
-    if (kind == kTT) return pick == tile::kBig ? launch<tile::Big, true, true>(p, s) : launch<tile::Mid, true, true>(p, s);
+    if (kind == kTT) return pick == tile::kBig ? launch<tile::Big, true, true>(p, s) : launch<tile::Mid, true,
+        true>(p, s);
     auto go = [&](auto ty) -> gnn_status {
         constexpr bool TY = decltype(ty)::value;
         switch (pick) {
@@ -306,7 +315,8 @@ int64_t logit_row_strips(int64_t M, int64_t N, int64_t R) {
 gnn_status logit_sums(const LogitArgs &a, hipStream_t s) {
     return with_logit_tile(a.M, a.N, a.R, [&](auto c) -> gnn_status {
         using C = decltype(c);
-        const int64_t grid = static_cast<int64_t>(round_up(ceil_div(a.M, int64_t(C::BM)) * ceil_div(a.N, int64_t(C::BN)), wide::kXcds));
+        const int64_t grid = static_cast<int64_t>(round_up(ceil_div(a.M, int64_t(C::BM)) * ceil_div(a.N,
+                int64_t(C::BN)), wide::kXcds));
         GNN_CHECK(grid <= kMaxGrid / C::kThreads, GNN_ESIZE, "update_ce: sizes exceed the grid limit");
         if (a.keep) class_sums_tile_kernel<C, true><<<static_cast<unsigned>(grid), C::kThreads, 0, s>>>(a);
         else class_sums_tile_kernel<C, false><<<static_cast<unsigned>(grid), C::kThreads, 0, s>>>(a);
@@ -318,7 +328,8 @@ gnn_status logit_sums(const LogitArgs &a, hipStream_t s) {
 gnn_status logit_dz(const LogitArgs &a, hipStream_t s) {
     return with_logit_tile(a.M, a.N, a.R, [&](auto c) -> gnn_status {
         using C = decltype(c);
-        const int64_t grid = static_cast<int64_t>(round_up(ceil_div(a.M, int64_t(C::BM)) * ceil_div(a.N, int64_t(C::BN)), wide::kXcds));
+        const int64_t grid = static_cast<int64_t>(round_up(ceil_div(a.M, int64_t(C::BM)) * ceil_div(a.N,
+                int64_t(C::BN)), wide::kXcds));
         GNN_CHECK(grid <= kMaxGrid / C::kThreads, GNN_ESIZE, "update_ce: sizes exceed the grid limit");
         class_dz_tile_kernel<C><<<static_cast<unsigned>(grid), C::kThreads, 0, s>>>(a);
         GNN_LAUNCHED("update_ce_dz");

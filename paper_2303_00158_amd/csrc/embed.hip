@@ -41,12 +41,14 @@ struct LookupArgs {
 // the wavefronts wait for memory (26,624 rows of 256 fp32 values 11.3 us with two, 12.6 with
 // four, 14.7 with eight; 131,072 of 4,096 bf16 310, 302 and 316).
 constexpr int64_t kFewUnits = 1 << 17;
-template <class TI, class TO, int VE, int LANES, int UNITS> __global__ void __launch_bounds__(kThreads) embed_fwd_kernel(LookupArgs a) {
+template <class TI, class TO, int VE, int LANES,
+    int UNITS> __global__ void __launch_bounds__(kThreads) embed_fwd_kernel(LookupArgs a) {
     constexpr int kRows = 64 / LANES;
     const int64_t n = row::live_rows(a.n_dev, a.cap);
     const int lane = threadIdx.x & (LANES - 1), slot = (threadIdx.x & 63) / LANES;
     const int64_t units = ceil_div(n, int64_t(kRows)) * a.passes;
-    const int64_t waves = static_cast<int64_t>(gridDim.x) * kWaves, wave = static_cast<int64_t>(blockIdx.x) * kWaves + (threadIdx.x >> 6);
+    const int64_t waves = static_cast<int64_t>(gridDim.x) * kWaves,
+        wave = static_cast<int64_t>(blockIdx.x) * kWaves + (threadIdx.x >> 6);
     const TI *table = static_cast<const TI *>(a.table);
     TO *out = static_cast<TO *>(a.out);
     for (int64_t u0 = wave * UNITS; u0 < units; u0 += waves * UNITS) {
@@ -134,7 +136,8 @@ template <int BITS> struct Digits {
     // own[k] = how many of the wavefront's earlier elements (of smaller k, or in a lower lane)
     // have the digit of its element k; bins[wave] = the wavefront's counts.
     template <int KEYS>
-    __device__ __forceinline__ static void rank(const uint32_t (&digit)[KEYS], const bool (&in)[KEYS], int rounds, WaveBins &bins,
+    __device__ __forceinline__ static void rank(const uint32_t (&digit)[KEYS], const bool (&in)[KEYS], int rounds,
+                                                WaveBins &bins,
                                                 uint32_t (&own)[KEYS]) {
         const int wave = threadIdx.x >> 6;
         for (int i = threadIdx.x; i < kSortWaves * kBins; i += kSortThreads) (&bins[0][0])[i] = 0;
@@ -167,7 +170,8 @@ template <int BITS> struct Digits {
     // smaller digits take `total` places of theirs and digit d starts `earlier` places on.
     // total and earlier: of the digits that threads 0 .. kSortThreads hold, kEach each.
     static constexpr int kEach = kBins > kSortThreads ? kBins / kSortThreads : 1;
-    __device__ __forceinline__ static void place(WaveBins &bins, const uint32_t (&total)[kEach], const uint32_t (&earlier)[kEach],
+    __device__ __forceinline__ static void place(WaveBins &bins, const uint32_t (&total)[kEach],
+                                                 const uint32_t (&earlier)[kEach],
                                                  uint32_t *sh) {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
         uint32_t mine = 0;
@@ -435,7 +439,8 @@ struct SumArgs {
     int64_t zero_rows;          // table rows of one of those
 };
 
-template <class T, int VE> __device__ __forceinline__ void put_row(const SumArgs &a, uint32_t row, int64_t c, float (&sum)[VE]) {
+template <class T, int VE> __device__ __forceinline__ void put_row(const SumArgs &a, uint32_t row, int64_t c,
+                                                                   float (&sum)[VE]) {
     T *to = static_cast<T *>(a.d_table) + static_cast<int64_t>(row) * a.dim + c;
     const int64_t room = a.dim - c;
     float y[VE];
@@ -599,7 +604,8 @@ __device__ __forceinline__ bool group_spanned(const SumArgs &a, int64_t u, uint3
     *run = a.key[beg];
     return *run < static_cast<uint32_t>(a.rows) && a.key[beg - 1] == *run && a.key[end - 1] == *run;
 }
-template <int VE> __device__ __forceinline__ void add_parts(const SumArgs &a, int64_t c, int64_t from, int64_t to, int64_t step, float (&sum)[VE]) {
+template <int VE> __device__ __forceinline__ void add_parts(const SumArgs &a, int64_t c, int64_t from, int64_t to,
+                                                            int64_t step, float (&sum)[VE]) {
 #pragma unroll 8
     for (int64_t u = from; u < to; u += step) {
         row::Vec<float, VE> x;
@@ -631,11 +637,13 @@ template <class T, int VE, int LANES> __global__ void __launch_bounds__(kThreads
     if (t + 1 >= a.tiles) return;
     const int64_t c = ((unit % a.passes) * LANES + lane) * VE, room = a.dim - c;
     const int64_t beg = t * a.tile, next = beg + a.tile;
-    const uint32_t run = a.key[next], end_key = a.key[next - 1], beg_key = a.key[beg], before = t > 0 ? a.key[beg - 1] : ~0u;
+    const uint32_t run = a.key[next], end_key = a.key[next - 1], beg_key = a.key[beg], before = t > 0
+        ? a.key[beg - 1] : ~0u;
     if (run >= static_cast<uint32_t>(a.rows) || end_key != run) return;
     if (beg_key == run && before == run) return;  // it began earlier
     const int64_t over = lower<LANES>(a.key, next, a.cap, run + 1);
-    const int64_t tiles = ceil_div(over, a.tile), head = a.tiles > kFewTiles ? min(tiles, ceil_div(t + 1, kGroup) * kGroup) : tiles;
+    const int64_t tiles = ceil_div(over, a.tile), head = a.tiles > kFewTiles ? min(tiles, ceil_div(t + 1,
+            kGroup) * kGroup) : tiles;
     const int64_t whole = max(head, over / (a.tile * kGroup) * kGroup);  // groups up to there are spanned
     row::Vec<float, VE> x;
     x.load_upto(a.last + t * a.dim + c, room);
@@ -688,7 +696,8 @@ gnn_status launch_embed_fwd(const void *table, int tdt, int64_t rows, int64_t di
             const int64_t units = ceil_div(cap, int64_t(64 / LANES)) * a.passes;
             auto go = [&](auto at_once) {
                 constexpr int UNITS = decltype(at_once)::value;
-                const unsigned grid = static_cast<unsigned>(std::min<int64_t>(ceil_div(units, int64_t(UNITS * kWaves)), 1 << 20));
+                const unsigned grid = static_cast<unsigned>(std::min<int64_t>(ceil_div(units,
+                        int64_t(UNITS * kWaves)), 1 << 20));
                 embed_fwd_kernel<decltype(ti), decltype(to), VE, LANES, UNITS><<<grid, kThreads, 0, s>>>(a);
             };
             if (units <= kFewUnits) go(std::integral_constant<int, 2>{});
@@ -733,7 +742,8 @@ gnn_status launch_embed_bwd(const void *g, int gdt, const int64_t *ids, const in
     // a workgroup of zeros: 24 KB where most stretches have no named row (113,538 x 1,024 in fp32
     // for three ids 91 us, with 64 or 160 KB 103), else 64 (262,144 ids of 131,072 x 2,048 401 us, with 24 KB 409)
     const int64_t stretch = cap < rows / 8 ? 24 << 10 : 64 << 10;
-    a.zero_rows = std::max<int64_t>(1, std::min<int64_t>(kThreads, stretch / (dim * static_cast<int64_t>(dtype_size(ddt)))));
+    a.zero_rows = std::max<int64_t>(1, std::min<int64_t>(kThreads,
+                                                         stretch / (dim * static_cast<int64_t>(dtype_size(ddt)))));
     const int64_t zero_blocks = add ? 0 : ceil_div(rows, a.zero_rows);
     gnn_status st = GNN_OK;
     with_types(gdt, ddt, [&](auto tg, auto td, auto ve) {
@@ -763,7 +773,8 @@ gnn_status launch_embed_bwd(const void *g, int gdt, const int64_t *ids, const in
             st = launch_status("embed_sum");
             if (st != GNN_OK || a.tiles < 2) return;
             if (a.tiles > kFewTiles) {
-                const int64_t groups = ceil_div(ceil_div(a.tiles / kGroup, int64_t(64 / LANES)) * a.passes, int64_t(kWaves));
+                const int64_t groups = ceil_div(ceil_div(a.tiles / kGroup, int64_t(64 / LANES)) * a.passes,
+                                                int64_t(kWaves));
                 embed_group_kernel<VE, LANES><<<static_cast<unsigned>(groups), kThreads, 0, s>>>(a);
                 st = launch_status("embed_group");
                 if (st != GNN_OK) return;
