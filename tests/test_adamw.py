@@ -382,7 +382,7 @@ P = (ctypes.addressof(BUF) + 255) // 256 * 256  # any address: a refused call re
     (dict(sdt=3, t=dict(v_scale=P + 2)), gnn.GNN_EINVAL, "misaligned"),
 ])
 def test_refusals(change, code, what):
-    t = dict(w=P, g=P + 1024, m=P + 2048, v=P + 3072, m_scale=P + 4096, v_scale=P + 4160, shadow=None, n=10, weight_decay=0.0,
+    t = dict(w=P, g=P + 1024, m=P + 2048, v=P + 3200, m_scale=P + 4096, v_scale=P + 4160, shadow=None, n=10, weight_decay=0.0,
              gdt=0) | change.pop("t", {})
     tensors = (gnn.AdamwTensor * 2)(gnn.AdamwTensor(n=0), gnn.AdamwTensor(*t.values()))
     a = dict(tensors=tensors, count=2, sdt=0, lr=0.1, b1=0.9, b2=0.99, eps=1e-8, step=1, lr_dev=None, step_dev=None, seed=0) | change

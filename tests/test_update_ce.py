@@ -364,7 +364,7 @@ P = (ctypes.addressof(BUF) + 255) // 256 * 256  # any address: a refused call re
 ])
 def test_refusals(change, code, what):
     a = dict(a=P, adt=0, b=4, k=8, wt=P + 1024, wdt=0, bias=None, c=10, labels=P, targets=None, scale=None, gemm=0, row=None, loss=P + 4096,
-             d_a=P + 2048, gdt=0, dwt=P + 3072, dwdt=0, db=None, ws=P, bytes=1 << 40) | change
+             d_a=P + 2048, gdt=0, dwt=P + 3200, dwdt=0, db=None, ws=P, bytes=1 << 40) | change
     got = gnn.lib().gnn_update_ce(*a.values(), None)
     assert got == code and what in gnn.lib().gnn_last_error().decode()
 
